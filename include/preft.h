@@ -124,7 +124,8 @@ enum { PREFT_F32 = 0, PREFT_BF16 = 1 };
 enum {
     PREFT_OK           =  0,
     PREFT_EINVAL       = -1,   /* null pointer, negative size, bad enum, ld < width      */
-    PREFT_EUNSUPPORTED = -2,   /* rank outside 1..PREFT_MAX_RANK                         */
+    PREFT_EUNSUPPORTED = -2,   /* rank outside 1..PREFT_MAX_RANK; attention: head_dim or   */
+                               /* page_size that is not offered                          */
     PREFT_EALIGN       = -3,   /* base pointer or row stride not 16-byte aligned, or a   */
                                /* width that is not a multiple of 16 bytes               */
     PREFT_EWORKSPACE   = -4,   /* workspace missing, misaligned or too small             */
@@ -133,12 +134,14 @@ enum {
     PREFT_ESCHEDULE    = -7,   /* preft_schedule_counts: an apply call found a schedule  */
                                /* built for another T, S, N or position set, and did nothing */
     PREFT_ETOOLARGE    = -8    /* preft_direft_apply_static: the batch's schedule does   */
-                               /* not fit the static area                                */
+                               /* not fit the static area; attention: T * n_heads of     */
+                               /* 2^30 and more                                          */
 };
 
 #define PREFT_MAX_RANK 128
 #define PREFT_MAX_LAYERS 1024      /* residual streams per preft_direft_apply_layers call */
 #define PREFT_MAX_PACKED 3      /* projections one packed call may fuse */
+#define PREFT_MAX_HEADS 1024       /* query heads of an attention call */
 #define PREFT_MAX_PARTS 32      /* matrices per adapter a slot manager may hold */
 
 /*
@@ -396,6 +399,87 @@ int preft_slots_acquire(preft_slots_t *m, const int32_t *adapter_ids, int32_t n,
 const void *const *preft_slots_pool(preft_slots_t *m, int32_t part);
 int32_t preft_slots_resident(const preft_slots_t *m, int32_t adapter);
 int preft_slots_stats(const preft_slots_t *m, int64_t *stats);
+
+/*
+ * Attention of an engine step, between the q, k, v projections and the o projection that the apply calls edit: the pages
+ * that keys and values are kept in, and the two calls that read them.  A step makes them in this order, the first once and the others in every layer:
+ *
+ *   preft_kv_plan           extends the requests' block tables and names a slot for every row of the batch;
+ *   preft_kv_store          writes the rows' keys and values to their slots;
+ *   preft_prompt_attention  causal attention over whole prompts, from the batch's own keys and values;
+ *   preft_cached_attention  attention of the other rows -- decode tokens, tokens proposed ahead, further chunks of a prompt --
+ *                           over the pages, where requests of one adapter may share a long prefix.
+ *
+ * The batch is that of the apply calls: seg_start and seg_prefill_len as above.  Types: PREFT_BF16 and PREFT_F32, one for all tensors of a call.
+ * Heads: n_heads query heads, n_kv_heads key/value heads, n_heads a multiple of n_kv_heads (query head h reads key/value head
+ * h / (n_heads / n_kv_heads)), at most PREFT_MAX_HEADS; head_dim 64 or 128.  Rows of q, k, v and out hold their heads one after the other, and may be column
+ * ranges of a wider buffer (a fused qkv output): ld is the distance of rows in elements, at most 2^20, 16-byte aligned like the base.
+ *
+ * Cache: [n_pages, n_kv_heads, page_size, head_dim], contiguous, one for keys and one for values; page_size a power of two, 8..1024.
+ * slot = page * page_size + position in the page.  Block tables: block_table[s * ld_table + i] is the page of tokens i * page_size .. of request s.
+ *
+ * As in the apply calls everything is enqueued on `stream`, nothing is allocated or synchronised, launch sizes follow from host-visible sizes,
+ * and contents of device tables are not validated: positions, pages and rows are clamped to what exists, so that a malformed table gives unspecified results,
+ * never an access out of range.
+ *
+ * preft_kv_plan: ctx_len[s] tokens of request s are in the cache, and its seg_start[s + 1] - seg_start[s] rows follow them.  For all rows t,
+ *   positions[t]  the row's position in its request (for rotary embeddings),
+ *   slot_map[t]   its slot, or -1 where there is no page for it,
+ * for all requests kv_len[s] = ctx_len[s] + rows, and in block_table [S, max_pages] the entries of pages that the step begins: request after request they are
+ * free_pages[0], [1], ... (n_free of them).  Entries of pages that hold earlier tokens are read, no other entry is touched.  counts[0]: pages taken from free_pages;
+ * counts[1]: pages that were needed and not there (free_pages exhausted, or more than max_pages of a request) -- where it is not 0, entries of missing pages are
+ * -1 (up to max_pages) and so are the slots of their rows.  Nothing is consumed: the caller takes counts[0] pages off its list, and a call that is repeated writes the same.
+ * With S = 0 (then T must be 0) nothing is written.
+ *
+ * preft_kv_store: k and v [T, n_kv_heads * head_dim] to the slots of slot_map[T]; rows whose slot is outside the cache (-1) are skipped.  Two rows with
+ * one slot: either is kept.  k, v and the caches must not overlap.
+ */
+int preft_kv_plan(int64_t *slot_map, int32_t *positions, int32_t *kv_len, int32_t *block_table, int64_t ld_table,
+                  int32_t max_pages, int32_t *counts, const int32_t *seg_start, const int32_t *ctx_len,
+                  int32_t S, int32_t T, const int32_t *free_pages, int32_t n_free, int32_t page_size, void *stream);
+
+int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_size,
+                   const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t T,
+                   int32_t n_kv_heads, int32_t head_dim, const int64_t *slot_map, int dtype, void *stream);
+
+/*
+ * out[t, h] = sum_j p_j v[j, h'] / sum_j p_j,  p_j = exp(scale q[t, h] . k[j, h']), over the keys j that row t sees.
+ *
+ * preft_prompt_attention: the rows of a whole prompt, the first seg_prefill_len[s] of segment s; row i sees rows 0..i of its segment.
+ * The other rows of out are neither read nor written, and the other rows of q, k and v are not looked at.
+ *
+ * preft_cached_attention: the other rows -- those after the first seg_prefill_len[s] of segment s, or every row where seg_prefill_len is NULL.
+ * With r of them in segment s, row i = 0..r-1 sees the first kv_len[s] - (r - 1 - i) tokens of the request, in the pages of its block table (the rows' own keys
+ * are stored before).  A row that sees no token gets zeros.
+ * Groups (n_groups may be 0, the tables then NULL): segments group_start[g] .. group_start[g + 1] - 1 have their first group_prefix_len[g] tokens in the same
+ * pages, or in copies that hold the same values; their keys are then read once for the rows of all of them, from the first member's table.  group_start[n_groups + 1] does not decrease; segments
+ * outside [group_start[0], group_start[n_groups]) are in no group.  The result is that of the call without groups, to rounding.
+ *
+ * Products are accumulated, and the softmax is computed, in fp32; in bf16 the weights p are rounded to bf16 for the product with v, and each output is
+ * rounded once.  What a row does not see does not reach it, infinities and NaN included.  scale must be positive and finite.
+ * out must not overlap q, k, v or the caches, except that column ranges of one buffer may be side by side.  Two calls with the same arguments give the same bits.
+ *
+ * The workspace (16-byte aligned, preft_attention_workspace_bytes) holds the call's schedule and the parts of rows whose keys are divided among workgroups.
+ * The schedule depends on the tables, T, S, the numbers of heads and the kind of call: with mode PREFT_SCHEDULE_READY (else 0) a call takes the one that the
+ * last call of its kind left in the workspace, as the layers of a step do.  A call that names other sizes than that schedule's does nothing and
+ * marks the workspace, which preft_schedule_counts reports as PREFT_ESCHEDULE (its counts are then those of work units, of joined tiles and of all tiles).
+ * preft_attention_workspace_bytes returns 0 for sizes that the calls refuse.
+ */
+size_t preft_attention_workspace_bytes(int32_t T, int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                       int32_t n_groups);
+
+int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, const void *k, int64_t ldk,
+                           const void *v, int64_t ldv, int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const int32_t *seg_start, const int32_t *seg_prefill_len, int32_t S,
+                           float scale, int dtype, int mode, void *workspace, size_t workspace_bytes, void *stream);
+
+int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, int32_t T,
+                           int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const int32_t *seg_start, const int32_t *seg_prefill_len, const int32_t *kv_len, int32_t S,
+                           const void *k_cache, const void *v_cache, int32_t n_pages, int32_t page_size,
+                           const int32_t *block_table, int64_t ld_table, int32_t max_pages,
+                           const int32_t *group_start, const int32_t *group_prefix_len, int32_t n_groups,
+                           float scale, int dtype, int mode, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Copies the schedule counters of a workspace to the host: counts[0] = multi-row work

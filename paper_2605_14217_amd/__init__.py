@@ -1,4 +1,5 @@
-"""MI355X-native prefill-only adapter apply (segmented multi-adapter LoRA, DiReFT and LoReFT).
+"""MI355X-native prefill-only adapter apply (segmented multi-adapter LoRA, DiReFT and LoReFT), and the attention
+side of the same engine step (pages of the key/value cache, prompt attention, attention over the pages).
 
 The compute lives in ``libpreft.so`` (hand-written HIP for gfx950, C ABI declared in
 ``include/preft.h``); this package is the thin Python binding with the same names.
@@ -14,4 +15,6 @@ from .binding import (  # noqa: F401
     preft_schedule_counts, preft_strerror, preft_version, preft_workspace_bytes, preft_workspace_bytes_z,
     new_workspace, preft_slots_create, preft_slots_destroy, preft_slots_store, preft_slots_acquire,
     preft_slots_pool, preft_slots_resident, preft_slots_stats, PREFT_ECAPACITY,
+    preft_kv_plan, preft_kv_store, preft_prompt_attention, preft_cached_attention, preft_attention_workspace_bytes,
+    new_attention_workspace,
 )

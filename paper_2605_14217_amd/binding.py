@@ -75,7 +75,8 @@ ABI_SYMBOLS = ("preft_workspace_bytes", "preft_workspace_bytes_z", "preft_schedu
                "preft_direft_apply", "preft_direft_apply_static", "preft_direft_apply_layers",
                "preft_loreft_prepare", "preft_loreft_apply", "preft_slots_create", "preft_slots_destroy",
                "preft_slots_store", "preft_slots_acquire", "preft_slots_pool", "preft_slots_resident",
-               "preft_slots_stats", "preft_schedule_counts", "preft_strerror", "preft_version")
+               "preft_slots_stats", "preft_kv_plan", "preft_kv_store", "preft_attention_workspace_bytes",
+               "preft_prompt_attention", "preft_cached_attention", "preft_schedule_counts", "preft_strerror", "preft_version")
 
 _lib = None
 _native = None                                                # _marshal, bound to _lib's entry points
@@ -141,6 +142,18 @@ def load_library(path: Optional[str] = None):
     lib.preft_slots_resident.argtypes = [vp, i32]
     lib.preft_slots_stats.restype = c.c_int
     lib.preft_slots_stats.argtypes = [vp, c.POINTER(i64)]
+    lib.preft_kv_plan.restype = c.c_int
+    lib.preft_kv_plan.argtypes = [vp, vp, vp, vp, i64, i32, vp, vp, vp, i32, i32, vp, i32, i32, vp]
+    lib.preft_kv_store.restype = c.c_int
+    lib.preft_kv_store.argtypes = [vp, vp, i32, i32, vp, i64, vp, i64, i32, i32, i32, vp, c.c_int, vp]
+    lib.preft_attention_workspace_bytes.restype = sz
+    lib.preft_attention_workspace_bytes.argtypes = [i32] * 6
+    lib.preft_prompt_attention.restype = c.c_int
+    lib.preft_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, i32, c.c_float, c.c_int, c.c_int,
+                                           vp, sz, vp]
+    lib.preft_cached_attention.restype = c.c_int
+    lib.preft_cached_attention.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp, i64, i32, vp, vp, i32,
+                                           c.c_float, c.c_int, c.c_int, vp, sz, vp]
     lib.preft_schedule_counts.restype = c.c_int
     lib.preft_schedule_counts.argtypes = [vp, c.POINTER(i32), vp]
     lib.preft_strerror.restype = c.c_char_p
@@ -169,6 +182,8 @@ def _load_marshal(lib):
     _marshal.bind(PoolRef, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.preft_schedule, lib.preft_lora_apply, lib.preft_lora_apply_packed, lib.preft_direft_apply, lib.preft_loreft_apply,
         lib.preft_direft_apply_layers)))
+    _marshal.bind_attention(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.preft_kv_plan, lib.preft_kv_store, lib.preft_prompt_attention, lib.preft_cached_attention)))
     return _marshal
 
 
@@ -531,3 +546,132 @@ def preft_slots_stats(handle: int) -> dict:
     _check(load_library().preft_slots_stats(handle, out), "preft_slots_stats")
     return dict(hits=int(out[0]), misses=int(out[1]), evictions=int(out[2]), bytes_copied=int(out[3]),
                 n_slots=int(out[4]))
+
+
+# ----------------------------------------------------------------------------------------
+# key/value pages and attention
+# ----------------------------------------------------------------------------------------
+def preft_attention_workspace_bytes(T: int, S: int, n_heads: int, n_kv_heads: int, head_dim: int, n_groups: int = 0) -> int:
+    return int(load_library().preft_attention_workspace_bytes(int(T), int(S), int(n_heads), int(n_kv_heads), int(head_dim), int(n_groups)))
+
+
+def new_attention_workspace(T: int, S: int, n_heads: int, n_kv_heads: int, head_dim: int, n_groups: int = 0, device="cuda") -> torch.Tensor:
+    """Caller-owned workspace of the attention calls of a batch of T rows in S segments and n_groups groups."""
+    n = preft_attention_workspace_bytes(T, S, n_heads, n_kv_heads, head_dim, n_groups)
+    if n == 0:
+        raise ValueError("no attention call takes these sizes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _block_table(t: torch.Tensor, S: int):
+    if t.dim() != 2 or t.dtype is not _INT32 or not t.is_cuda or t.shape[0] != S or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"block_table: need an int32 device tensor of {S} rows with unit column stride")
+    return t.data_ptr(), t.stride(0) if S > 1 else t.shape[1], t.shape[1]
+
+
+def _cache(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None):
+    if t.dim() != 4 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous device tensor [n_pages, n_kv_heads, page_size, head_dim]")
+    if like is not None and (t.shape != like.shape or t.dtype is not like.dtype):
+        raise ValueError("k_cache and v_cache must agree in shape and dtype")
+    return t.data_ptr()
+
+
+def preft_kv_plan(slot_map: torch.Tensor, positions: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, counts: torch.Tensor,
+                  seg_start: torch.Tensor, ctx_len: torch.Tensor, free_pages: torch.Tensor, page_size: int, stream=None) -> None:
+    """Slots and positions of the batch's rows, the requests' new lengths and the new entries of their block tables.  counts (2 values): pages
+    taken from free_pages, pages that were missing."""
+    if _native is not None:
+        rc = _native.kv_plan(slot_map, positions, kv_len, block_table, counts, seg_start, ctx_len, free_pages, page_size, _native_stream(stream))
+        if rc is not None:
+            return _check(rc, "preft_kv_plan")
+    S, T = int(ctx_len.numel()), int(slot_map.numel())
+    if slot_map.dtype is not _INT64 or not slot_map.is_cuda or not slot_map.is_contiguous():
+        raise ValueError("slot_map: need a contiguous int64 device tensor")
+    table, ld, max_pages = _block_table(block_table, S)
+    n_free = int(free_pages.numel())
+    rc = load_library().preft_kv_plan(
+        slot_map.data_ptr(), _table(positions, "positions", T), _table(kv_len, "kv_len", S), table, ld, max_pages, _table(counts, "counts", 2),
+        _table(seg_start, "seg_start", S + 1), _table(ctx_len, "ctx_len", S), S, T, _table(free_pages, "free_pages", n_free), n_free,
+        int(page_size), _stream(stream))
+    _check(rc, "preft_kv_plan")
+
+
+def preft_kv_store(k_cache: torch.Tensor, v_cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, stream=None) -> None:
+    """k and v ([T, n_kv_heads * head_dim], also columns of a wider tensor) to the slots of slot_map; a row whose slot is -1 is skipped."""
+    if _native is not None:
+        rc = _native.kv_store(k_cache, v_cache, k, v, slot_map, _native_stream(stream))
+        if rc is not None:
+            return _check(rc, "preft_kv_store")
+    kc, vc = _cache(k_cache, "k_cache"), _cache(v_cache, "v_cache", k_cache)
+    n_pages, heads, page, dim = k_cache.shape
+    kp, ldk, T, width = _matrix(k, "k")
+    vp, ldv, T2, width2 = _matrix(v, "v")
+    if T2 != T or width != heads * dim or width2 != width or k.dtype is not k_cache.dtype or v.dtype is not k_cache.dtype:
+        raise ValueError("k and v must agree in rows, and with the caches in heads, head size and dtype")
+    if slot_map.dtype is not _INT64 or slot_map.numel() != T or not slot_map.is_cuda or not slot_map.is_contiguous():
+        raise ValueError(f"slot_map: need a contiguous int64 device tensor of {T} entries")
+    rc = load_library().preft_kv_store(kc, vc, n_pages, page, kp, ldk, vp, ldv, T, heads, dim, slot_map.data_ptr(), _dtype_code(k_cache),
+                                       _stream(stream))
+    _check(rc, "preft_kv_store")
+
+
+def preft_prompt_attention(out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seg_start: torch.Tensor,
+                           seg_prefill_len: torch.Tensor, n_heads: int, n_kv_heads: int, scale: float, mode: int, workspace: torch.Tensor,
+                           stream=None) -> None:
+    """Causal attention of the first seg_prefill_len rows of every segment over themselves.  out and q: [T, n_heads * head_dim]; k and v:
+    [T, n_kv_heads * head_dim]; other rows are left as they are.  mode: 0, or PREFT_SCHEDULE_READY."""
+    if _native is not None:
+        rc = _native.prompt_attention(out, q, k, v, seg_start, seg_prefill_len, n_heads, n_kv_heads, scale, mode, workspace, _native_stream(stream))
+        if rc is not None:
+            return _check(rc, "preft_prompt_attention")
+    op, ldo, T, width = _matrix(out, "out")
+    qp, ldq, T1, width1 = _matrix(q, "q")
+    kp, ldk, T2, width2 = _matrix(k, "k")
+    vp, ldv, T3, width3 = _matrix(v, "v")
+    heads, kv_heads = int(n_heads), int(n_kv_heads)
+    dim = width // heads if heads > 0 else 0
+    if not T == T1 == T2 == T3 or not (q.dtype is out.dtype and k.dtype is out.dtype and v.dtype is out.dtype):
+        raise ValueError("out, q, k and v must agree in rows and dtype")
+    if dim * heads != width or width1 != width or width2 != kv_heads * dim or width3 != width2:
+        raise ValueError("out and q must have n_heads heads, k and v n_kv_heads of the same size")
+    S = int(seg_prefill_len.numel())
+    rc = load_library().preft_prompt_attention(
+        op, ldo, qp, ldq, kp, ldk, vp, ldv, T, heads, kv_heads, dim, _table(seg_start, "seg_start", S + 1),
+        _table(seg_prefill_len, "seg_prefill_len", S), S, float(scale), _dtype_code(out), int(mode), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(rc, "preft_prompt_attention")
+
+
+def preft_cached_attention(out: torch.Tensor, q: torch.Tensor, seg_start: torch.Tensor, seg_prefill_len: Optional[torch.Tensor],
+                           kv_len: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                           group_start: Optional[torch.Tensor], group_prefix_len: Optional[torch.Tensor], n_heads: int, scale: float, mode: int,
+                           workspace: torch.Tensor, stream=None) -> None:
+    """Attention of the rows after the first seg_prefill_len of every segment (None: of every row) over the pages of their requests: row i of r
+    sees the first kv_len - (r - 1 - i) tokens.  group_start and group_prefix_len: runs of segments that share their first tokens (None: none do)."""
+    if _native is not None:
+        rc = _native.cached_attention(out, q, seg_start, seg_prefill_len, kv_len, k_cache, v_cache, block_table, group_start, group_prefix_len,
+                                      n_heads, scale, mode, workspace, _native_stream(stream))
+        if rc is not None:
+            return _check(rc, "preft_cached_attention")
+    op, ldo, T, width = _matrix(out, "out")
+    qp, ldq, T1, width1 = _matrix(q, "q")
+    kc, vc = _cache(k_cache, "k_cache"), _cache(v_cache, "v_cache", k_cache)
+    n_pages, kv_heads, page, dim = k_cache.shape
+    heads = int(n_heads)
+    if T1 != T or q.dtype is not out.dtype or k_cache.dtype is not out.dtype:
+        raise ValueError("out, q and the caches must agree in rows and dtype")
+    if width != heads * dim or width1 != width:
+        raise ValueError("out and q must have n_heads heads of the caches' size")
+    S = int(kv_len.numel())
+    table, ld, max_pages = _block_table(block_table, S)
+    if (group_start is None) != (group_prefix_len is None):
+        raise ValueError("group_start and group_prefix_len go together")
+    n_groups = 0 if group_prefix_len is None else int(group_prefix_len.numel())
+    rc = load_library().preft_cached_attention(
+        op, ldo, qp, ldq, T, heads, kv_heads, dim, _table(seg_start, "seg_start", S + 1),
+        None if seg_prefill_len is None else _table(seg_prefill_len, "seg_prefill_len", S), _table(kv_len, "kv_len", S), S, kc, vc, n_pages, page,
+        table, ld, max_pages, None if n_groups == 0 else _table(group_start, "group_start", n_groups + 1),
+        None if n_groups == 0 else _table(group_prefix_len, "group_prefix_len", n_groups), n_groups, float(scale), _dtype_code(out), int(mode),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(rc, "preft_cached_attention")

@@ -18,11 +18,12 @@ HIPCC_FLAGS = [
 
 
 def sources():
-    """preft_api.hip (the C ABI, the launch logic and the few kernels it instantiates itself), slots.hip, and
-    the kernel instantiations of csrc/instances/ (written by csrc/gen_instances.py)."""
+    """preft_api.hip (the C ABI of the apply calls, the launch logic and the few kernels it instantiates itself), slots.hip,
+    kv_pages.hip and attention.hip (pages and attention, each with its entry points), and the kernel instantiations of
+    csrc/instances/ (written by csrc/gen_instances.py)."""
     inst = os.path.join(CSRC, "instances")
     groups = sorted(os.path.join(inst, n) for n in os.listdir(inst) if n.endswith(".hip")) if os.path.isdir(inst) else []
-    return [os.path.join(CSRC, "preft_api.hip"), os.path.join(CSRC, "slots.hip")] + groups
+    return [os.path.join(CSRC, n) for n in ("preft_api.hip", "slots.hip", "kv_pages.hip", "attention.hip")] + groups
 
 
 def built_for() -> str:

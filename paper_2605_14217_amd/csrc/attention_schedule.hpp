@@ -1,0 +1,307 @@
+// Schedule of an attention call: segment tables -> work units (a tile of query columns and a range of keys) and merges.
+//
+// The columns of a segment are its (row, query head of the key/value head) pairs, column c = row * G + head: G query heads share every key that is
+// read, and a decode row fills G columns of a tile instead of one.  Units are cut into tiles of 128 columns, and along the keys into ranges of
+// about total / TARGET each where there are too few tiles to fill the chip; the ranges' parts are joined by the merge kernel.
+// Rows of a group see their shared first keys through units of the group, which carry the rows of all its members.
+#pragma once
+#include "common.hpp"
+#include "block_scan.hpp"
+
+namespace preft {
+
+constexpr int ATTN_COLS      = 128;   // columns of a unit (four wavefronts of 32)
+constexpr int ATTN_FEW_COLS  = 32;    // up to here the four wavefronts of a unit share the keys instead
+constexpr int ATTN_KEYS      = 64;    // keys of a tile
+constexpr int ATTN_TARGET    = 512;   // workgroups that run side by side: two on each of 256 compute units
+constexpr int ATTN_GROUP_ROWS = 4096; // rows of groups that are listed; the rest see their prefix by themselves
+constexpr int ATTN_MIN_PREFIX = 64;   // shorter prefixes are not worth a part of their own
+constexpr int ATTN_SCAN      = 4096;  // items whose tile offsets are kept in LDS
+
+struct AttnUnit {
+    int32_t table;     // row of the block table; packed keys: the row of key 0
+    int32_t col0;      // first column within the item
+    int32_t ncols;     // 1..ATTN_COLS
+    int32_t key0, key1;
+    int32_t row0;      // batch row of the item's row 0; a group: -1 - (its first entry in the row list)
+    int32_t lim0;      // row i of the item sees keys below lim0 + i
+    int32_t slot;      // first part column, head-major; -1: the unit writes the result
+};
+struct AttnMerge {
+    int32_t row0, col0, ncols;
+    int32_t parts, slot;                                   // of the segment's own keys
+    int32_t group_parts, group_slot, group_col0, group_cols;
+    int32_t pad[3];
+};
+
+struct AttnLists {
+    int32_t   *header;     // HEADER_INTS ints, laid out as the adapter schedule's where they mean the same
+    AttnUnit  *units;
+    AttnMerge *merges;
+    int2      *group_rows; // {batch row, keys it sees}
+    int32_t   *tiles;      // [S + groups + 1] first column tile of every item
+    int32_t   *rows_before;// [S + 1]
+    int32_t   *group_of;   // [S]
+    int32_t   *group_list; // [groups] first entry in group_rows, or -1
+    int32_t   *group_slot; // [groups] first part column of the group's units
+    float     *part_o;     // [slots][head_dim]
+    float2    *part_ml;    // [slots] {largest exponent, sum}
+    int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
+};
+
+constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9;
+
+struct AttnScheduleArgs {
+    const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
+    const int32_t *kv_len;                                 // null: packed whole prompts
+    const int32_t *group_start, *group_prefix;
+    int32_t S, T, n_groups, heads, kv_heads, max_keys, can_split, min_tiles;
+    AttnLists l;
+};
+
+struct AttnItem { int32_t row0, rows, lim0, key0, key1; };
+
+__device__ __forceinline__ AttnItem attn_segment(const AttnScheduleArgs &a, int32_t s)
+{
+    AttnItem r;
+    const int32_t lo = max(0, min(a.seg_start[s], a.T)), hi = max(lo, min(a.seg_start[s + 1], a.T));
+    const int32_t prompt = a.seg_prefill_len ? max(0, min(a.seg_prefill_len[s], hi - lo)) : 0;
+    if (a.kv_len) {
+        const int32_t kv = max(0, min(a.kv_len[s], a.max_keys));
+        r.row0 = lo + prompt;
+        r.rows = hi - r.row0;
+        r.lim0 = kv - r.rows + 1;
+        r.key1 = kv;
+    } else {
+        r.row0 = lo;
+        r.rows = prompt;
+        r.lim0 = 1;
+        r.key1 = prompt;
+    }
+    r.key0 = 0;
+    return r;
+}
+
+__device__ __forceinline__ int32_t ceil_div(int32_t a, int32_t b) { return (int32_t)(((int64_t)a + b - 1) / b); }
+__device__ __forceinline__ int32_t key_tiles(int32_t key0, int32_t key1) { return key1 > key0 ? (key1 - 1) / ATTN_KEYS - key0 / ATTN_KEYS + 1 : 0; }
+
+__device__ __forceinline__ int32_t ranges_of(int32_t tiles, int32_t range) { return tiles > range ? ceil_div(tiles, range) : 1; }
+
+struct AttnGroup { int32_t begin, end, rows, prefix; };
+
+__device__ __forceinline__ AttnGroup attn_group(const AttnScheduleArgs &a, int32_t g)
+{
+    AttnGroup m;
+    m.begin = max(0, min(a.group_start[g], a.S));
+    m.end = max(m.begin, min(a.group_start[g + 1], a.S));
+    m.rows = a.l.rows_before[m.end] - a.l.rows_before[m.begin];
+    m.prefix = max(0, min(a.group_prefix[g], a.max_keys));
+    return m;
+}
+
+// last i of [0, n) with first[i] <= x; first[0] <= x
+template <typename P>
+__device__ __forceinline__ int32_t last_at_or_before(P first, int32_t n, int32_t x)
+{
+    int32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (first[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// One workgroup: the lists are a few kilobytes, and what a step waits for is the chain of reads and barriers, not the work.
+// Units stand in the order of falling cost (counting sort over 256 cost classes): the longest of a causal prompt begin first and the short ones
+// fill the ends.  Their order does not change a result: every unit has an output or part of its own.
+__global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnScheduleArgs a)
+{
+    __shared__ int32_t lds[32];
+    __shared__ int32_t first_tile[ATTN_SCAN + 1];
+    __shared__ int32_t bins[256];
+    __shared__ int32_t n_units, n_merges, n_slots;
+    __shared__ unsigned long long cost_sum;
+    const int tid = threadIdx.x, nt = blockDim.x;
+    const int32_t G = a.heads / a.kv_heads, items = a.S + a.n_groups;
+    const bool in_lds = items <= ATTN_SCAN;
+    if (tid == 0) { n_merges = 0; n_slots = 0; cost_sum = 0; }
+    for (int b = tid; b < 256; b += nt) bins[b] = 0;
+
+    // groups: how many rows each has, and where they stand in the row list
+    if (a.n_groups > 0) {
+        int32_t carry = 0;
+        for (int32_t s0 = 0; s0 < a.S; s0 += nt) {
+            const int32_t s = s0 + tid;
+            int32_t total;
+            const int32_t rows = s < a.S ? attn_segment(a, s).rows : 0;
+            const int32_t before = block_exclusive_scan(rows, lds, &total);
+            if (s < a.S) a.l.rows_before[s] = carry + before;
+            carry += total;
+        }
+        if (tid == 0) a.l.rows_before[a.S] = carry;
+        __syncthreads();
+        carry = 0;
+        for (int32_t g0 = 0; g0 < a.n_groups; g0 += nt) {
+            const int32_t g = g0 + tid;
+            int32_t rows = 0, total;
+            if (g < a.n_groups) {
+                const AttnGroup m = attn_group(a, g);
+                rows = m.prefix >= ATTN_MIN_PREFIX && m.rows >= 2 ? m.rows : 0;
+            }
+            const int32_t before = block_exclusive_scan(rows, lds, &total);
+            const int64_t end = (int64_t)carry + before + rows;
+            if (g < a.n_groups) a.l.group_list[g] = rows > 0 && end <= a.l.group_row_cap ? carry + before : -1;
+            carry = (int32_t)min((int64_t)INT32_MAX / 2, (int64_t)carry + total);
+        }
+        __syncthreads();
+    }
+
+    // items: column tiles, and the work of all
+    int32_t carry = 0;
+    unsigned long long cost = 0;
+    for (int32_t i0 = 0; i0 < items; i0 += nt) {
+        const int32_t i = i0 + tid;
+        int32_t tiles = 0, total;
+        if (i < a.S) {
+            AttnItem it = attn_segment(a, i);
+            if (a.n_groups > 0) {
+                const int32_t g = last_at_or_before(a.group_start, a.n_groups, i);
+                const AttnGroup m = attn_group(a, g);
+                const bool in = m.begin <= i && i < m.end && a.l.group_list[g] >= 0;
+                a.l.group_of[i] = in ? g : -1;
+                if (in) {
+                    const int32_t at = a.l.group_list[g] + a.l.rows_before[i] - a.l.rows_before[m.begin];
+                    for (int32_t r = 0; r < it.rows; ++r)
+                        if (at + r < a.l.group_row_cap) a.l.group_rows[at + r] = make_int2(it.row0 + r, min(it.lim0 + r, m.prefix));
+                    it.key0 = m.prefix;
+                }
+            }
+            tiles = it.rows > 0 ? (int32_t)(((int64_t)it.rows * G + ATTN_COLS - 1) / ATTN_COLS) : 0;
+            // a causal prompt: tiles see half of the keys on average
+            if (tiles > 0) {
+                const int32_t low = min(it.key1, it.lim0 + (int32_t)(min((int64_t)it.rows * G, (int64_t)ATTN_COLS) - 1) / G);
+                cost += (unsigned long long)tiles * (unsigned)(key_tiles(it.key0, low) + key_tiles(it.key0, it.key1) + 1) / 2;
+            }
+        } else if (i < items) {
+            const int32_t g = i - a.S;
+            if (a.l.group_list[g] >= 0) {
+                const AttnGroup m = attn_group(a, g);
+                tiles = (int32_t)(((int64_t)m.rows * G + ATTN_COLS - 1) / ATTN_COLS);
+                cost += (unsigned long long)tiles * (unsigned)key_tiles(0, m.prefix);
+            }
+        }
+        const int32_t before = block_exclusive_scan(tiles, lds, &total);
+        if (i < items) {
+            if (in_lds) first_tile[i] = carry + before;
+            else a.l.tiles[i] = carry + before;
+        }
+        carry += total;
+    }
+    for (int off = 32; off > 0; off >>= 1) cost += __shfl_xor(cost, off, 64);
+    if ((tid & 63) == 0) atomicAdd(&cost_sum, cost);
+    __syncthreads();
+    const int32_t n_tiles = min(carry, a.l.tile_cap);
+    // a range of keys: no shorter than the whole work over the workgroups that run side by side
+    int32_t range = INT32_MAX;
+    if (a.can_split) {
+        const unsigned long long even = (cost_sum * (unsigned)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET;
+        range = max(a.min_tiles, (int32_t)min(even, (unsigned long long)INT32_MAX));
+    }
+    if (a.n_groups > 0) {                                  // a group's parts stand together, tile by tile: its members find them by their columns
+        int64_t base = 0;
+        for (int32_t g0 = 0; g0 < a.n_groups; g0 += nt) {
+            const int32_t g = g0 + tid;
+            int64_t need = 0;
+            if (g < a.n_groups && a.l.group_list[g] >= 0) {
+                const AttnGroup m = attn_group(a, g);
+                need = (int64_t)m.rows * G * a.kv_heads * ranges_of(key_tiles(0, m.prefix), range);
+            }
+            int32_t total;
+            const int32_t before = block_exclusive_scan((int32_t)min(need, (int64_t)a.l.slot_cap), lds, &total);
+            if (g < a.n_groups) a.l.group_slot[g] = (int32_t)min(base + before, (int64_t)INT32_MAX / 2);
+            base += total;
+        }
+        if (tid == 0) n_slots = (int32_t)min(base, (int64_t)INT32_MAX / 2);
+        __syncthreads();
+    }
+
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int32_t t = tid; t < n_tiles; t += nt) {
+            const int32_t i = in_lds ? last_at_or_before(first_tile, items, t) : last_at_or_before(a.l.tiles, items, t);
+            const int32_t tile = t - (in_lds ? first_tile[i] : a.l.tiles[i]);
+            AttnUnit u;
+            AttnItem it;
+            AttnGroup m = {0, 0, 0, 0};
+            int32_t g = -1, group_ranges = 0;
+            if (i < a.S) {
+                it = attn_segment(a, i);
+                if (a.n_groups > 0) g = a.l.group_of[i];
+                if (g >= 0) {
+                    m = attn_group(a, g);
+                    it.key0 = m.prefix;
+                    group_ranges = ranges_of(key_tiles(0, m.prefix), range);
+                }
+                u.table = a.kv_len ? i : it.row0;
+                u.row0 = it.row0; u.lim0 = it.lim0;
+            } else {
+                m = attn_group(a, i - a.S);
+                it.rows = m.rows; it.key0 = 0; it.key1 = m.prefix;
+                u.table = min(m.begin, a.S - 1);
+                u.row0 = -1 - a.l.group_list[i - a.S]; u.lim0 = 0;
+            }
+            u.col0 = tile * ATTN_COLS;
+            u.ncols = min(ATTN_COLS, it.rows * G - u.col0);
+            const int32_t key1 = i < a.S ? min(it.key1, it.lim0 + (u.col0 + u.ncols - 1) / G) : it.key1;
+            const int32_t n = key_tiles(it.key0, key1);
+            const int32_t splits = n == 0 && g >= 0 ? 0 : ranges_of(n, range);     // 0: the group's part is all there is
+            const bool parts = splits > 1 || g >= 0 || i >= a.S;
+            const int32_t each = splits > 0 ? n / splits : 0;
+            const int32_t cls = 255 - (each < 128 ? each : min(255, 128 + (each - 128) / 16));
+            if (pass == 0) {
+                if (splits > 0) atomicAdd(&bins[cls], splits);
+                continue;
+            }
+            int32_t at = splits > 0 ? atomicAdd(&bins[cls], splits) : 0;
+            int32_t slot = -1;
+            const int32_t step = u.ncols * a.kv_heads;
+            if (i >= a.S) slot = a.l.group_slot[i - a.S] + tile * ATTN_COLS * a.kv_heads * splits;
+            else if (parts) slot = atomicAdd(&n_slots, splits * step);
+            const bool fits = !parts || (slot >= 0 && (int64_t)slot + (int64_t)splits * step <= a.l.slot_cap);   // not so: the tables are malformed
+            for (int32_t k = 0; k < splits; ++k, ++at) {
+                const int32_t first = it.key0 / ATTN_KEYS;
+                const int64_t k0 = first + (int64_t)n * k / splits, k1 = first + (int64_t)n * (k + 1) / splits;
+                u.key0 = max(it.key0, (int32_t)(k0 * ATTN_KEYS));
+                u.key1 = max(u.key0, (int32_t)min((int64_t)key1, k1 * ATTN_KEYS));
+                u.slot = parts ? slot + k * step : -1;
+                if (!fits) { u.slot = 0; u.ncols = 0; }
+                if (at < a.l.unit_cap) a.l.units[at] = u;
+            }
+            if (parts && i < a.S && fits) {
+                AttnMerge j;
+                j.row0 = u.row0; j.col0 = u.col0; j.ncols = u.ncols; j.parts = splits; j.slot = slot;
+                j.group_parts = group_ranges; j.group_slot = g >= 0 ? a.l.group_slot[g] : 0;
+                j.group_col0 = g >= 0 ? (a.l.rows_before[i] - a.l.rows_before[m.begin]) * G + u.col0 : 0;
+                j.group_cols = m.rows * G;
+                j.pad[0] = j.pad[1] = j.pad[2] = 0;
+                const int32_t to = atomicAdd(&n_merges, 1);
+                if (to < a.l.merge_cap) a.l.merges[to] = j;
+            }
+        }
+        __syncthreads();
+        if (pass == 0) {
+            int32_t total;
+            const int32_t v = tid < 256 ? bins[tid] : 0;
+            const int32_t before = block_exclusive_scan(v, lds, &total);
+            if (tid < 256) bins[tid] = before;
+            if (tid == 0) n_units = min(total, a.l.unit_cap);
+            __syncthreads();
+        }
+    }
+    if (tid == 0) {
+        int32_t *h = a.l.header;
+        h[AH_UNITS] = n_units; h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
+        h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
+    }
+}
+
+}  // namespace preft

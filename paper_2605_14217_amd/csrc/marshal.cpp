@@ -19,6 +19,10 @@ decltype(&preft_lora_apply_packed) g_packed;
 decltype(&preft_direft_apply) g_direft;
 decltype(&preft_loreft_apply) g_loreft;
 decltype(&preft_direft_apply_layers) g_layers;
+decltype(&preft_kv_plan) g_plan;
+decltype(&preft_kv_store) g_store;
+decltype(&preft_prompt_attention) g_prompt;
+decltype(&preft_cached_attention) g_cached;
 
 const at::Tensor *tensor(PyObject *o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
 
@@ -263,6 +267,152 @@ PyObject *reft_layers(PyObject *, PyObject *const *o, Py_ssize_t n)
     });
 }
 
+struct Pages { int32_t *p, max_pages; int64_t ld; };
+
+// int32 device tensor of S rows, unit column stride
+bool as_block_table(PyObject *o, int32_t S, Pages &b)
+{
+    const at::Tensor *t = tensor(o);
+    if (!t || t->dim() != 2 || t->scalar_type() != at::kInt || !t->is_cuda() || t->size(0) != S || t->size(1) > INT32_MAX ||
+        (t->size(1) > 1 && t->stride(1) != 1)) return false;
+    b = {static_cast<int32_t *>(t->data_ptr()), (int32_t)t->size(1), S > 1 ? t->stride(0) : t->size(1)};
+    return true;
+}
+
+struct Cache { void *k, *v; int32_t n_pages, heads, page, dim; at::ScalarType type; };
+
+// contiguous device tensors [n_pages, n_kv_heads, page_size, head_dim]
+bool as_cache(PyObject *ko, PyObject *vo, Cache &c)
+{
+    const at::Tensor *k = tensor(ko), *v = tensor(vo);
+    if (!k || !v || k->dim() != 4 || !k->is_cuda() || !v->is_cuda() || !k->is_contiguous() || !v->is_contiguous() || k->sizes() != v->sizes() ||
+        k->scalar_type() != v->scalar_type()) return false;
+    for (int i = 0; i < 4; ++i)
+        if (k->size(i) > INT32_MAX) return false;
+    c = {k->data_ptr(), v->data_ptr(), (int32_t)k->size(0), (int32_t)k->size(1), (int32_t)k->size(2), (int32_t)k->size(3), k->scalar_type()};
+    return c.type == at::kBFloat16 || c.type == at::kFloat;
+}
+
+// entries of a one-dimensional table, or -1
+int64_t entries(PyObject *o)
+{
+    const at::Tensor *t = tensor(o);
+    return t && t->numel() < INT32_MAX ? t->numel() : -1;
+}
+
+// (slot_map, positions, kv_len, block_table, counts, seg_start, ctx_len, free_pages, page_size, stream)
+PyObject *kv_plan(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        if (n != 10 || !g_plan) return false;
+        const int64_t S = entries(o[6]), T = entries(o[0]), n_free = entries(o[7]);
+        int64_t *slots;
+        int32_t *positions, *kv_len, *counts, *start, *ctx, *free_pages, page;
+        Pages b;
+        void *stream;
+        if (S < 0 || T < 0 || n_free < 0 || !as_table(o[0], T, slots) || !as_table(o[1], T, positions) || !as_table(o[2], S, kv_len) ||
+            !as_block_table(o[3], (int32_t)S, b) || !as_table(o[4], 2, counts) || !as_table(o[5], S + 1, start) || !as_table(o[6], S, ctx) ||
+            !as_table(o[7], n_free, free_pages) || !as_int(o[8], page) || !as_stream(o[9], stream)) return false;
+        rc = without_gil([&] {
+            return g_plan(slots, positions, kv_len, b.p, b.ld, b.max_pages, counts, start, ctx, (int32_t)S, (int32_t)T, free_pages, (int32_t)n_free, page,
+                          stream);
+        });
+        return true;
+    });
+}
+
+// (k_cache, v_cache, k, v, slot_map, stream)
+PyObject *kv_store(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        Cache c;
+        Matrix k, v;
+        int64_t *slots;
+        void *stream;
+        if (n != 6 || !g_store || !as_cache(o[0], o[1], c) || !as_matrix(o[2], k) || !as_matrix(o[3], v) || k.rows != v.rows || k.cols != v.cols ||
+            k.cols != (int64_t)c.heads * c.dim || k.type != c.type || v.type != c.type || !as_table(o[4], k.rows, slots) || !as_stream(o[5], stream))
+            return false;
+        rc = without_gil([&] { return g_store(c.k, c.v, c.n_pages, c.page, k.p, k.ld, v.p, v.ld, k.rows, c.heads, c.dim, slots, dtype_of(c.type), stream); });
+        return true;
+    });
+}
+
+// scale, mode, workspace, stream
+struct Last { float scale; int32_t mode; void *workspace, *stream; size_t bytes; };
+
+bool as_last(PyObject *const *o, Last &l)
+{
+    const double scale = PyFloat_AsDouble(o[0]);
+    if (scale == -1.0 && PyErr_Occurred()) return false;
+    l.scale = (float)scale;
+    return as_int(o[1], l.mode) && as_workspace(o[2], l.workspace, l.bytes) && as_stream(o[3], l.stream);
+}
+
+// (out, q, k, v, seg_start, seg_prefill_len, n_heads, n_kv_heads, scale, mode, workspace, stream)
+PyObject *prompt_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        Matrix out, q, k, v;
+        int32_t heads, kv_heads, *start, *prefill;
+        Last l;
+        if (n != 12 || !g_prompt || !as_matrix(o[0], out) || !as_matrix(o[1], q) || !as_matrix(o[2], k) || !as_matrix(o[3], v)) return false;
+        const int64_t S = entries(o[5]);
+        if (S < 0 || !as_table(o[4], S + 1, start) || !as_table(o[5], S, prefill) || !as_int(o[6], heads) || !as_int(o[7], kv_heads) || !as_last(o + 8, l))
+            return false;
+        if (heads < 1 || kv_heads < 1 || out.cols % heads != 0 || q.cols != out.cols || k.cols != (int64_t)kv_heads * (out.cols / heads) ||
+            v.cols != k.cols || q.rows != out.rows || k.rows != out.rows || v.rows != out.rows || q.type != out.type || k.type != out.type ||
+            v.type != out.type) return false;
+        rc = without_gil([&] {
+            return g_prompt(out.p, out.ld, q.p, q.ld, k.p, k.ld, v.p, v.ld, out.rows, heads, kv_heads, out.cols / heads, start, prefill, (int32_t)S,
+                            l.scale, dtype_of(out.type), l.mode, l.workspace, l.bytes, l.stream);
+        });
+        return true;
+    });
+}
+
+// (out, q, seg_start, seg_prefill_len or None, kv_len, k_cache, v_cache, block_table, group_start or None, group_prefix_len or None, n_heads, scale,
+//  mode, workspace, stream)
+PyObject *cached_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        Matrix out, q;
+        Cache c;
+        Pages b;
+        int32_t heads, *start, *prefill = nullptr, *kv_len, *groups = nullptr, *prefix = nullptr;
+        Last l;
+        if (n != 15 || !g_cached || !as_matrix(o[0], out) || !as_matrix(o[1], q)) return false;
+        const int64_t S = entries(o[4]);
+        if (S < 0 || !as_table(o[2], S + 1, start) || (o[3] != Py_None && !as_table(o[3], S, prefill)) || !as_table(o[4], S, kv_len) ||
+            !as_cache(o[5], o[6], c) || !as_block_table(o[7], (int32_t)S, b) || !as_int(o[10], heads) || !as_last(o + 11, l)) return false;
+        if ((o[8] == Py_None) != (o[9] == Py_None)) return false;
+        const int64_t n_groups = o[9] == Py_None ? 0 : entries(o[9]);
+        if (n_groups < 0 || (n_groups > 0 && (!as_table(o[8], n_groups + 1, groups) || !as_table(o[9], n_groups, prefix)))) return false;
+        if (heads < 1 || out.cols != (int64_t)heads * c.dim || q.cols != out.cols || q.rows != out.rows || q.type != out.type || c.type != out.type)
+            return false;
+        rc = without_gil([&] {
+            return g_cached(out.p, out.ld, q.p, q.ld, out.rows, heads, c.heads, c.dim, start, prefill, kv_len, (int32_t)S, c.k, c.v, c.n_pages, c.page,
+                            b.p, b.ld, b.max_pages, groups, prefix, (int32_t)n_groups, l.scale, dtype_of(out.type), l.mode, l.workspace, l.bytes, l.stream);
+        });
+        return true;
+    });
+}
+
+// the addresses of the four calls above
+PyObject *bind_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    void *p[4];
+    if (n != 4) { PyErr_SetString(PyExc_TypeError, "four addresses"); return nullptr; }
+    for (int i = 0; i < 4; ++i) {
+        p[i] = PyLong_AsVoidPtr(o[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    g_plan = reinterpret_cast<decltype(g_plan)>(p[0]);
+    g_store = reinterpret_cast<decltype(g_store)>(p[1]);
+    g_prompt = reinterpret_cast<decltype(g_prompt)>(p[2]);
+    g_cached = reinterpret_cast<decltype(g_cached)>(p[3]);
+    Py_RETURN_NONE;
+}
+
 // binding.PoolRef, and the addresses of the loaded library's entry points in the order below
 PyObject *bind(PyObject *, PyObject *const *o, Py_ssize_t n)
 {
@@ -299,6 +449,11 @@ PyMethodDef methods[] = {
     {"lora_packed", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(lora_packed)), METH_FASTCALL, nullptr},
     {"reft", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(reft)), METH_FASTCALL, nullptr},
     {"reft_layers", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(reft_layers)), METH_FASTCALL, nullptr},
+    {"kv_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_plan)), METH_FASTCALL, nullptr},
+    {"kv_store", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_store)), METH_FASTCALL, nullptr},
+    {"prompt_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(prompt_attention)), METH_FASTCALL, nullptr},
+    {"cached_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cached_attention)), METH_FASTCALL, nullptr},
+    {"bind_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

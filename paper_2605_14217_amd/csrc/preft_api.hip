@@ -1303,13 +1303,13 @@ const char *preft_strerror(int code)
 {
     switch (code) {
     case PREFT_OK:           return "ok";
-    case PREFT_EINVAL:       return "invalid argument (null pointer, negative size, bad enum, overlapping x and y, or row stride below the width)";
-    case PREFT_EUNSUPPORTED: return "unsupported rank (must be 1..128)";
+    case PREFT_EINVAL:       return "invalid argument (null pointer, negative size, bad enum, overlapping inputs and outputs, or row stride below the width)";
+    case PREFT_EUNSUPPORTED: return "unsupported rank (must be 1..128), head_dim (64 or 128) or page_size (a power of two, 8..1024)";
     case PREFT_EALIGN:       return "pointer, width or row stride not a multiple of 16 bytes";
-    case PREFT_EWORKSPACE:   return "workspace missing, misaligned or smaller than preft_workspace_bytes(T, S)";
+    case PREFT_EWORKSPACE:   return "workspace missing, misaligned or smaller than preft_workspace_bytes(T, S) or preft_attention_workspace_bytes(...)";
     case PREFT_EHIP:         return "HIP runtime error (launch, copy or allocation)";
     case PREFT_ECAPACITY:    return "more distinct adapters in one batch than the slot manager has slots";
-    case PREFT_ETOOLARGE:    return "batch too large for the static schedule area of preft_direft_apply_static (preft_workspace_bytes(T, S) exceeds PREFT_STATIC_SCRATCH_BYTES)";
+    case PREFT_ETOOLARGE:    return "batch too large for the static schedule area of preft_direft_apply_static (preft_workspace_bytes(T, S) exceeds PREFT_STATIC_SCRATCH_BYTES), or an attention call of 2^30 and more (row, head) pairs";
     case PREFT_ESCHEDULE:    return "an apply call named another T, S, N or position set than the schedule in its workspace was built for; that call did nothing";
     default:                 return "unknown preft error code";
     }

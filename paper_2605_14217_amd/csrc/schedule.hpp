@@ -5,13 +5,13 @@
 // segment without a valid adapter has no active row.  Inactive rows appear in no unit, so
 // the apply kernels never touch them.
 #pragma once
+#include "block_scan.hpp"
 #include "common.hpp"
 
 namespace preft {
 
 // One workgroup of up to 16 wavefronts.  A step of a few dozen segments waits for the chain of barriers, not for work: one wavefront for every
 // 64 segments or 256 adapters.
-constexpr int SCHED_THREADS = 1024;
 inline int sched_threads(int64_t S, int64_t N)
 {
     const int64_t n = S > N / 4 ? S : N / 4;
@@ -36,34 +36,6 @@ __device__ __forceinline__ SegInfo seg_info(const int32_t *seg_start, const int3
     r.row0 = lo;
     r.n_act = n;
     return r;
-}
-
-// Exclusive scan of one int per thread over the block; returns the block total through *total.
-__device__ __forceinline__ int32_t block_exclusive_scan(int32_t v, int32_t *lds /* >= 32 ints */, int32_t *total)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-    int32_t incl = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        int32_t up = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += up;
-    }
-    if (n_waves == 1) {                      // uniform
-        __syncthreads();                     // as below: what the wavefront did to LDS before a scan is seen after it
-        *total = __shfl(incl, 63, 64);
-        return incl - v;
-    }
-    __syncthreads();                         // lds may still be read from a previous scan
-    if (lane == 63) lds[wave] = incl;
-    __syncthreads();
-    int32_t base = 0, sum = 0;
-    for (int w = 0; w < n_waves; ++w) {
-        int32_t t = lds[w];
-        if (w < wave) base += t;
-        sum += t;
-    }
-    *total = sum;
-    return base + incl - v;
 }
 
 // A gathered tile names entries [first, first + n) of the short-row list.  With well-formed
