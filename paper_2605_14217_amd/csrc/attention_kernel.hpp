@@ -121,25 +121,34 @@ template <typename E, int D, bool PAGED> struct AttnSource {
         return min(id, (uint32_t)(n_pages - 1));
     }
 
-    // copies rows key .. key + rows - 1 of K or V (COPIES x ROWS_PER_COPY rows) to `to`; `row0`: place of the first in its tile
+    // Copies COPIES x ROWS_PER_COPY rows of K or V, from `key` on, to `to`; `row0`: place of the first in its tile.  ROWS_PER_COPY divides both.
     template <bool V, int COPIES>
     __device__ __forceinline__ void copy(uint32_t to, int32_t key, int row0)
     {
         const int lane = threadIdx.x & 63, r = lane / X::PIECES, c = lane % X::PIECES;
+        if constexpr (PAGED) {
+            const char *base = nullptr;
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            const int row = row0 + i * X::ROWS_PER_COPY;
-            const int turn = V ? X::v_turn(row + r) : X::k_turn(row + r);
-            const int32_t at = min(key + i * X::ROWS_PER_COPY, last);
-            if constexpr (PAGED) {
-                const int32_t first = at & ~(X::ROWS_PER_COPY - 1);
-                const char *base = (V ? v : k) + page_of(at) * page_bytes + (int64_t)(first & ((1 << page_shift) - 1)) * X::ROW;
+            for (int i = 0; i < COPIES; ++i) {
+                const int32_t at = key + i * X::ROWS_PER_COPY;
+                const int turn = V ? X::v_turn(row0 + i * X::ROWS_PER_COPY + r) : X::k_turn(row0 + i * X::ROWS_PER_COPY + r);
+                if (i == 0 || (at & ((1 << page_shift) - 1)) == 0) {       // another page; past the last key: the last key's page
+                    const int32_t in = at & ((1 << page_shift) - 1);
+                    base = (V ? v : k) + page_of(min(at, last)) * page_bytes + in * X::ROW;
+                } else {
+                    base += X::ROWS_PER_COPY * X::ROW;
+                }
                 copy_to_lds(to + i * 1024, base, (uint32_t)(r * X::ROW + ((c ^ turn) << 4)));
-            } else {
-                const int64_t ld = V ? ldv : ldk;
-                const char *base = (V ? v : k) + (int64_t)at * ld;
-                const int32_t rel = min(r, last - at);           // rows past the last: the last again
-                copy_to_lds(to + i * 1024, base, (uint32_t)(rel * (int32_t)ld + ((c ^ turn) << 4)));
+            }
+        } else {
+            const int64_t ld = V ? ldv : ldk;
+            const int32_t first = min(key, last), most = last - first;     // rows past the last: the last again
+            const char *base = (V ? v : k) + first * ld;
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const int row = i * X::ROWS_PER_COPY + r;
+                const int turn = V ? X::v_turn(row0 + row) : X::k_turn(row0 + row);
+                copy_to_lds(to + i * 1024, base, (uint32_t)(min(row, most) * (int32_t)ld + ((c ^ turn) << 4)));
             }
         }
     }
@@ -190,6 +199,13 @@ template <typename E, int D> struct AttnColumns {
             for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
         m = ATTN_LOWEST;
         l = 0.0f;
+    }
+
+    // The queries are there: the compiler, which does not know of the copies in flight, would else wait for them in every turn of a loop.
+    __device__ __forceinline__ void arrived()
+    {
+#pragma unroll
+        for (int s = 0; s < X::STEPS; ++s) asm volatile("" : "+v"(q[s]));
     }
 
     // S^T of 32 keys from row `row0` of the K tile on
@@ -302,31 +318,37 @@ template <typename E, int D> struct AttnColumns {
             else ((PREFT_LDS float *)scratch)[at] = p[i];
         }
         wait_lds_reads();
-        for (int j = 0; j < 32; ++j) {
-            if (key + j < key0 || key + j >= lim) continue;
-            float w;
-            if constexpr (sizeof(E) == 2) w = (float)((const PREFT_LDS __bf16 *)scratch)[j * 32 + (lane & 31)];
-            else w = ((const PREFT_LDS float *)scratch)[j * 32 + (lane & 31)];
-            const int turn = X::v_turn(row0 + j);
+        const int32_t from = max(key0 - key, 0), to = min(lim - key, 32);
 #pragma unroll
-            for (int b = 0; b < X::BLOCKS; ++b)
+        for (int b = 0; b < X::BLOCKS; ++b) {
+            f32x16_t sum;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+            for (int j = 0; j < 32; ++j) {
+                if (j < from || j >= to) continue;
+                float w;
+                if constexpr (sizeof(E) == 2) w = (float)((const PREFT_LDS __bf16 *)scratch)[j * 32 + (lane & 31)];
+                else w = ((const PREFT_LDS float *)scratch)[j * 32 + (lane & 31)];
+                const int turn = X::v_turn(row0 + j);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {                     // dimensions 32 b + 8 i + 4 half ..
                     const int byte = (b * 32 + 8 * i + 4 * half) * X::ELEM;
                     const lds_t at = tile + (row0 + j) * X::ROW + (((byte >> 4) ^ turn) << 4) + (byte & 15);
                     if constexpr (sizeof(E) == 2) {
                         const u32x2_t v = *(const PREFT_LDS u32x2_t *)at;
-                        o[b][4 * i] += w * bf16_lo(v.x);
-                        o[b][4 * i + 1] += w * bf16_hi(v.x);
-                        o[b][4 * i + 2] += w * bf16_lo(v.y);
-                        o[b][4 * i + 3] += w * bf16_hi(v.y);
+                        sum[4 * i] += w * bf16_lo(v.x);
+                        sum[4 * i + 1] += w * bf16_hi(v.x);
+                        sum[4 * i + 2] += w * bf16_lo(v.y);
+                        sum[4 * i + 3] += w * bf16_hi(v.y);
                     } else {
                         const f32x4_t v = *(const PREFT_LDS f32x4_t *)at;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[b][4 * i + e] += w * v[e];
+                        for (int e = 0; e < 4; ++e) sum[4 * i + e] += w * v[e];
                     }
-                    __builtin_amdgcn_sched_barrier(0);            // few registers, not speed
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[b][i] += sum[i];
         }
     }
 };
@@ -393,6 +415,7 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
     AttnColumns<E, D> w;
     w.init(a, u, kv_head, wave * 32);
     if (lane == 0) { bounds[wave] = w.low; bounds[4 + wave] = w.high; }
+    w.arrived();
     __syncthreads();
     const int32_t low = uniform(min(min(bounds[0], bounds[1]), min(bounds[2], bounds[3])));
     const int32_t high = uniform(max(max(bounds[4], bounds[5]), max(bounds[6], bounds[7])));
@@ -414,26 +437,41 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
         w.add(vt, 0, s[0]);
         w.add(vt, 32, s[1]);
     }
+    bool bad = false;
     for (; i < n; ++i) {
         arrive(i);
         const lds_t kt = lds + (i & 1) * X::TILE, vt = kt + 2 * X::TILE;
         const int32_t key = key_of(i);
-        const bool bad = __syncthreads_or(clean_rows<E, D>(vt, key, u.key0, low, high, threadIdx.x, 256, X::TILE / 16));
+        bad = __syncthreads_or(clean_rows<E, D>(vt, key, u.key0, low, high, threadIdx.x, 256, X::TILE / 16));
+        if (bad) break;
         f32x16_t s[2];
         s[0] = w.scores(kt, 0);
         s[1] = w.scores(kt, 32);
         w.hide(s[0], key, u.key0);
         w.hide(s[1], key + 32, u.key0);
         w.template exponentials<2>(s, c);
-        if (bad) {
-            __syncthreads();                                      // the K tile becomes scratch
-            const lds_t scratch = kt + wave * (X::TILE / 4);
-            w.careful(vt, 0, s[0], scratch, key, u.key0);
-            w.careful(vt, 32, s[1], scratch, key + 32, u.key0);
-        } else {
-            w.add(vt, 0, s[0]);
-            w.add(vt, 32, s[1]);
+        w.add(vt, 0, s[0]);
+        w.add(vt, 32, s[1]);
+    }
+    for (; i < n; ++i) {                                          // from a tile with infinities or NaN on: a loop of its own, for its registers
+        if (!bad) {
+            arrive(i);
+            clean_rows<E, D>(lds + (i & 1) * X::TILE + 2 * X::TILE, key_of(i), u.key0, low, high, threadIdx.x, 256, X::TILE / 16);
+            __syncthreads();
         }
+        bad = false;
+        const lds_t kt = lds + (i & 1) * X::TILE, vt = kt + 2 * X::TILE;
+        const int32_t key = key_of(i);
+        f32x16_t s[2];
+        s[0] = w.scores(kt, 0);
+        s[1] = w.scores(kt, 32);
+        w.hide(s[0], key, u.key0);
+        w.hide(s[1], key + 32, u.key0);
+        w.template exponentials<2>(s, c);
+        __syncthreads();                                          // the K tile becomes scratch
+        const lds_t scratch = kt + wave * (X::TILE / 4);
+        w.careful(vt, 0, s[0], scratch, key, u.key0);
+        w.careful(vt, 32, s[1], scratch, key + 32, u.key0);
     }
     const float l = both_halves_sum(w.l);
     if (!w.valid) return;
@@ -483,7 +521,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     AttnColumns<E, D> w;
     w.init(a, u, kv_head, 0);
     const float c = a.scale_log2;
-    wait_copies<0>();                                             // the queries and the first block
+    w.arrived();
     const int32_t before = (w.low - base) / 32 - wave;            // blocks from this wavefront's first on that all columns see whole
     const int32_t full = min(n, max(0, (before + 3) / 4 - skip));
     int32_t i = 0;
@@ -501,17 +539,34 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
         wait_lds_reads();
         if (more) src.template copy<true, COPIES>(va, key_of(i + 1), 0);
     }
+    bool bad = false;
     for (; i < n; ++i) {
         const int32_t key = key_of(i);
         wait_copies<0>();
+        bad = __any(clean_rows<E, D>(vt, key, u.key0, w.low, w.high, lane, 64, HALF / 16));
+        if (bad) break;
         f32x16_t s[1];
         s[0] = w.scores(kt, 0);
         w.hide(s[0], key, u.key0);
         w.template exponentials<1>(s, c);
-        const bool bad = clean_rows<E, D>(vt, key, u.key0, w.low, w.high, lane, 64, HALF / 16);
+        w.add(vt, 0, s[0]);
         wait_lds_reads();
-        if (__any(bad)) w.careful(vt, 0, s[0], kt, key, u.key0);
-        else w.add(vt, 0, s[0]);
+        if (i + 1 < n) {
+            src.template copy<false, COPIES>(ka, key_of(i + 1), 0);
+            src.template copy<true, COPIES>(va, key_of(i + 1), 0);
+        }
+    }
+    for (; i < n; ++i) {                                          // as above
+        const int32_t key = key_of(i);
+        wait_copies<0>();
+        if (!bad) clean_rows<E, D>(vt, key, u.key0, w.low, w.high, lane, 64, HALF / 16);
+        bad = false;
+        f32x16_t s[1];
+        s[0] = w.scores(kt, 0);
+        w.hide(s[0], key, u.key0);
+        w.template exponentials<1>(s, c);
+        wait_lds_reads();
+        w.careful(vt, 0, s[0], kt, key, u.key0);
         wait_lds_reads();
         if (i + 1 < n) {
             src.template copy<false, COPIES>(ka, key_of(i + 1), 0);
