@@ -133,7 +133,8 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
     AttnArgs a = {};
     a.q = q; a.k = k; a.v = v; a.out = out;
     a.ldq = ldq * e; a.ldk = ldk * e; a.ldv = ldv * e; a.ldo = ldo * e;
-    a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads;
+    a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads; a.group = n_heads / n_kv_heads;
+    a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.l = lists_of(l, workspace);
     const bool split = (int64_t)l.tile_cap * n_kv_heads < 4 * ATTN_TARGET;     // else there are tiles enough
@@ -174,7 +175,8 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     AttnArgs a = {};
     a.q = q; a.k = k_cache; a.v = v_cache; a.out = out; a.ldq = ldq * e; a.ldo = ldo * e;
     a.table = block_table; a.ld_table = ld_table; a.n_pages = n_pages; a.page_shift = shift; a.max_pages = max_pages;
-    a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads; a.n_groups = n_groups;
+    a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads; a.group = n_heads / n_kv_heads; a.n_groups = n_groups;
+    a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.l = lists_of(l, workspace);
     if (!(mode & PREFT_SCHEDULE_READY)) {

@@ -29,8 +29,9 @@ struct AttnArgs {
     const int32_t *table;
     int64_t ld_table;
     int32_t n_pages, page_shift, max_pages;
-    int32_t T, S, heads, kv_heads, n_groups;
+    int32_t T, S, heads, kv_heads, group, n_groups;      // group: query heads of a key/value head, G
     float scale_log2;
+    uint32_t per_head;                // ceil(2^21 / G): x / G = x per_head >> 21 for x < 2048 (G <= 1024)
     AttnLists l;
 };
 
@@ -163,16 +164,15 @@ template <typename E, int D> struct AttnColumns {
     f32x16_t o[X::BLOCKS];
     float    m, l;                    // l: of this lane's keys
     int32_t  lim;                     // this lane's column sees keys below it
-    int32_t  low, high;               // smallest and largest of them over the wavefront's columns
     int32_t  row, head;               // of the query
     bool     valid;
 
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
     {
-        const int lane = threadIdx.x & 63, half = lane >> 5, col = first + (lane & 31), G = a.heads / a.kv_heads;
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = first + (lane & 31), G = a.group;
         valid = col < u.ncols;
-        const int32_t c = u.col0 + (valid ? col : u.ncols - 1), i = c / G;
-        head = kv_head * G + (c - i * G);
+        const int32_t x = u.head0 + min(col, u.ncols - 1), i = (int32_t)((uint32_t)x * a.per_head >> 21);
+        head = kv_head * G + (x - i * G);
         if (u.row0 >= 0) {
             row = u.row0 + i;
             lim = u.lim0 + i;
@@ -183,13 +183,6 @@ template <typename E, int D> struct AttnColumns {
         }
         row = max(0, min(row, a.T - 1));
         lim = min(lim, u.key1);
-        low = lim; high = lim;
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            low = min(low, __shfl_xor(low, off, 64));
-            high = max(high, __shfl_xor(high, off, 64));
-        }
-        low = uniform(low); high = uniform(high);
         const gcptr_t from = as_global((const char *)a.q + (int64_t)row * a.ldq + head * X::ROW + half * 16);
 #pragma unroll
         for (int s = 0; s < X::STEPS; ++s) q[s] = ld16(from + s * 32);
@@ -234,11 +227,13 @@ template <typename E, int D> struct AttnColumns {
     // the keys of register i of a block of 32: 8 (i / 4) + 4 half + i % 4
     __device__ __forceinline__ void hide(f32x16_t &s, int32_t key, int32_t key0) const
     {
-        const int half = (threadIdx.x & 63) >> 5;
+        const int32_t at = key + 4 * ((threadIdx.x & 63) >> 5), n = lim - at;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int32_t j = key + 8 * (i / 4) + 4 * half + i % 4;
-            s[i] = j >= key0 && j < lim ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 < n ? s[i] : -INFINITY;
+        if (key < key0) {
+            const int32_t from = key0 - at;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 >= from ? s[i] : -INFINITY;
         }
     }
 
@@ -353,29 +348,36 @@ template <typename E, int D> struct AttnColumns {
     }
 };
 
-// 16 bytes of a V row hold an infinity or a NaN
+// 16 bytes of a V row hold an infinity or a NaN: an exponent of ones is the largest there is
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 template <typename E> __device__ __forceinline__ bool not_finite(u32x4_t v)
 {
-    bool bad = false;
+    if constexpr (sizeof(E) == 2) {
+        u16x2_t top = __builtin_bit_cast(u16x2_t, v[0] & 0x7fff7fffu);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(E) == 2) bad = bad || (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-        else bad = bad || (v[i] & 0x7f800000u) == 0x7f800000u;
+        for (int i = 1; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, v[i] & 0x7fff7fffu));
+        return max(top.x, top.y) >= 0x7f80;
+    } else {
+        const uint32_t top = max(max(v[0] & 0x7fffffffu, v[1] & 0x7fffffffu), max(v[2] & 0x7fffffffu, v[3] & 0x7fffffffu));
+        return top >= 0x7f800000u;
     }
-    return bad;
 }
 
-// Rows of a V tile that no column sees become zero; says whether a row that only some see is not finite.  `n` pieces from `tid` on, `step` apart.
-template <typename E, int D>
-__device__ __forceinline__ bool clean_rows(lds_t tile, int32_t key, int32_t key0, int32_t low, int32_t high, int tid, int step, int n)
+// Rows of a V tile that no column sees become zero; says whether a row that only some see is not finite.  PIECES_EACH pieces of 16 bytes from `tid`
+// on, `step` apart.
+template <typename E, int D, int PIECES_EACH>
+__device__ __forceinline__ bool clean_rows(lds_t tile, int32_t key, int32_t key0, int32_t low, int32_t high, int tid, int step)
 {
     using X = AttnTile<E, D>;
+    u32x4_t v[PIECES_EACH];
+#pragma unroll
+    for (int k = 0; k < PIECES_EACH; ++k) v[k] = *(PREFT_LDS u32x4_t *)(tile + (tid + k * step) * 16);
     bool bad = false;
-    for (int p = tid; p < n; p += step) {
-        const int32_t j = key + p / X::PIECES;
-        PREFT_LDS u32x4_t *at = (PREFT_LDS u32x4_t *)(tile + p * 16);
-        if (j < key0 || j >= high) *at = u32x4_t{0, 0, 0, 0};
-        else if (j >= low) bad = bad || not_finite<E>(*at);
+#pragma unroll
+    for (int k = 0; k < PIECES_EACH; ++k) {
+        const int32_t j = key + (tid + k * step) / X::PIECES;
+        if (j < key0 || j >= high) *(PREFT_LDS u32x4_t *)(tile + (tid + k * step) * 16) = u32x4_t{0, 0, 0, 0};
+        else if (j >= low) bad = bad || not_finite<E>(v[k]);
     }
     return bad;
 }
@@ -393,7 +395,7 @@ __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.
 // tile ahead.
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, bool PAGED>
-__device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, int32_t *bounds)
+__device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, int32_t *votes)
 {
     using X = AttnTile<E, D>;
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
@@ -414,11 +416,8 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
     if (n > 0) fetch(0);
     AttnColumns<E, D> w;
     w.init(a, u, kv_head, wave * 32);
-    if (lane == 0) { bounds[wave] = w.low; bounds[4 + wave] = w.high; }
     w.arrived();
-    __syncthreads();
-    const int32_t low = uniform(min(min(bounds[0], bounds[1]), min(bounds[2], bounds[3])));
-    const int32_t high = uniform(max(max(bounds[4], bounds[5]), max(bounds[6], bounds[7])));
+    const int32_t low = min(u.lim0, u.key1), high = u.key1;       // keys that every column sees, and that some column sees
     const float c = a.scale_log2;
     auto arrive = [&](int32_t i) {
         // this wavefront's copies of turn i and its reads of turn i - 1 are done, then everybody's
@@ -442,11 +441,14 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
         arrive(i);
         const lds_t kt = lds + (i & 1) * X::TILE, vt = kt + 2 * X::TILE;
         const int32_t key = key_of(i);
-        bad = __syncthreads_or(clean_rows<E, D>(vt, key, u.key0, low, high, threadIdx.x, 256, X::TILE / 16));
-        if (bad) break;
+        const bool mine = __any(clean_rows<E, D, X::TILE / 16 / 256>(vt, key, u.key0, low, high, threadIdx.x, 256));
+        if (lane == 0) votes[wave] = mine;
         f32x16_t s[2];
         s[0] = w.scores(kt, 0);
         s[1] = w.scores(kt, 32);
+        __syncthreads();
+        bad = votes[0] | votes[1] | votes[2] | votes[3];
+        if (bad) break;
         w.hide(s[0], key, u.key0);
         w.hide(s[1], key + 32, u.key0);
         w.template exponentials<2>(s, c);
@@ -456,7 +458,7 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
     for (; i < n; ++i) {                                          // from a tile with infinities or NaN on: a loop of its own, for its registers
         if (!bad) {
             arrive(i);
-            clean_rows<E, D>(lds + (i & 1) * X::TILE + 2 * X::TILE, key_of(i), u.key0, low, high, threadIdx.x, 256, X::TILE / 16);
+            clean_rows<E, D, X::TILE / 16 / 256>(lds + (i & 1) * X::TILE + 2 * X::TILE, key_of(i), u.key0, low, high, threadIdx.x, 256);
             __syncthreads();
         }
         bad = false;
@@ -474,16 +476,31 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
         w.careful(vt, 32, s[1], scratch, key + 32, u.key0);
     }
     const float l = both_halves_sum(w.l);
-    if (!w.valid) return;
     if (u.slot < 0) {
         const float f = inverse(l);
-        const gptr_t to = as_global((char *)a.out + (int64_t)w.row * a.ldo + w.head * X::ROW + half * 4 * X::ELEM);
+        const gptr_t to = as_global((char *)a.out + (int64_t)w.row * a.ldo + w.head * X::ROW + half * (X::ELEM == 2 ? 16 : 4 * X::ELEM));
 #pragma unroll
-        for (int b = 0; b < X::BLOCKS; ++b)
+        for (int b = 0; b < X::BLOCKS; ++b) {
+            if constexpr (X::ELEM == 2) {                         // the two lanes of a column trade halves: 16 bytes each, of consecutive dimensions
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                store4<E>(to + (b * 32 + 8 * r) * X::ELEM, w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f);
-    } else {
+                for (int r = 0; r < 4; r += 2) {
+                    u32x4_t v;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(w.o[b][4 * r + 2 * e] * f, w.o[b][4 * r + 2 * e + 1] * f),
+                                                                        pack_bf16(w.o[b][4 * r + 4 + 2 * e] * f, w.o[b][4 * r + 5 + 2 * e] * f), false, false);
+                        v[e] = x[0];
+                        v[2 + e] = x[1];
+                    }
+                    if (w.valid) st16(to + (b * 32 + 8 * r) * X::ELEM, v);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (w.valid) store4<E>(to + (b * 32 + 8 * r) * X::ELEM, w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f);
+            }
+        }
+    } else if (w.valid) {
         const int64_t part = (int64_t)u.slot + kv_head * u.ncols + wave * 32 + (lane & 31);
         const gptr_t to = as_global((void *)(a.l.part_o + part * D + half * 4));
 #pragma unroll
@@ -522,7 +539,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     w.init(a, u, kv_head, 0);
     const float c = a.scale_log2;
     w.arrived();
-    const int32_t before = (w.low - base) / 32 - wave;            // blocks from this wavefront's first on that all columns see whole
+    const int32_t low = min(u.lim0, u.key1), before = (low - base) / 32 - wave;            // blocks from this wavefront's first on that all columns see whole
     const int32_t full = min(n, max(0, (before + 3) / 4 - skip));
     int32_t i = 0;
     for (; i < full; ++i) {
@@ -543,7 +560,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     for (; i < n; ++i) {
         const int32_t key = key_of(i);
         wait_copies<0>();
-        bad = __any(clean_rows<E, D>(vt, key, u.key0, w.low, w.high, lane, 64, HALF / 16));
+        bad = __any(clean_rows<E, D, HALF / 1024>(vt, key, u.key0, low, u.key1, lane, 64));
         if (bad) break;
         f32x16_t s[1];
         s[0] = w.scores(kt, 0);
@@ -559,7 +576,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     for (; i < n; ++i) {                                          // as above
         const int32_t key = key_of(i);
         wait_copies<0>();
-        if (!bad) clean_rows<E, D>(vt, key, u.key0, w.low, w.high, lane, 64, HALF / 16);
+        if (!bad) clean_rows<E, D, HALF / 1024>(vt, key, u.key0, low, u.key1, lane, 64);
         bad = false;
         f32x16_t s[1];
         s[0] = w.scores(kt, 0);
@@ -591,7 +608,6 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
             }
     }
     __syncthreads();
-    const int G = a.heads / a.kv_heads;
     for (int i = tid; i < u.ncols * (D / 4); i += 256) {
         const int cc = i / (D / 4), d = i % (D / 4) * 4;
         const float m0 = join[cc], m1 = join[32 + cc], m2 = join[64 + cc], m3 = join[96 + cc];
@@ -606,7 +622,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }
         if (u.slot < 0) {
-            const int32_t q = (u.col0 + cc) / G, head = kv_head * G + (u.col0 + cc - q * G);
+            const int32_t x = u.head0 + cc, q = (int32_t)((uint32_t)x * a.per_head >> 21), head = kv_head * a.group + (x - q * a.group);
             const float inv = inverse(ll);
             const int32_t row = max(0, min(u.row0 + q, a.T - 1));   // a group's units always have parts
             store4<E>(as_global((char *)a.out + (int64_t)row * a.ldo + head * X::ROW + d * X::ELEM), v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
@@ -640,7 +656,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
     if (unit >= as_const(a.l.header)[AH_UNITS]) return;
     const PREFT_CONST AttnUnit *p = as_const(a.l.units) + unit;
     AttnUnit u;
-    u.table = p->table; u.col0 = p->col0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
+    u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
     if (u.ncols <= 0) return;
     if (u.ncols > ATTN_FEW_COLS) attend_columns<E, D, PAGED>(a, u, kv_head, (lds_t)lds, (int32_t *)join);
     else attend_keys<E, D, PAGED>(a, u, kv_head, (lds_t)lds, join);
@@ -651,7 +667,7 @@ template <typename E, int D>
 __global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, int kind)
 {
     using X = AttnTile<E, D>;
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, kv_head = blockIdx.y, G = a.heads / a.kv_heads;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, kv_head = blockIdx.y, G = a.group;
     if (!attn_schedule_is(a, kind)) return;
     const int32_t n = as_const(a.l.header)[AH_MERGES];
     for (int32_t i = blockIdx.x; i < n; i += gridDim.x) {

@@ -20,11 +20,11 @@ constexpr int ATTN_SCAN      = 4096;  // items whose tile offsets are kept in LD
 
 struct AttnUnit {
     int32_t table;     // row of the block table; packed keys: the row of key 0
-    int32_t col0;      // first column within the item
+    int32_t head0;     // column c of the unit is query head (head0 + c) % G of row (head0 + c) / G
     int32_t ncols;     // 1..ATTN_COLS
     int32_t key0, key1;
-    int32_t row0;      // batch row of the item's row 0; a group: -1 - (its first entry in the row list)
-    int32_t lim0;      // row i of the item sees keys below lim0 + i
+    int32_t row0;      // batch row of the unit's row 0, the next ones follow; a group: -1 - (its entry in the row list)
+    int32_t lim0;      // row i sees keys below lim0 + i; a group: every row sees those below
     int32_t slot;      // first part column, head-major; -1: the unit writes the result
 };
 struct AttnMerge {
@@ -242,16 +242,27 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
                     group_ranges = ranges_of(key_tiles(0, m.prefix), range);
                 }
                 u.table = a.kv_len ? i : it.row0;
-                u.row0 = it.row0; u.lim0 = it.lim0;
             } else {
                 m = attn_group(a, i - a.S);
                 it.rows = m.rows; it.key0 = 0; it.key1 = m.prefix;
                 u.table = min(m.begin, a.S - 1);
-                u.row0 = -1 - a.l.group_list[i - a.S]; u.lim0 = 0;
             }
-            u.col0 = tile * ATTN_COLS;
-            u.ncols = min(ATTN_COLS, it.rows * G - u.col0);
-            const int32_t key1 = i < a.S ? min(it.key1, it.lim0 + (u.col0 + u.ncols - 1) / G) : it.key1;
+            const int32_t col0 = tile * ATTN_COLS, first = col0 / G;
+            u.ncols = min(ATTN_COLS, it.rows * G - col0);
+            u.head0 = col0 - first * G;
+            const int32_t rows = (u.head0 + u.ncols - 1) / G + 1;
+            int32_t key1 = it.key1;
+            if (i < a.S) {
+                u.row0 = it.row0 + first;
+                u.lim0 = it.lim0 + first;
+                key1 = min(key1, u.lim0 + rows - 1);
+            } else {
+                const int32_t at = a.l.group_list[i - a.S] + first;
+                u.row0 = -1 - at;
+                u.lim0 = key1;
+                if (pass == 1)
+                    for (int32_t r = 0; r < rows; ++r) u.lim0 = min(u.lim0, a.l.group_rows[min(at + r, a.l.group_row_cap - 1)].y);
+            }
             const int32_t n = key_tiles(it.key0, key1);
             const int32_t splits = n == 0 && g >= 0 ? 0 : ranges_of(n, range);     // 0: the group's part is all there is
             const bool parts = splits > 1 || g >= 0 || i >= a.S;
@@ -278,9 +289,9 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             }
             if (parts && i < a.S && fits) {
                 AttnMerge j;
-                j.row0 = u.row0; j.col0 = u.col0; j.ncols = u.ncols; j.parts = splits; j.slot = slot;
+                j.row0 = it.row0; j.col0 = col0; j.ncols = u.ncols; j.parts = splits; j.slot = slot;
                 j.group_parts = group_ranges; j.group_slot = g >= 0 ? a.l.group_slot[g] : 0;
-                j.group_col0 = g >= 0 ? (a.l.rows_before[i] - a.l.rows_before[m.begin]) * G + u.col0 : 0;
+                j.group_col0 = g >= 0 ? (a.l.rows_before[i] - a.l.rows_before[m.begin]) * G + col0 : 0;
                 j.group_cols = m.rows * G;
                 j.pad[0] = j.pad[1] = j.pad[2] = 0;
                 const int32_t to = atomicAdd(&n_merges, 1);
