@@ -46,12 +46,13 @@ template <typename E, int D> struct AttnTile {
     static constexpr int BLOCKS = D / 32;
     static constexpr int TILE = ATTN_KEYS * ROW;
     static constexpr int LDS = 4 * TILE;                  // K and V, two tiles each; or K and V of 32 keys for every wavefront
-    // Pieces of 16 bytes are exchanged within a row so that the lanes of a read, which want the same piece of consecutive rows, spread over all banks.
-    static __device__ __forceinline__ int k_turn(int row) { return row & (PIECES < 16 ? PIECES - 1 : 15); }
+    // Pieces of 16 bytes are exchanged within a row so that what LDS reads in one cycle, 256 bytes, comes from all 64 banks: 16 lanes' 16 bytes of one piece of
+    // 16 rows of K; 32 lanes' 8 bytes of four pieces of 4 rows of V (bf16), or 128 bytes each of two rows 4 apart (f32).
+    static __device__ __forceinline__ int k_turn(int row) { return PIECES < 16 ? (row >> 1) & 7 : row & 15; }
     static __device__ __forceinline__ int v_turn(int row)
     {
         if constexpr (ELEM == 4) return 8 * ((row >> 2) & 1);
-        else return PIECES >= 16 ? 2 * (row & 3) + 8 * ((row >> 2) & 1) : 2 * (row & 3);
+        else return PIECES >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
     }
 };
 
