@@ -10,10 +10,11 @@ namespace {
 
 using namespace preft;
 
-// Work ranges may be cut where the tiles of all segments are few.  Bounds on the lists, for tables that are well-formed:
+// Bounds on the lists, for tables that are well-formed:
 //   column tiles   T G / 128 + one part-filled tile a segment, and the same of groups;
-//   units          a tile is cut into ceil(n / range) <= 1 + n / range ranges, and the n of all tiles add up to at most TARGET / kv_heads ranges
-//                  and one more a tile (the estimate of a causal prompt's work is half a tile off each way);
+//   units          a tile of n key tiles is cut into ceil(n / range) < 1 + n / range ranges, and range is at least the estimate of all tiles' n times
+//                  kv_heads / TARGET.  That estimate, from the first and the last tile of a segment, is short by up to two a tile of a causal prompt (list), and
+//                  at least half of what counting every tile of a segment like its last gives (direct);
 //   part columns   a tile that is cut has at most twice n / range parts of at most 128 columns; rows of groups have one of their own and their group's.
 struct Layout {
     int32_t tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
@@ -27,7 +28,7 @@ Layout layout_of(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t 
     const int64_t seg_tiles = cols / ATTN_COLS + (S < T ? S : T);
     const int64_t tiles = groups > 0 ? 2 * seg_tiles + groups : seg_tiles;
     l.tile_cap = (int32_t)tiles;
-    l.unit_cap = (int32_t)(2 * tiles + ATTN_TARGET + 64);
+    l.unit_cap = (int32_t)(3 * tiles + 2 * ((ATTN_TARGET + kv_heads - 1) / kv_heads) + 2);
     l.merge_cap = (int32_t)seg_tiles;
     l.group_row_cap = groups > 0 ? (int32_t)(T < ATTN_GROUP_ROWS ? T : ATTN_GROUP_ROWS) : 0;
     l.slot_cap = (int32_t)(4 * ATTN_TARGET * (cols < ATTN_COLS ? cols : ATTN_COLS) + 2 * l.group_row_cap * heads);
@@ -68,31 +69,59 @@ AttnLists lists_of(const Layout &l, void *workspace)
 
 bool sizes_fit(int64_t T, int64_t S, int64_t heads, int64_t groups) { return T * heads < (1ll << 30) && S + groups < (1ll << 28); }
 
-template <typename E, int D, bool PAGED>
-int launch(const AttnArgs &a, bool split, hipStream_t st)
+// How a call runs: its units found by the workgroups themselves or listed by the schedule kernel, its keys cut into ranges or not.
+struct Plan { bool direct, split; int64_t units, tiles; };
+
+// Few segments and workgroups: the schedule kernel's 6 to 8 us are a third of the call (one decode row over 1500 keys: 20.7 us with it, see the table of
+// DESIGN without); with more than two rounds of workgroups each one's search, about a microsecond, costs as much, and the order by cost pays.
+// Keys are cut where the tiles alone do not fill the chip and some tile may be longer than a range.
+Plan plan_of(const AttnScheduleArgs &s, int64_t most_keys)
 {
-    const unsigned units = split ? (unsigned)a.l.unit_cap : (unsigned)a.l.tile_cap;
-    hipLaunchKernelGGL((attention_kernel<E, D, PAGED>), dim3(units * (unsigned)a.kv_heads), dim3(256), 0, st, a);
-    if (split) {
-        const unsigned x = a.l.merge_cap < 1024 ? (unsigned)a.l.merge_cap : 1024u;
-        const unsigned z = x * (unsigned)a.kv_heads < 512 && (int64_t)a.T * (a.heads / a.kv_heads) > 4 ? 8u : 1u;
-        hipLaunchKernelGGL((attention_merge_kernel<E, D>), dim3(x, (unsigned)a.kv_heads, z), dim3(256), 0, st, a, PAGED ? 2 : 1);
+    Plan p;
+    const int64_t key_tiles = (most_keys + ATTN_KEYS - 1) / ATTN_KEYS;
+    p.tiles = s.l.tile_cap;
+    p.split = s.can_split && key_tiles > s.min_tiles;
+    p.direct = s.n_groups == 0 && s.S <= ATTN_DIRECT && p.tiles * s.kv_heads <= 2 * ATTN_TARGET;
+    const int64_t ranges = (ATTN_TARGET + s.kv_heads - 1) / s.kv_heads;
+    p.units = !p.split ? p.tiles : p.direct ? p.tiles + 2 * ranges + 2 : 3 * p.tiles + ranges + 2;
+    const int64_t most = p.tiles * ((key_tiles + s.min_tiles - 1) / s.min_tiles);
+    if (p.split && p.units > most) p.units = most;
+    return p;
+}
+
+template <typename E, int D, bool PAGED, bool DIRECT>
+int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
+{
+    hipLaunchKernelGGL((attention_kernel<E, D, PAGED, DIRECT>), dim3((unsigned)(p.units * a.kv_heads)), dim3(256), 0, st, a);
+    if (p.split) {
+        const unsigned tiles = (unsigned)(DIRECT ? p.tiles : a.l.merge_cap < 1024 ? a.l.merge_cap : 1024);
+        const unsigned z = tiles * (unsigned)a.kv_heads < 512 && (int64_t)a.T * a.group > 4 ? 8u : 1u;
+        hipLaunchKernelGGL((attention_merge_kernel<E, D, DIRECT>), dim3(tiles, (unsigned)a.kv_heads, z), dim3(256), 0, st, a, PAGED ? 2 : 1);
     }
     return launched();
 }
 
-template <bool PAGED>
-int dispatch(const AttnArgs &a, int dtype, int32_t head_dim, bool split, hipStream_t st)
+template <bool PAGED, bool DIRECT>
+int launch_typed(const AttnArgs &a, int dtype, int32_t head_dim, const Plan &p, hipStream_t st)
 {
-    if (dtype == PREFT_BF16) return head_dim == 128 ? launch<__bf16, 128, PAGED>(a, split, st) : launch<__bf16, 64, PAGED>(a, split, st);
-    return head_dim == 128 ? launch<float, 128, PAGED>(a, split, st) : launch<float, 64, PAGED>(a, split, st);
+    if (dtype == PREFT_BF16)
+        return head_dim == 128 ? launch<__bf16, 128, PAGED, DIRECT>(a, p, st) : launch<__bf16, 64, PAGED, DIRECT>(a, p, st);
+    return head_dim == 128 ? launch<float, 128, PAGED, DIRECT>(a, p, st) : launch<float, 64, PAGED, DIRECT>(a, p, st);
 }
 
-void launch_schedule(const AttnScheduleArgs &s, hipStream_t st)
+template <bool PAGED>
+int run(AttnArgs &a, int dtype, int32_t head_dim, int mode, int64_t most_keys, hipStream_t st)
 {
-    const int64_t n = (int64_t)s.S + s.n_groups > s.l.tile_cap ? (int64_t)s.S + s.n_groups : s.l.tile_cap;
-    const int threads = n >= SCHED_THREADS ? SCHED_THREADS : n <= 256 ? 256 : (int)((n + 63) / 64 * 64);
-    hipLaunchKernelGGL(attn_schedule_kernel, dim3(1), dim3(threads), 0, st, s);
+    Plan p = plan_of(a.s, most_keys);
+    if (!p.split) a.s.can_split = 0;
+    a.ready = mode & PREFT_SCHEDULE_READY;
+    if (p.direct) return launch_typed<PAGED, true>(a, dtype, head_dim, p, st);
+    if (!a.ready) {
+        const int64_t items = (int64_t)a.s.S + a.s.n_groups, n = items > a.l.tile_cap ? items : a.l.tile_cap;
+        const int threads = n >= SCHED_THREADS ? SCHED_THREADS : n <= 256 ? 256 : (int)((n + 63) / 64 * 64);
+        hipLaunchKernelGGL(attn_schedule_kernel, dim3(1), dim3(threads), 0, st, a.s);
+    }
+    return launch_typed<PAGED, false>(a, dtype, head_dim, p, st);
 }
 
 int check_call(int32_t T, int32_t S, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t groups, float scale, int dtype, int mode)
@@ -137,14 +166,12 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
     a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.l = lists_of(l, workspace);
-    const bool split = (int64_t)l.tile_cap * n_kv_heads < 4 * ATTN_TARGET;     // else there are tiles enough
-    if (!(mode & PREFT_SCHEDULE_READY)) {
-        AttnScheduleArgs s = {};
-        s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads;
-        s.max_keys = T; s.can_split = split; s.min_tiles = 8; s.l = a.l;
-        launch_schedule(s, st);
-    }
-    return dispatch<false>(a, dtype, head_dim, split, st);
+    AttnScheduleArgs &s = a.s;
+    s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads;
+    s.max_keys = T; s.l = a.l;
+    s.can_split = (int64_t)l.tile_cap * n_kv_heads < 4 * ATTN_TARGET;              // else there are tiles enough
+    s.min_tiles = dtype == PREFT_BF16 ? 8 : 2;
+    return run<false>(a, dtype, head_dim, mode, T, st);
 }
 
 int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -179,16 +206,14 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.l = lists_of(l, workspace);
-    if (!(mode & PREFT_SCHEDULE_READY)) {
-        AttnScheduleArgs s = {};
-        s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.kv_len = kv_len; s.group_start = group_start; s.group_prefix = group_prefix_len;
-        s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads;
-        const int64_t most = (int64_t)max_pages << shift;
-        s.max_keys = keys ? (int32_t)(most < (1 << 30) ? most : (1 << 30)) : 0;
-        s.can_split = 1; s.min_tiles = 4; s.l = a.l;
-        launch_schedule(s, st);
-    }
-    return dispatch<true>(a, dtype, head_dim, true, st);
+    AttnScheduleArgs &s = a.s;
+    s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.kv_len = kv_len; s.group_start = group_start; s.group_prefix = group_prefix_len;
+    s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads; s.l = a.l;
+    const int64_t most = (int64_t)max_pages << shift;
+    s.max_keys = keys ? (int32_t)(most < (1 << 30) ? most : (1 << 30)) : 0;
+    s.can_split = 1;
+    s.min_tiles = dtype == PREFT_BF16 ? 2 : 1;
+    return run<true>(a, dtype, head_dim, mode, s.max_keys, st);
 }
 
 }  // extern "C"

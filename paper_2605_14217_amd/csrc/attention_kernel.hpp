@@ -33,6 +33,8 @@ struct AttnArgs {
     float scale_log2;
     uint32_t per_head;                // ceil(2^21 / G): x / G = x per_head >> 21 for x < 2048 (G <= 1024)
     AttnLists l;
+    AttnScheduleArgs s;               // direct calls find their units from it
+    int32_t ready;                    // direct calls: the header is there already
 };
 
 constexpr float ATTN_LOWEST = -3.0e38f;   // below every score's exponent, and finite: 2^(-inf - it) is 0, not NaN
@@ -645,19 +647,31 @@ __device__ __forceinline__ bool attn_schedule_is(const AttnArgs &a, int kind)
 }
 
 // Consecutive workgroups take the key/value heads of one unit: with 8 heads, or a multiple, every XCD keeps to its own heads' keys in its L2.
-template <typename E, int D, bool PAGED>
+// DIRECT: there is no list, every wavefront finds the unit by itself; the first workgroup leaves the header that a later call asks for.
+template <typename E, int D, bool PAGED, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
 {
     using X = AttnTile<E, D>;
-    constexpr int JOIN = 4 * 32 * (D + 4) * 4;
+    constexpr int JOIN = 4 * 32 * (D + 4) * 4, KIND = PAGED ? 2 : 1;
     __shared__ __align__(1024) char lds[X::LDS > JOIN ? X::LDS : JOIN];
     __shared__ float join[256];
-    if (!attn_schedule_is(a, PAGED ? 2 : 1)) return;
     const int32_t unit = (int32_t)blockIdx.x / a.kv_heads, kv_head = (int32_t)blockIdx.x % a.kv_heads;
-    if (unit >= as_const(a.l.header)[AH_UNITS]) return;
-    const PREFT_CONST AttnUnit *p = as_const(a.l.units) + unit;
     AttnUnit u;
-    u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
+    if constexpr (DIRECT) {
+        if (a.ready && !attn_schedule_is(a, KIND)) return;
+        const AttnDirect d = attn_direct<false>(a.s, unit);
+        if (!a.ready && blockIdx.x == 0 && threadIdx.x == 0) {
+            int32_t *h = a.l.header;
+            h[AH_UNITS] = d.units; h[AH_MERGES] = d.joined; h[AH_TILES] = d.tiles; h[AH_KIND] = KIND;
+            h[AH_GROUPS] = 0; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
+        }
+        if (!d.found) return;
+        u = attn_unit_of(a.s, d);
+    } else {
+        if (!attn_schedule_is(a, KIND) || unit >= as_const(a.l.header)[AH_UNITS]) return;
+        const PREFT_CONST AttnUnit *p = as_const(a.l.units) + unit;
+        u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
+    }
     if (u.ncols <= 0) return;
     if (u.ncols > ATTN_FEW_COLS) attend_columns<E, D, PAGED>(a, u, kv_head, (lds_t)lds, (int32_t *)join);
     else attend_keys<E, D, PAGED>(a, u, kv_head, (lds_t)lds, join);
@@ -665,43 +679,58 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
 
 // Joins the parts of a column: M = max m_j, out = sum 2^(m_j - M) o_j / sum 2^(m_j - M) l_j, in the order of the parts.  One wavefront a column.
 template <typename E, int D>
-__global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, int kind)
+__device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j, int kv_head)
 {
     using X = AttnTile<E, D>;
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, kv_head = blockIdx.y, G = a.group;
-    if (!attn_schedule_is(a, kind)) return;
-    const int32_t n = as_const(a.l.header)[AH_MERGES];
-    for (int32_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const AttnMerge j = a.l.merges[i];
-        for (int32_t c = blockIdx.z * 4 + wave; c < j.ncols; c += 4 * gridDim.z) {
-            const int32_t gc = j.group_col0 + c, tile = gc / ATTN_COLS;
-            const int32_t width = min(ATTN_COLS, j.group_cols - tile * ATTN_COLS);
-            const int64_t group = (int64_t)j.group_slot + (int64_t)tile * ATTN_COLS * a.kv_heads * j.group_parts + kv_head * width + gc % ATTN_COLS;
-            const int64_t mine = (int64_t)j.slot + kv_head * j.ncols + c;
-            const int32_t parts = j.parts + j.group_parts;
-            auto part = [&](int32_t k) {
-                const int64_t p = k < j.parts ? mine + (int64_t)k * j.ncols * a.kv_heads : group + (int64_t)(k - j.parts) * width * a.kv_heads;
-                return p < 0 || p >= a.l.slot_cap ? (int64_t)0 : p;
-            };
-            float top = ATTN_LOWEST;
-            for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, a.l.part_ml[part(k)].x);
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, G = a.group;
+    for (int32_t c = blockIdx.z * 4 + wave; c < j.ncols; c += 4 * gridDim.z) {
+        const int32_t gc = j.group_col0 + c, tile = gc / ATTN_COLS;
+        const int32_t width = min(ATTN_COLS, j.group_cols - tile * ATTN_COLS);
+        const int64_t group = (int64_t)j.group_slot + (int64_t)tile * ATTN_COLS * a.kv_heads * j.group_parts + kv_head * width + gc % ATTN_COLS;
+        const int64_t mine = (int64_t)j.slot + kv_head * j.ncols + c;
+        const int32_t parts = j.parts + j.group_parts;
+        auto part = [&](int32_t k) {
+            const int64_t p = k < j.parts ? mine + (int64_t)k * j.ncols * a.kv_heads : group + (int64_t)(k - j.parts) * width * a.kv_heads;
+            return p < 0 || p >= a.l.slot_cap ? (int64_t)0 : p;
+        };
+        float top = ATTN_LOWEST;
+        for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, a.l.part_ml[part(k)].x);
 #pragma unroll
-            for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-            float o[D / 64] = {}, l = 0.0f;
-            for (int32_t k = 0; k < parts; ++k) {
-                const int64_t p = part(k);
-                const float2 ml = a.l.part_ml[p];
-                const float f = __builtin_amdgcn_exp2f(ml.x - top);
-                l += ml.y * f;
+        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        float o[D / 64] = {}, l = 0.0f;
+#pragma unroll 4
+        for (int32_t k = 0; k < parts; ++k) {
+            const int64_t p = part(k);
+            const float2 ml = a.l.part_ml[p];
+            const float f = __builtin_amdgcn_exp2f(ml.x - top);
+            l += ml.y * f;
 #pragma unroll
-                for (int d = 0; d < D / 64; ++d) o[d] += a.l.part_o[p * D + d * 64 + lane] * f;
-            }
-            const float inv = inverse(l);
-            const int32_t q = (j.col0 + c) / G, head = kv_head * G + (j.col0 + c - q * G), row = max(0, min(j.row0 + q, a.T - 1));
-            E *to = (E *)((char *)a.out + (int64_t)row * a.ldo + head * X::ROW);
-#pragma unroll
-            for (int d = 0; d < D / 64; ++d) to[d * 64 + lane] = (E)(o[d] * inv);
+            for (int d = 0; d < D / 64; ++d) o[d] += a.l.part_o[p * D + d * 64 + lane] * f;
         }
+        const float inv = inverse(l);
+        const int32_t q = (j.col0 + c) / G, head = kv_head * G + (j.col0 + c - q * G), row = max(0, min(j.row0 + q, a.T - 1));
+        E *to = (E *)((char *)a.out + (int64_t)row * a.ldo + head * X::ROW);
+#pragma unroll
+        for (int d = 0; d < D / 64; ++d) to[d * 64 + lane] = (E)(o[d] * inv);
+    }
+}
+
+template <typename E, int D, bool DIRECT>
+__global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, int kind)
+{
+    if constexpr (DIRECT) {
+        if (a.ready && !attn_schedule_is(a, kind)) return;
+        const AttnDirect d = attn_direct<true>(a.s, (int32_t)blockIdx.x);
+        if (!d.found || d.parts <= 1) return;
+        AttnMerge j = {};
+        j.row0 = d.it.row0; j.col0 = d.tile * ATTN_COLS; j.ncols = min(ATTN_COLS, d.it.rows * a.group - j.col0);
+        j.parts = d.parts; j.slot = d.slot + j.col0 * d.parts * a.kv_heads;
+        j.group_cols = ATTN_COLS;
+        join_tile<E, D>(a, j, (int)blockIdx.y);
+    } else {
+        if (!attn_schedule_is(a, kind)) return;
+        const int32_t n = as_const(a.l.header)[AH_MERGES];
+        for (int32_t i = blockIdx.x; i < n; i += gridDim.x) join_tile<E, D>(a, a.l.merges[i], (int)blockIdx.y);
     }
 }
 

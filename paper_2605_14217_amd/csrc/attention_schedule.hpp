@@ -17,6 +17,7 @@ constexpr int ATTN_TARGET    = 512;   // workgroups that run side by side: two o
 constexpr int ATTN_GROUP_ROWS = 4096; // rows of groups that are listed; the rest see their prefix by themselves
 constexpr int ATTN_MIN_PREFIX = 64;   // shorter prefixes are not worth a part of their own
 constexpr int ATTN_SCAN      = 4096;  // items whose tile offsets are kept in LDS
+constexpr int ATTN_DIRECT    = 256;   // segments of a call whose workgroups find their unit by themselves, four a lane
 
 struct AttnUnit {
     int32_t table;     // row of the block table; packed keys: the row of key 0
@@ -111,21 +112,31 @@ __device__ __forceinline__ int32_t last_at_or_before(P first, int32_t n, int32_t
     return lo;
 }
 
+// Wide units (more than 32 columns: bound by the matrix cores) and narrow ones (bound by memory) take turns, ATTN_TURN narrow ones to a wide one, so that
+// a compute unit has one of each.
+constexpr int ATTN_TURN = 1;
+__device__ __forceinline__ int32_t place_of(int32_t i, int32_t wide, int32_t narrow)
+{
+    if (i < wide) return i + min(i * ATTN_TURN, narrow);
+    i -= wide;
+    return i + min(i / ATTN_TURN + 1, wide);
+}
+
 // One workgroup: the lists are a few kilobytes, and what a step waits for is the chain of reads and barriers, not the work.
-// Units stand in the order of falling cost (counting sort over 256 cost classes): the longest of a causal prompt begin first and the short ones
-// fill the ends.  Their order does not change a result: every unit has an output or part of its own.
+// Units of a kind stand in the order of falling cost (counting sort over 256 cost classes): the longest of a causal prompt begin first and the
+// short ones fill the ends.  Their order does not change a result: every unit has an output or part of its own.
 __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnScheduleArgs a)
 {
     __shared__ int32_t lds[32];
     __shared__ int32_t first_tile[ATTN_SCAN + 1];
-    __shared__ int32_t bins[256];
-    __shared__ int32_t n_units, n_merges, n_slots;
+    __shared__ int32_t bins[512];
+    __shared__ int32_t n_units, n_wide, n_merges, n_slots;
     __shared__ unsigned long long cost_sum;
     const int tid = threadIdx.x, nt = blockDim.x;
     const int32_t G = a.heads / a.kv_heads, items = a.S + a.n_groups;
     const bool in_lds = items <= ATTN_SCAN;
     if (tid == 0) { n_merges = 0; n_slots = 0; cost_sum = 0; }
-    for (int b = tid; b < 256; b += nt) bins[b] = 0;
+    for (int b = tid; b < 512; b += nt) bins[b] = 0;
 
     // groups: how many rows each has, and where they stand in the row list
     if (a.n_groups > 0) {
@@ -267,25 +278,26 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             const int32_t splits = n == 0 && g >= 0 ? 0 : ranges_of(n, range);     // 0: the group's part is all there is
             const bool parts = splits > 1 || g >= 0 || i >= a.S;
             const int32_t each = splits > 0 ? n / splits : 0;
-            const int32_t cls = 255 - (each < 128 ? each : min(255, 128 + (each - 128) / 16));
+            const int32_t cls = (u.ncols > ATTN_FEW_COLS ? 0 : 256) + 255 - (each < 128 ? each : min(255, 128 + (each - 128) / 16));
             if (pass == 0) {
                 if (splits > 0) atomicAdd(&bins[cls], splits);
                 continue;
             }
-            int32_t at = splits > 0 ? atomicAdd(&bins[cls], splits) : 0;
+            const int32_t at = splits > 0 ? atomicAdd(&bins[cls], splits) : 0;
             int32_t slot = -1;
             const int32_t step = u.ncols * a.kv_heads;
             if (i >= a.S) slot = a.l.group_slot[i - a.S] + tile * ATTN_COLS * a.kv_heads * splits;
             else if (parts) slot = atomicAdd(&n_slots, splits * step);
             const bool fits = !parts || (slot >= 0 && (int64_t)slot + (int64_t)splits * step <= a.l.slot_cap);   // not so: the tables are malformed
-            for (int32_t k = 0; k < splits; ++k, ++at) {
+            for (int32_t k = 0; k < splits; ++k) {
                 const int32_t first = it.key0 / ATTN_KEYS;
                 const int64_t k0 = first + (int64_t)n * k / splits, k1 = first + (int64_t)n * (k + 1) / splits;
                 u.key0 = max(it.key0, (int32_t)(k0 * ATTN_KEYS));
                 u.key1 = max(u.key0, (int32_t)min((int64_t)key1, k1 * ATTN_KEYS));
                 u.slot = parts ? slot + k * step : -1;
                 if (!fits) { u.slot = 0; u.ncols = 0; }
-                if (at < a.l.unit_cap) a.l.units[at] = u;
+                const int32_t to = place_of(at + k, n_wide, n_units - n_wide);
+                if (to >= 0 && to < a.l.unit_cap) a.l.units[to] = u;
             }
             if (parts && i < a.S && fits) {
                 AttnMerge j;
@@ -301,18 +313,127 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         __syncthreads();
         if (pass == 0) {
             int32_t total;
-            const int32_t v = tid < 256 ? bins[tid] : 0;
-            const int32_t before = block_exclusive_scan(v, lds, &total);
-            if (tid < 256) bins[tid] = before;
-            if (tid == 0) n_units = min(total, a.l.unit_cap);
+            const int32_t v0 = tid < 256 ? bins[2 * tid] : 0, v1 = tid < 256 ? bins[2 * tid + 1] : 0;
+            const int32_t before = block_exclusive_scan(v0 + v1, lds, &total);
+            if (tid < 256) { bins[2 * tid] = before; bins[2 * tid + 1] = before + v0; }
+            if (tid == 128) n_wide = before;
+            if (tid == 0) n_units = total;
             __syncthreads();
         }
     }
     if (tid == 0) {
         int32_t *h = a.l.header;
-        h[AH_UNITS] = n_units; h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
+        h[AH_UNITS] = min(n_units, a.l.unit_cap); h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
         h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
     }
+}
+
+// ---------------------------------------------------------------------------------------
+// Without a schedule kernel: a wavefront finds the unit (or the tile to join) of its workgroup from the tables by itself, in a microsecond where the
+// kernel would take six.  For calls of few segments and workgroups, without groups.  All tiles of a segment are cut into as many ranges, so that the sums over the
+// segments before are all it takes.
+// ---------------------------------------------------------------------------------------
+struct AttnDirect {
+    AttnItem it;
+    int32_t s, tile, part, parts;      // parts 1: the unit writes the result
+    int32_t slot;                      // first part column of the segment
+    int32_t units, tiles, joined;      // of the call, for index 0
+    bool found;
+};
+
+__device__ __forceinline__ int32_t wave_inclusive(int32_t v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int32_t up = __shfl_up(v, off, 64);
+        if (lane >= off) v += up;
+    }
+    return v;
+}
+
+// the unit `index` of the call, or with BY_TILE its tile `index`
+template <bool BY_TILE>
+__device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int32_t index)
+{
+    constexpr int EACH = ATTN_DIRECT / 64;
+    const int lane = threadIdx.x & 63, G = a.heads / a.kv_heads;
+    AttnItem it[EACH];
+    int32_t tiles[EACH], cost = 0;
+#pragma unroll
+    for (int c = 0; c < EACH; ++c) {
+        it[c] = AttnItem{0, 0, 0, 0, 0};
+        tiles[c] = 0;
+        if (c * 64 >= a.S) continue;
+        const int32_t s = c * 64 + lane;
+        if (s < a.S) it[c] = attn_segment(a, s);
+        tiles[c] = (it[c].rows * G + ATTN_COLS - 1) / ATTN_COLS;
+        if (tiles[c] > 0) {
+            const int32_t low = min(it[c].key1, it[c].lim0 + (min(it[c].rows * G, ATTN_COLS) - 1) / G);
+            cost += (int32_t)min(((int64_t)tiles[c] * (key_tiles(0, low) + key_tiles(0, it[c].key1) + 1)) / 2, (int64_t)(INT32_MAX / 1024));
+        }
+    }
+    int32_t range = INT32_MAX;
+    if (a.can_split) {
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) cost += __shfl_xor(cost, off, 64);
+        range = max(a.min_tiles, (int32_t)min(((int64_t)cost * a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET, (int64_t)INT32_MAX));
+    }
+    AttnDirect r = {};
+    int32_t before = 0, slots = 0;
+#pragma unroll
+    for (int c = 0; c < EACH; ++c) {
+        if (c * 64 >= a.S) continue;
+        const int32_t parts = ranges_of(key_tiles(0, it[c].key1), range), units = tiles[c] * parts;
+        const int32_t mine = BY_TILE ? tiles[c] : units;
+        const int32_t need = parts > 1 ? (int32_t)min((int64_t)it[c].rows * G * parts * a.kv_heads, (int64_t)a.l.slot_cap) : 0;
+        const int32_t upto = wave_inclusive(mine), slot = wave_inclusive(need);
+        const uint64_t past = __ballot(before + upto > index);
+        if (!r.found && past != 0) {
+            const int at = __builtin_ctzll(past);
+            auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
+            const int32_t i = index - before - (of(upto) - of(mine));
+            r.found = true;
+            r.s = c * 64 + at;
+            r.it.row0 = of(it[c].row0); r.it.rows = of(it[c].rows); r.it.lim0 = of(it[c].lim0); r.it.key0 = 0; r.it.key1 = of(it[c].key1);
+            r.parts = of(parts);
+            r.tile = BY_TILE ? i : i / r.parts;
+            r.part = BY_TILE ? 0 : i - r.tile * r.parts;
+            r.slot = slots + of(slot) - of(need);
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+        slots += __builtin_amdgcn_readlane(slot, 63);
+        if (!BY_TILE && index == 0) {
+            r.tiles += __builtin_amdgcn_readlane(wave_inclusive(tiles[c]), 63);
+            r.joined += __builtin_amdgcn_readlane(wave_inclusive(parts > 1 ? tiles[c] : 0), 63);
+        }
+    }
+    r.units = before;
+    return r;
+}
+
+__device__ __forceinline__ AttnUnit attn_unit_of(const AttnScheduleArgs &a, const AttnDirect &d)
+{
+    const int32_t G = a.heads / a.kv_heads;
+    AttnUnit u;
+    // the last tile of a causal prompt sees the most keys: it begins first
+    const int32_t tiles = (d.it.rows * G + ATTN_COLS - 1) / ATTN_COLS, tile = tiles - 1 - d.tile;
+    const int32_t col0 = tile * ATTN_COLS, first = col0 / G;
+    u.table = a.kv_len ? d.s : d.it.row0;
+    u.ncols = min(ATTN_COLS, d.it.rows * G - col0);
+    u.head0 = col0 - first * G;
+    u.row0 = d.it.row0 + first;
+    u.lim0 = d.it.lim0 + first;
+    const int32_t key1 = min(d.it.key1, u.lim0 + (u.head0 + u.ncols - 1) / G), n = key_tiles(0, key1);
+    const int32_t k0 = (int32_t)((int64_t)n * d.part / d.parts), k1 = (int32_t)((int64_t)n * (d.part + 1) / d.parts);
+    u.key0 = k0 * ATTN_KEYS;
+    u.key1 = max(u.key0, (int32_t)min((int64_t)key1, (int64_t)k1 * ATTN_KEYS));
+    u.slot = -1;
+    if (d.parts > 1) {
+        u.slot = d.slot + col0 * d.parts * a.kv_heads + d.part * u.ncols * a.kv_heads;
+        if (u.slot < 0 || (int64_t)u.slot + (int64_t)u.ncols * a.kv_heads > a.l.slot_cap) u.ncols = 0;      // malformed tables
+    }
+    return u;
 }
 
 }  // namespace preft
