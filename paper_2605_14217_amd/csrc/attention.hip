@@ -18,7 +18,7 @@ using namespace preft;
 //   part columns   a tile that is cut has at most twice n / range parts of at most 128 columns; rows of groups have one of their own and their group's.
 struct Layout {
     int32_t tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
-    size_t units, merges, group_rows, tiles, rows_before, group_of, group_list, group_slot, part_ml, part_o, bytes;
+    size_t units, merges, group_rows, tiles, rows_before, group_of, group_list, group_slot, group_low, part_ml, part_o, bytes;
 };
 
 Layout layout_of(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
@@ -42,6 +42,7 @@ Layout layout_of(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t 
     l.group_of = take(groups > 0 ? (size_t)S * 4 : 0);
     l.group_list = take((size_t)groups * 4);
     l.group_slot = take((size_t)groups * 4);
+    l.group_low = take((size_t)groups * 4);
     l.part_ml = take((size_t)l.slot_cap * sizeof(float2));
     l.part_o = take((size_t)l.slot_cap * D * 4);
     l.bytes = at;
@@ -61,6 +62,7 @@ AttnLists lists_of(const Layout &l, void *workspace)
     r.group_of = (int32_t *)(p + l.group_of);
     r.group_list = (int32_t *)(p + l.group_list);
     r.group_slot = (int32_t *)(p + l.group_slot);
+    r.group_low = (int32_t *)(p + l.group_low);
     r.part_ml = (float2 *)(p + l.part_ml);
     r.part_o = (float *)(p + l.part_o);
     r.tile_cap = l.tile_cap; r.unit_cap = l.unit_cap; r.merge_cap = l.merge_cap; r.group_row_cap = l.group_row_cap; r.slot_cap = l.slot_cap;
@@ -80,7 +82,7 @@ Plan plan_of(const AttnScheduleArgs &s, int64_t most_keys)
     Plan p;
     const int64_t key_tiles = (most_keys + ATTN_KEYS - 1) / ATTN_KEYS;
     p.tiles = s.l.tile_cap;
-    p.split = s.can_split && key_tiles > s.min_tiles;
+    p.split = s.can_split && key_tiles > 2 * s.min_tiles;
     p.direct = s.n_groups == 0 && s.S <= ATTN_DIRECT && p.tiles * s.kv_heads <= 2 * ATTN_TARGET;
     const int64_t ranges = (ATTN_TARGET + s.kv_heads - 1) / s.kv_heads;
     p.units = !p.split ? p.tiles : p.direct ? p.tiles + 2 * ranges + 2 : 3 * p.tiles + ranges + 2;
@@ -167,10 +169,12 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.l = lists_of(l, workspace);
     AttnScheduleArgs &s = a.s;
-    s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads;
+    s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = a.group;
     s.max_keys = T; s.l = a.l;
-    s.can_split = (int64_t)l.tile_cap * n_kv_heads < 4 * ATTN_TARGET;              // else there are tiles enough
-    s.min_tiles = dtype == PREFT_BF16 ? 8 : 2;
+    // Cut only where the prompts are long on average and their tiles do not fill the chip twice over: a prompt has tiles by its rows as it has keys, and a
+    // merge launch with nothing to join costs 4 us of the 10 that a batch of chat-length prompts takes.
+    s.can_split = (int64_t)l.tile_cap * n_kv_heads < 2 * ATTN_TARGET && T >= 512 * (int64_t)S;
+    s.min_tiles = dtype == PREFT_BF16 ? 8 : 4;
     return run<false>(a, dtype, head_dim, mode, T, st);
 }
 
@@ -208,7 +212,7 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     a.l = lists_of(l, workspace);
     AttnScheduleArgs &s = a.s;
     s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.kv_len = kv_len; s.group_start = group_start; s.group_prefix = group_prefix_len;
-    s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads; s.l = a.l;
+    s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = a.group; s.l = a.l;
     const int64_t most = (int64_t)max_pages << shift;
     s.max_keys = keys ? (int32_t)(most < (1 << 30) ? most : (1 << 30)) : 0;
     s.can_split = 1;

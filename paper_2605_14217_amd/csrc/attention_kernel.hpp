@@ -689,23 +689,40 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
         const int64_t group = (int64_t)j.group_slot + (int64_t)tile * ATTN_COLS * a.kv_heads * j.group_parts + kv_head * width + gc % ATTN_COLS;
         const int64_t mine = (int64_t)j.slot + kv_head * j.ncols + c;
         const int32_t parts = j.parts + j.group_parts;
-        auto part = [&](int32_t k) {
+        auto part = [&](int32_t k) {                               // slots are below 2^31: checked where the workspace is laid out
             const int64_t p = k < j.parts ? mine + (int64_t)k * j.ncols * a.kv_heads : group + (int64_t)(k - j.parts) * width * a.kv_heads;
-            return p < 0 || p >= a.l.slot_cap ? (int64_t)0 : p;
+            return p < 0 || p >= a.l.slot_cap ? 0 : (int32_t)p;
         };
+        // a lane has the place and the factor of a part, 64 parts at a time; their rows are then read eight at a time, with nothing to wait for in between
         float top = ATTN_LOWEST;
         for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, a.l.part_ml[part(k)].x);
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
         float o[D / 64] = {}, l = 0.0f;
-#pragma unroll 4
-        for (int32_t k = 0; k < parts; ++k) {
-            const int64_t p = part(k);
-            const float2 ml = a.l.part_ml[p];
+        for (int32_t k0 = 0; k0 < parts; k0 += 64) {
+            const int32_t n = min(64, parts - k0), at = part(min(k0 + lane, parts - 1));
+            const float2 ml = a.l.part_ml[at];
             const float f = __builtin_amdgcn_exp2f(ml.x - top);
-            l += ml.y * f;
+            float sum = lane < n ? ml.y * f : 0.0f;
 #pragma unroll
-            for (int d = 0; d < D / 64; ++d) o[d] += a.l.part_o[p * D + d * 64 + lane] * f;
+            for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+            l += sum;
+            for (int32_t k = 0; k < n; k += 8) {
+                float x[8][D / 64] = {};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (k + e >= n) continue;
+                    const float *from = a.l.part_o + (int64_t)__builtin_amdgcn_readlane(at, k + e) * D + lane;
+#pragma unroll
+                    for (int d = 0; d < D / 64; ++d) x[e][d] = from[d * 64];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), min(k + e, n - 1)));
+#pragma unroll
+                    for (int d = 0; d < D / 64; ++d) o[d] += x[e][d] * w;
+                }
+            }
         }
         const float inv = inverse(l);
         const int32_t q = (j.col0 + c) / G, head = kv_head * G + (j.col0 + c - q * G), row = max(0, min(j.row0 + q, a.T - 1));

@@ -45,6 +45,7 @@ struct AttnLists {
     int32_t   *group_of;   // [S]
     int32_t   *group_list; // [groups] first entry in group_rows, or -1
     int32_t   *group_slot; // [groups] first part column of the group's units
+    int32_t   *group_low;  // [groups] keys that all of the group's rows see
     float     *part_o;     // [slots][head_dim]
     float2    *part_ml;    // [slots] {largest exponent, sum}
     int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
@@ -56,7 +57,7 @@ struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
     const int32_t *kv_len;                                 // null: packed whole prompts
     const int32_t *group_start, *group_prefix;
-    int32_t S, T, n_groups, heads, kv_heads, max_keys, can_split, min_tiles;
+    int32_t S, T, n_groups, heads, kv_heads, group, max_keys, can_split, min_tiles;    // group: heads / kv_heads
     AttnLists l;
 };
 
@@ -83,10 +84,15 @@ __device__ __forceinline__ AttnItem attn_segment(const AttnScheduleArgs &a, int3
     return r;
 }
 
-__device__ __forceinline__ int32_t ceil_div(int32_t a, int32_t b) { return (int32_t)(((int64_t)a + b - 1) / b); }
 __device__ __forceinline__ int32_t key_tiles(int32_t key0, int32_t key1) { return key1 > key0 ? (key1 - 1) / ATTN_KEYS - key0 / ATTN_KEYS + 1 : 0; }
 
-__device__ __forceinline__ int32_t ranges_of(int32_t tiles, int32_t range) { return tiles > range ? ceil_div(tiles, range) : 1; }
+__device__ __forceinline__ int32_t ranges_of(int32_t tiles, int32_t range) { return tiles > range ? (int32_t)((uint32_t)(tiles - 1) / (uint32_t)range) + 1 : 1; }
+// where part k of `parts` of n tiles begins: the first n % parts have one more
+__device__ __forceinline__ int32_t part_begin(int32_t n, int32_t parts, int32_t k)
+{
+    const int32_t each = (int32_t)((uint32_t)n / (uint32_t)parts);
+    return each * k + min(k, n - each * parts);
+}
 
 struct AttnGroup { int32_t begin, end, rows, prefix; };
 
@@ -112,28 +118,19 @@ __device__ __forceinline__ int32_t last_at_or_before(P first, int32_t n, int32_t
     return lo;
 }
 
-// Wide units (more than 32 columns: bound by the matrix cores) and narrow ones (bound by memory) take turns, ATTN_TURN narrow ones to a wide one, so that
-// a compute unit has one of each.
-constexpr int ATTN_TURN = 1;
-__device__ __forceinline__ int32_t place_of(int32_t i, int32_t wide, int32_t narrow)
-{
-    if (i < wide) return i + min(i * ATTN_TURN, narrow);
-    i -= wide;
-    return i + min(i / ATTN_TURN + 1, wide);
-}
-
 // One workgroup: the lists are a few kilobytes, and what a step waits for is the chain of reads and barriers, not the work.
-// Units of a kind stand in the order of falling cost (counting sort over 256 cost classes): the longest of a causal prompt begin first and the
-// short ones fill the ends.  Their order does not change a result: every unit has an output or part of its own.
+// Wide units (more than 32 columns) come first, and units of a kind stand in the order of falling cost (counting sort over 256 cost classes): the longest
+// of a causal prompt begin first and the short ones fill the ends.  (Wide units, bound by the matrix cores, and narrow ones, bound by memory, in turns, so
+// that a compute unit has one of each: 229 us against 187 on 256 rows of 64 heads with prefixes of 8192 -- the wide ones then end late.)  Their order does not change a result: every unit has an output or part of its own.
 __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnScheduleArgs a)
 {
     __shared__ int32_t lds[32];
     __shared__ int32_t first_tile[ATTN_SCAN + 1];
     __shared__ int32_t bins[512];
-    __shared__ int32_t n_units, n_wide, n_merges, n_slots;
+    __shared__ int32_t n_units, n_merges, n_slots;
     __shared__ unsigned long long cost_sum;
     const int tid = threadIdx.x, nt = blockDim.x;
-    const int32_t G = a.heads / a.kv_heads, items = a.S + a.n_groups;
+    const int32_t G = a.group, items = a.S + a.n_groups;
     const bool in_lds = items <= ATTN_SCAN;
     if (tid == 0) { n_merges = 0; n_slots = 0; cost_sum = 0; }
     for (int b = tid; b < 512; b += nt) bins[b] = 0;
@@ -161,7 +158,10 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             }
             const int32_t before = block_exclusive_scan(rows, lds, &total);
             const int64_t end = (int64_t)carry + before + rows;
-            if (g < a.n_groups) a.l.group_list[g] = rows > 0 && end <= a.l.group_row_cap ? carry + before : -1;
+            if (g < a.n_groups) {
+                a.l.group_list[g] = rows > 0 && end <= a.l.group_row_cap ? carry + before : -1;
+                a.l.group_low[g] = max(0, min(a.group_prefix[g], a.max_keys));
+            }
             carry = (int32_t)min((int64_t)INT32_MAX / 2, (int64_t)carry + total);
         }
         __syncthreads();
@@ -184,6 +184,7 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
                     const int32_t at = a.l.group_list[g] + a.l.rows_before[i] - a.l.rows_before[m.begin];
                     for (int32_t r = 0; r < it.rows; ++r)
                         if (at + r < a.l.group_row_cap) a.l.group_rows[at + r] = make_int2(it.row0 + r, min(it.lim0 + r, m.prefix));
+                    if (it.rows > 0 && it.lim0 < m.prefix) atomicMin(&a.l.group_low[g], it.lim0);
                     it.key0 = m.prefix;
                 }
             }
@@ -270,9 +271,7 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             } else {
                 const int32_t at = a.l.group_list[i - a.S] + first;
                 u.row0 = -1 - at;
-                u.lim0 = key1;
-                if (pass == 1)
-                    for (int32_t r = 0; r < rows; ++r) u.lim0 = min(u.lim0, a.l.group_rows[min(at + r, a.l.group_row_cap - 1)].y);
+                u.lim0 = __hip_atomic_load(&a.l.group_low[i - a.S], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             const int32_t n = key_tiles(it.key0, key1);
             const int32_t splits = n == 0 && g >= 0 ? 0 : ranges_of(n, range);     // 0: the group's part is all there is
@@ -291,13 +290,12 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             const bool fits = !parts || (slot >= 0 && (int64_t)slot + (int64_t)splits * step <= a.l.slot_cap);   // not so: the tables are malformed
             for (int32_t k = 0; k < splits; ++k) {
                 const int32_t first = it.key0 / ATTN_KEYS;
-                const int64_t k0 = first + (int64_t)n * k / splits, k1 = first + (int64_t)n * (k + 1) / splits;
+                const int64_t k0 = first + part_begin(n, splits, k), k1 = first + part_begin(n, splits, k + 1);
                 u.key0 = max(it.key0, (int32_t)(k0 * ATTN_KEYS));
                 u.key1 = max(u.key0, (int32_t)min((int64_t)key1, k1 * ATTN_KEYS));
                 u.slot = parts ? slot + k * step : -1;
                 if (!fits) { u.slot = 0; u.ncols = 0; }
-                const int32_t to = place_of(at + k, n_wide, n_units - n_wide);
-                if (to >= 0 && to < a.l.unit_cap) a.l.units[to] = u;
+                if (at + k < a.l.unit_cap) a.l.units[at + k] = u;
             }
             if (parts && i < a.S && fits) {
                 AttnMerge j;
@@ -316,7 +314,6 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             const int32_t v0 = tid < 256 ? bins[2 * tid] : 0, v1 = tid < 256 ? bins[2 * tid + 1] : 0;
             const int32_t before = block_exclusive_scan(v0 + v1, lds, &total);
             if (tid < 256) { bins[2 * tid] = before; bins[2 * tid + 1] = before + v0; }
-            if (tid == 128) n_wide = before;
             if (tid == 0) n_units = total;
             __syncthreads();
         }
@@ -357,7 +354,7 @@ template <bool BY_TILE>
 __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int32_t index)
 {
     constexpr int EACH = ATTN_DIRECT / 64;
-    const int lane = threadIdx.x & 63, G = a.heads / a.kv_heads;
+    const int lane = threadIdx.x & 63, G = a.group;
     AttnItem it[EACH];
     int32_t tiles[EACH], cost = 0;
 #pragma unroll
@@ -377,7 +374,7 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
     if (a.can_split) {
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) cost += __shfl_xor(cost, off, 64);
-        range = max(a.min_tiles, (int32_t)min(((int64_t)cost * a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET, (int64_t)INT32_MAX));
+        range = max(a.min_tiles, (int32_t)min(((uint64_t)(uint32_t)cost * (uint32_t)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET, (uint64_t)INT32_MAX));
     }
     AttnDirect r = {};
     int32_t before = 0, slots = 0;
@@ -397,7 +394,7 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
             r.s = c * 64 + at;
             r.it.row0 = of(it[c].row0); r.it.rows = of(it[c].rows); r.it.lim0 = of(it[c].lim0); r.it.key0 = 0; r.it.key1 = of(it[c].key1);
             r.parts = of(parts);
-            r.tile = BY_TILE ? i : i / r.parts;
+            r.tile = BY_TILE || r.parts == 1 ? i : (int32_t)((uint32_t)i / (uint32_t)r.parts);
             r.part = BY_TILE ? 0 : i - r.tile * r.parts;
             r.slot = slots + of(slot) - of(need);
         }
@@ -414,7 +411,7 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
 
 __device__ __forceinline__ AttnUnit attn_unit_of(const AttnScheduleArgs &a, const AttnDirect &d)
 {
-    const int32_t G = a.heads / a.kv_heads;
+    const int32_t G = a.group;
     AttnUnit u;
     // the last tile of a causal prompt sees the most keys: it begins first
     const int32_t tiles = (d.it.rows * G + ATTN_COLS - 1) / ATTN_COLS, tile = tiles - 1 - d.tile;
@@ -425,7 +422,7 @@ __device__ __forceinline__ AttnUnit attn_unit_of(const AttnScheduleArgs &a, cons
     u.row0 = d.it.row0 + first;
     u.lim0 = d.it.lim0 + first;
     const int32_t key1 = min(d.it.key1, u.lim0 + (u.head0 + u.ncols - 1) / G), n = key_tiles(0, key1);
-    const int32_t k0 = (int32_t)((int64_t)n * d.part / d.parts), k1 = (int32_t)((int64_t)n * (d.part + 1) / d.parts);
+    const int32_t k0 = part_begin(n, d.parts, d.part), k1 = part_begin(n, d.parts, d.part + 1);
     u.key0 = k0 * ATTN_KEYS;
     u.key1 = max(u.key0, (int32_t)min((int64_t)key1, (int64_t)k1 * ATTN_KEYS));
     u.slot = -1;

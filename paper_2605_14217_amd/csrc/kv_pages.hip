@@ -19,52 +19,78 @@ struct PlanArgs {
 
 constexpr int PLAN_THREADS = 1024;
 
+struct PlanRequest { int32_t lo, hi, ctx, need, over; };     // rows, tokens before them, pages to begin within and beyond the table
+
+__device__ __forceinline__ PlanRequest plan_request(const PlanArgs &a, int32_t s)
+{
+    PlanRequest r;
+    const int32_t page = 1 << a.page_shift;
+    r.lo = max(0, min(a.seg_start[s], a.T));
+    r.hi = max(r.lo, min(a.seg_start[s + 1], a.T));
+    r.ctx = max(0, min(a.ctx_len[s], INT32_MAX - (r.hi - r.lo)));
+    const int32_t have = (int32_t)(((int64_t)r.ctx + page - 1) >> a.page_shift), want = (int32_t)(((int64_t)r.ctx + (r.hi - r.lo) + page - 1) >> a.page_shift);
+    r.need = min(want, a.max_pages) - min(have, a.max_pages);
+    r.over = want - have - r.need;
+    return r;
+}
+
 // have = ceil(ctx / page), want = ceil((ctx + n) / page), both cut at max_pages; page k of a request, have <= k < want, is
 // free_pages[off + k - have] with off = sum of want - have over the requests before it.  Latency is what bounds it: a handful of
-// bytes per request, and a chain of reads.  Every workgroup therefore sums the requests before its rows by itself (four bytes each,
-// from the cache) instead of waiting for another launch to do it, keeps the requests that own its rows in LDS, and writes its rows; the last one,
-// which walks all requests, writes kv_len and the counts.  32 requests: 6 us; 4096 requests and 356 000 rows: see the table of DESIGN.
+// bytes per request, and a chain of reads.  Every workgroup therefore sums the requests before its rows by itself (eight bytes each, from the cache, all
+// reads in flight at once) instead of waiting for another launch to do it, keeps the requests that own its rows in LDS, and writes its rows; the
+// last one sums all requests and writes kv_len and the counts.
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a)
 {
     __shared__ int32_t lds[32];
+    __shared__ int64_t sums[3][PLAN_THREADS / 64];
     __shared__ int32_t own_start[PLAN_THREADS], own_end[PLAN_THREADS], own_ctx[PLAN_THREADS], own_off[PLAN_THREADS], own_seg[PLAN_THREADS];
-    const int32_t page = 1 << a.page_shift, n_threads = (int32_t)blockDim.x;
+    const int32_t page = 1 << a.page_shift, n_threads = (int32_t)blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t row0 = (int32_t)blockIdx.x * n_threads, row1 = min(a.T, row0 + n_threads);
     const bool last = blockIdx.x + 1 == gridDim.x;
+    // requests that end before this workgroup's rows: their pages, and how many they are; all requests: their pages, and those that do not fit the table
+    int64_t before = 0, all = 0, over = 0;
+    int32_t first = 0;
+#pragma unroll 4
+    for (int32_t s = (int32_t)threadIdx.x; s < a.S; s += n_threads) {
+        const PlanRequest r = plan_request(a, s);
+        if (r.hi <= row0) { before += r.need; ++first; }
+        all += r.need;
+        over += r.over;
+        if (last) a.kv_len[s] = r.ctx + (r.hi - r.lo);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        before += __shfl_xor(before, off, 64);
+        first += __shfl_xor(first, off, 64);
+        if (last) { all += __shfl_xor(all, off, 64); over += __shfl_xor(over, off, 64); }
+    }
+    if (lane == 0) { lds[wave] = first; sums[0][wave] = before; sums[1][wave] = all; sums[2][wave] = over; }
+    __syncthreads();
+    before = all = over = 0;
+    first = 0;
+    for (int w = 0; w < n_threads / 64; ++w) { first += lds[w]; before += sums[0][w]; all += sums[1][w]; over += sums[2][w]; }
+    if (last && threadIdx.x == 0) {
+        const int64_t taken = min((int64_t)a.n_free, all);
+        a.counts[0] = (int32_t)taken;
+        a.counts[1] = (int32_t)min((int64_t)INT32_MAX, all - taken + over);
+    }
+    int64_t off = before;
     int32_t owned = 0;
-    int64_t off = 0, missing = 0;
-    for (int32_t s0 = 0; s0 < a.S; s0 += n_threads) {
+    for (int32_t s0 = first; s0 < a.S; s0 += n_threads) {
         const int32_t s = s0 + (int32_t)threadIdx.x;
-        int32_t lo = 0, hi = 0, ctx = 0, need = 0, over = 0;
-        if (s < a.S) {
-            lo = max(0, min(a.seg_start[s], a.T));
-            hi = max(lo, min(a.seg_start[s + 1], a.T));
-            ctx = max(0, min(a.ctx_len[s], INT32_MAX - (hi - lo)));
-            const int32_t len = ctx + (hi - lo);
-            const int32_t have = (int32_t)(((int64_t)ctx + page - 1) >> a.page_shift), want = (int32_t)(((int64_t)len + page - 1) >> a.page_shift);
-            need = min(want, a.max_pages) - min(have, a.max_pages);
-            over = want - have - need;
-            if (last) a.kv_len[s] = len;
-        }
+        PlanRequest r = {};
+        if (s < a.S) r = plan_request(a, s);
         int32_t total, mine;
-        const int32_t before = block_exclusive_scan(need, lds, &total);
-        const bool owns = hi > lo && lo < row1 && hi > row0;
+        const int32_t here = block_exclusive_scan(r.need, lds, &total);
+        const bool owns = r.hi > r.lo && r.lo < row1 && r.hi > row0;
         const int32_t at = owned + block_exclusive_scan(owns ? 1 : 0, lds, &mine);
         if (owns && at < n_threads) {                  // well-formed segments do not share rows: at most one for every row
-            own_start[at] = lo; own_end[at] = hi; own_ctx[at] = ctx; own_seg[at] = s;
-            own_off[at] = (int32_t)min((int64_t)INT32_MAX, off + before);
+            own_start[at] = r.lo; own_end[at] = r.hi; own_ctx[at] = r.ctx; own_seg[at] = s;
+            own_off[at] = (int32_t)min((int64_t)INT32_MAX, off + here);
         }
         owned = min(n_threads, owned + mine);
         off += total;
-        if (last) {
-            int32_t sum;
-            block_exclusive_scan(over, lds, &sum);
-            missing += sum;
-        } else if (a.seg_start[min(s0 + n_threads, a.S)] >= row1) break;
-    }
-    if (last && threadIdx.x == 0) {
-        a.counts[0] = (int32_t)min((int64_t)a.n_free, off);
-        a.counts[1] = (int32_t)min((int64_t)INT32_MAX, off - min((int64_t)a.n_free, off) + missing);
+        if (a.seg_start[min(s0 + n_threads, a.S)] >= row1) break;
     }
     __syncthreads();
     const int32_t row = row0 + (int32_t)threadIdx.x;
