@@ -416,9 +416,9 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
         src.template copy<false, COPIES>(to, key, wave * ROWS);
         src.template copy<true, COPIES>(to + 2 * X::TILE, key, wave * ROWS);
     };
-    if (n > 0) fetch(0);
     AttnColumns<E, D> w;
     w.init(a, u, kv_head, wave * 32);
+    if (n > 0) fetch(0);
     w.arrived();
     const int32_t low = min(u.lim0, u.key1), high = u.key1;       // keys that every column sees, and that some column sees
     const float c = a.scale_log2;
@@ -534,12 +534,12 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     const int32_t base = u.key0 / 32 * 32, blocks = u.key1 > u.key0 ? (u.key1 - 1 - base) / 32 + 1 : 0, n = (blocks - wave + 3) / 4;
     const int32_t skip = wave == 0 && u.key0 > base ? 1 : 0;
     auto key_of = [&](int32_t i) { return base + (wave + 4 * (i + skip < n ? i + skip : i + skip - n)) * 32; };
+    AttnColumns<E, D> w;
+    w.init(a, u, kv_head, 0);                                     // the queries are on their way while the first page is looked up
     if (n > 0) {
         src.template copy<false, COPIES>(ka, key_of(0), 0);
         src.template copy<true, COPIES>(va, key_of(0), 0);
     }
-    AttnColumns<E, D> w;
-    w.init(a, u, kv_head, 0);
     const float c = a.scale_log2;
     w.arrived();
     const int32_t low = min(u.lim0, u.key1), before = (low - base) / 32 - wave;            // blocks from this wavefront's first on that all columns see whole

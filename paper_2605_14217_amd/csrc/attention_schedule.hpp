@@ -237,87 +237,97 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         __syncthreads();
     }
 
-    for (int pass = 0; pass < 2; ++pass) {
-        for (int32_t t = tid; t < n_tiles; t += nt) {
-            const int32_t i = in_lds ? last_at_or_before(first_tile, items, t) : last_at_or_before(a.l.tiles, items, t);
-            const int32_t tile = t - (in_lds ? first_tile[i] : a.l.tiles[i]);
-            AttnUnit u;
-            AttnItem it;
-            AttnGroup m = {0, 0, 0, 0};
-            int32_t g = -1, group_ranges = 0;
-            if (i < a.S) {
-                it = attn_segment(a, i);
-                if (a.n_groups > 0) g = a.l.group_of[i];
-                if (g >= 0) {
-                    m = attn_group(a, g);
-                    it.key0 = m.prefix;
-                    group_ranges = ranges_of(key_tiles(0, m.prefix), range);
-                }
-                u.table = a.kv_len ? i : it.row0;
-            } else {
-                m = attn_group(a, i - a.S);
-                it.rows = m.rows; it.key0 = 0; it.key1 = m.prefix;
-                u.table = min(m.begin, a.S - 1);
+    struct Tile {
+        AttnUnit u;
+        int32_t n, splits, cls, key0, key1, group_ranges, col0, rows0, i, g, begin, group_cols;
+        bool parts;
+    };
+    auto describe = [&](int32_t t) {
+        Tile d;
+        const int32_t i = in_lds ? last_at_or_before(first_tile, items, t) : last_at_or_before(a.l.tiles, items, t);
+        const int32_t tile = t - (in_lds ? first_tile[i] : a.l.tiles[i]);
+        AttnItem it;
+        AttnGroup m = {0, 0, 0, 0};
+        d.i = i; d.g = -1; d.group_ranges = 0;
+        if (i < a.S) {
+            it = attn_segment(a, i);
+            if (a.n_groups > 0) d.g = a.l.group_of[i];
+            if (d.g >= 0) {
+                m = attn_group(a, d.g);
+                it.key0 = m.prefix;
+                d.group_ranges = ranges_of(key_tiles(0, m.prefix), range);
             }
-            const int32_t col0 = tile * ATTN_COLS, first = col0 / G;
-            u.ncols = min(ATTN_COLS, it.rows * G - col0);
-            u.head0 = col0 - first * G;
-            const int32_t rows = (u.head0 + u.ncols - 1) / G + 1;
-            int32_t key1 = it.key1;
-            if (i < a.S) {
-                u.row0 = it.row0 + first;
-                u.lim0 = it.lim0 + first;
-                key1 = min(key1, u.lim0 + rows - 1);
-            } else {
-                const int32_t at = a.l.group_list[i - a.S] + first;
-                u.row0 = -1 - at;
-                u.lim0 = __hip_atomic_load(&a.l.group_low[i - a.S], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            const int32_t n = key_tiles(it.key0, key1);
-            const int32_t splits = n == 0 && g >= 0 ? 0 : ranges_of(n, range);     // 0: the group's part is all there is
-            const bool parts = splits > 1 || g >= 0 || i >= a.S;
-            const int32_t each = splits > 0 ? n / splits : 0;
-            const int32_t cls = (u.ncols > ATTN_FEW_COLS ? 0 : 256) + 255 - (each < 128 ? each : min(255, 128 + (each - 128) / 16));
-            if (pass == 0) {
-                if (splits > 0) atomicAdd(&bins[cls], splits);
-                continue;
-            }
-            const int32_t at = splits > 0 ? atomicAdd(&bins[cls], splits) : 0;
-            int32_t slot = -1;
-            const int32_t step = u.ncols * a.kv_heads;
-            if (i >= a.S) slot = a.l.group_slot[i - a.S] + tile * ATTN_COLS * a.kv_heads * splits;
-            else if (parts) slot = atomicAdd(&n_slots, splits * step);
-            const bool fits = !parts || (slot >= 0 && (int64_t)slot + (int64_t)splits * step <= a.l.slot_cap);   // not so: the tables are malformed
-            for (int32_t k = 0; k < splits; ++k) {
-                const int32_t first = it.key0 / ATTN_KEYS;
-                const int64_t k0 = first + part_begin(n, splits, k), k1 = first + part_begin(n, splits, k + 1);
-                u.key0 = max(it.key0, (int32_t)(k0 * ATTN_KEYS));
-                u.key1 = max(u.key0, (int32_t)min((int64_t)key1, k1 * ATTN_KEYS));
-                u.slot = parts ? slot + k * step : -1;
-                if (!fits) { u.slot = 0; u.ncols = 0; }
-                if (at + k < a.l.unit_cap) a.l.units[at + k] = u;
-            }
-            if (parts && i < a.S && fits) {
-                AttnMerge j;
-                j.row0 = it.row0; j.col0 = col0; j.ncols = u.ncols; j.parts = splits; j.slot = slot;
-                j.group_parts = group_ranges; j.group_slot = g >= 0 ? a.l.group_slot[g] : 0;
-                j.group_col0 = g >= 0 ? (a.l.rows_before[i] - a.l.rows_before[m.begin]) * G + col0 : 0;
-                j.group_cols = m.rows * G;
-                j.pad[0] = j.pad[1] = j.pad[2] = 0;
-                const int32_t to = atomicAdd(&n_merges, 1);
-                if (to < a.l.merge_cap) a.l.merges[to] = j;
-            }
+            d.u.table = a.kv_len ? i : it.row0;
+        } else {
+            m = attn_group(a, i - a.S);
+            it.row0 = 0; it.rows = m.rows; it.key0 = 0; it.key1 = m.prefix;
+            d.u.table = min(m.begin, a.S - 1);
         }
+        d.begin = m.begin; d.group_cols = m.rows * G;
+        d.col0 = tile * ATTN_COLS;
+        d.rows0 = it.row0;
+        const int32_t first = d.col0 / G;
+        d.u.ncols = min(ATTN_COLS, it.rows * G - d.col0);
+        d.u.head0 = d.col0 - first * G;
+        d.key0 = it.key0; d.key1 = it.key1;
+        if (i < a.S) {
+            d.u.row0 = it.row0 + first;
+            d.u.lim0 = it.lim0 + first;
+            d.key1 = min(d.key1, d.u.lim0 + (d.u.head0 + d.u.ncols - 1) / G);
+        } else {
+            d.u.row0 = -1 - (a.l.group_list[i - a.S] + first);
+            d.u.lim0 = __hip_atomic_load(&a.l.group_low[i - a.S], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        d.n = key_tiles(d.key0, d.key1);
+        d.splits = d.n == 0 && d.g >= 0 ? 0 : ranges_of(d.n, range);      // 0: the group's part is all there is
+        d.parts = d.splits > 1 || d.g >= 0 || i >= a.S;
+        const int32_t each = d.splits > 0 ? (int32_t)((uint32_t)d.n / (uint32_t)d.splits) : 0;
+        d.cls = (d.u.ncols > ATTN_FEW_COLS ? 0 : 256) + 255 - (each < 128 ? each : min(255, 128 + (each - 128) / 16));
+        return d;
+    };
+    Tile d;
+    for (int32_t t = tid; t < n_tiles; t += nt) {
+        d = describe(t);
+        if (d.splits > 0) atomicAdd(&bins[d.cls], d.splits);
+    }
+    __syncthreads();
+    {
+        int32_t total;
+        const int32_t v0 = tid < 256 ? bins[2 * tid] : 0, v1 = tid < 256 ? bins[2 * tid + 1] : 0;
+        const int32_t before = block_exclusive_scan(v0 + v1, lds, &total);
+        if (tid < 256) { bins[2 * tid] = before; bins[2 * tid + 1] = before + v0; }
+        if (tid == 0) n_units = total;
         __syncthreads();
-        if (pass == 0) {
-            int32_t total;
-            const int32_t v0 = tid < 256 ? bins[2 * tid] : 0, v1 = tid < 256 ? bins[2 * tid + 1] : 0;
-            const int32_t before = block_exclusive_scan(v0 + v1, lds, &total);
-            if (tid < 256) { bins[2 * tid] = before; bins[2 * tid + 1] = before + v0; }
-            if (tid == 0) n_units = total;
-            __syncthreads();
+    }
+    for (int32_t t = tid; t < n_tiles; t += nt) {
+        if (n_tiles > nt) d = describe(t);                     // else every thread has its only one still
+        const int32_t at = d.splits > 0 ? atomicAdd(&bins[d.cls], d.splits) : 0, step = d.u.ncols * a.kv_heads;
+        int32_t slot = -1;
+        if (d.i >= a.S) slot = a.l.group_slot[d.i - a.S] + d.col0 * a.kv_heads * d.splits;
+        else if (d.parts) slot = atomicAdd(&n_slots, d.splits * step);
+        const bool fits = !d.parts || (slot >= 0 && (int64_t)slot + (int64_t)d.splits * step <= a.l.slot_cap);   // not so: the tables are malformed
+        const int32_t first = d.key0 / ATTN_KEYS;
+        for (int32_t k = 0; k < d.splits; ++k) {
+            AttnUnit u = d.u;
+            const int64_t k0 = first + part_begin(d.n, d.splits, k), k1 = first + part_begin(d.n, d.splits, k + 1);
+            u.key0 = max(d.key0, (int32_t)(k0 * ATTN_KEYS));
+            u.key1 = max(u.key0, (int32_t)min((int64_t)d.key1, k1 * ATTN_KEYS));
+            u.slot = d.parts ? slot + k * step : -1;
+            if (!fits) { u.slot = 0; u.ncols = 0; }
+            if (at + k < a.l.unit_cap) a.l.units[at + k] = u;
+        }
+        if (d.parts && d.i < a.S && fits) {
+            AttnMerge j;
+            j.row0 = d.rows0; j.col0 = d.col0; j.ncols = d.u.ncols; j.parts = d.splits; j.slot = slot;
+            j.group_parts = d.group_ranges; j.group_slot = d.g >= 0 ? a.l.group_slot[d.g] : 0;
+            j.group_col0 = d.g >= 0 ? (a.l.rows_before[d.i] - a.l.rows_before[d.begin]) * G + d.col0 : 0;
+            j.group_cols = d.group_cols;
+            j.pad[0] = j.pad[1] = j.pad[2] = 0;
+            const int32_t to = atomicAdd(&n_merges, 1);
+            if (to < a.l.merge_cap) a.l.merges[to] = j;
         }
     }
+    __syncthreads();
     if (tid == 0) {
         int32_t *h = a.l.header;
         h[AH_UNITS] = min(n_units, a.l.unit_cap); h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
@@ -338,11 +348,11 @@ struct AttnDirect {
     bool found;
 };
 
-__device__ __forceinline__ int32_t wave_inclusive(int32_t v)
+// inclusive sums over the lanes, of which only the first `n` hold anything (a step of a few requests does not wait for six exchanges)
+__device__ __forceinline__ int32_t wave_inclusive(int32_t v, int32_t n)
 {
     const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
+    for (int off = 1; off < n; off <<= 1) {
         const int32_t up = __shfl_up(v, off, 64);
         if (lane >= off) v += up;
     }
@@ -372,8 +382,8 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
     }
     int32_t range = INT32_MAX;
     if (a.can_split) {
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) cost += __shfl_xor(cost, off, 64);
+        const int32_t n = min(a.S, 64);
+        cost = __builtin_amdgcn_readlane(wave_inclusive(cost, n), n - 1);
         range = max(a.min_tiles, (int32_t)min(((uint64_t)(uint32_t)cost * (uint32_t)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET, (uint64_t)INT32_MAX));
     }
     AttnDirect r = {};
@@ -384,8 +394,9 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
         const int32_t parts = ranges_of(key_tiles(0, it[c].key1), range), units = tiles[c] * parts;
         const int32_t mine = BY_TILE ? tiles[c] : units;
         const int32_t need = parts > 1 ? (int32_t)min((int64_t)it[c].rows * G * parts * a.kv_heads, (int64_t)a.l.slot_cap) : 0;
-        const int32_t upto = wave_inclusive(mine), slot = wave_inclusive(need);
-        const uint64_t past = __ballot(before + upto > index);
+        const int32_t lanes = min(a.S - c * 64, 64);
+        const int32_t upto = wave_inclusive(mine, lanes), slot = a.can_split ? wave_inclusive(need, lanes) : 0;
+        const uint64_t past = __ballot(lane < lanes && before + upto > index);
         if (!r.found && past != 0) {
             const int at = __builtin_ctzll(past);
             auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
@@ -398,11 +409,11 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
             r.part = BY_TILE ? 0 : i - r.tile * r.parts;
             r.slot = slots + of(slot) - of(need);
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
-        slots += __builtin_amdgcn_readlane(slot, 63);
+        before += __builtin_amdgcn_readlane(upto, lanes - 1);
+        slots += __builtin_amdgcn_readlane(slot, lanes - 1);
         if (!BY_TILE && index == 0) {
-            r.tiles += __builtin_amdgcn_readlane(wave_inclusive(tiles[c]), 63);
-            r.joined += __builtin_amdgcn_readlane(wave_inclusive(parts > 1 ? tiles[c] : 0), 63);
+            r.tiles += __builtin_amdgcn_readlane(wave_inclusive(tiles[c], lanes), lanes - 1);
+            r.joined += __builtin_amdgcn_readlane(wave_inclusive(parts > 1 ? tiles[c] : 0, lanes), lanes - 1);
         }
     }
     r.units = before;
