@@ -393,6 +393,49 @@ template <typename E> __device__ __forceinline__ void store4(gptr_t p, float a, 
 }
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // a row that sees no key is zero
 
+// The results of a wavefront's 32 columns, or their part.
+template <typename E, int D>
+__device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit &u, AttnColumns<E, D> &w, int kv_head, int first)
+{
+    using X = AttnTile<E, D>;
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const float l = both_halves_sum(w.l);
+    if (u.slot < 0) {
+        const float f = inverse(l);
+        const gptr_t to = as_global((char *)a.out + (int64_t)w.row * a.ldo + w.head * X::ROW + half * (X::ELEM == 2 ? 16 : 4 * X::ELEM));
+#pragma unroll
+        for (int b = 0; b < X::BLOCKS; ++b) {
+            if constexpr (X::ELEM == 2) {                         // the two lanes of a column trade halves: 16 bytes each, of consecutive dimensions
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    u32x4_t v;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(w.o[b][4 * r + 2 * e] * f, w.o[b][4 * r + 2 * e + 1] * f),
+                                                                        pack_bf16(w.o[b][4 * r + 4 + 2 * e] * f, w.o[b][4 * r + 5 + 2 * e] * f), false, false);
+                        v[e] = x[0];
+                        v[2 + e] = x[1];
+                    }
+                    if (w.valid) st16(to + (b * 32 + 8 * r) * X::ELEM, v);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (w.valid) store4<E>(to + (b * 32 + 8 * r) * X::ELEM, w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f);
+            }
+        }
+    } else if (w.valid) {
+        const int64_t part = (int64_t)u.slot + kv_head * u.ncols + first + (lane & 31);
+        const gptr_t to = as_global((void *)(a.l.part_o + part * D + half * 4));
+#pragma unroll
+        for (int b = 0; b < X::BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                store4<float>(to + (b * 32 + 8 * r) * 4, w.o[b][4 * r], w.o[b][4 * r + 1], w.o[b][4 * r + 2], w.o[b][4 * r + 3]);
+        if (half == 0) a.l.part_ml[part] = make_float2(w.m, l);
+    }
+}
+
 // ---------------------------------------------------------------------------------------
 // A unit of more than 32 columns: every wavefront has 32 of them, and all read the tiles of 64 keys that the workgroup brings to LDS, one
 // tile ahead.
@@ -478,48 +521,16 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
         w.careful(vt, 0, s[0], scratch, key, u.key0);
         w.careful(vt, 32, s[1], scratch, key + 32, u.key0);
     }
-    const float l = both_halves_sum(w.l);
-    if (u.slot < 0) {
-        const float f = inverse(l);
-        const gptr_t to = as_global((char *)a.out + (int64_t)w.row * a.ldo + w.head * X::ROW + half * (X::ELEM == 2 ? 16 : 4 * X::ELEM));
-#pragma unroll
-        for (int b = 0; b < X::BLOCKS; ++b) {
-            if constexpr (X::ELEM == 2) {                         // the two lanes of a column trade halves: 16 bytes each, of consecutive dimensions
-#pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    u32x4_t v;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(w.o[b][4 * r + 2 * e] * f, w.o[b][4 * r + 2 * e + 1] * f),
-                                                                        pack_bf16(w.o[b][4 * r + 4 + 2 * e] * f, w.o[b][4 * r + 5 + 2 * e] * f), false, false);
-                        v[e] = x[0];
-                        v[2 + e] = x[1];
-                    }
-                    if (w.valid) st16(to + (b * 32 + 8 * r) * X::ELEM, v);
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (w.valid) store4<E>(to + (b * 32 + 8 * r) * X::ELEM, w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f);
-            }
-        }
-    } else if (w.valid) {
-        const int64_t part = (int64_t)u.slot + kv_head * u.ncols + wave * 32 + (lane & 31);
-        const gptr_t to = as_global((void *)(a.l.part_o + part * D + half * 4));
-#pragma unroll
-        for (int b = 0; b < X::BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                store4<float>(to + (b * 32 + 8 * r) * 4, w.o[b][4 * r], w.o[b][4 * r + 1], w.o[b][4 * r + 2], w.o[b][4 * r + 3]);
-        if (half == 0) a.l.part_ml[part] = make_float2(w.m, l);
-    }
+    write_columns<E, D>(a, u, w, kv_head, wave * 32);
 }
 
 // ---------------------------------------------------------------------------------------
 // A unit of up to 32 columns: bound by the bytes of its keys.  The four wavefronts take blocks of 32 keys in turn, each through LDS of its own without a
 // barrier -- K of the next block is asked for as soon as this one's is in registers, V likewise -- and join their sums at the end.
+// SOLO: the unit is one wavefront's.  Where short units are many this costs the look-ups before the first block once in 12 blocks instead of once in 3, and no join
+// (SOLO_FIGURES).
 // ---------------------------------------------------------------------------------------
-template <typename E, int D, bool PAGED>
+template <typename E, int D, bool PAGED, bool SOLO>
 __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)
 {
     using X = AttnTile<E, D>;
@@ -530,10 +541,12 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     src.init(a, u, kv_head);
     const lds_t kt = lds + wave * 2 * HALF, vt = kt + HALF;
     const uint32_t ka = lds_address(kt), va = ka + HALF;
-    // Blocks wave, wave + 4, ... of 32 keys; the first one last if it begins before key0.
-    const int32_t base = u.key0 / 32 * 32, blocks = u.key1 > u.key0 ? (u.key1 - 1 - base) / 32 + 1 : 0, n = (blocks - wave + 3) / 4;
-    const int32_t skip = wave == 0 && u.key0 > base ? 1 : 0;
-    auto key_of = [&](int32_t i) { return base + (wave + 4 * (i + skip < n ? i + skip : i + skip - n)) * 32; };
+    // Blocks first, first + STEP, ... of 32 keys; the first one last if it begins before key0.
+    constexpr int STEP = SOLO ? 1 : 4;
+    const int first = SOLO ? 0 : wave;
+    const int32_t base = u.key0 / 32 * 32, blocks = u.key1 > u.key0 ? (u.key1 - 1 - base) / 32 + 1 : 0, n = (blocks - first + STEP - 1) / STEP;
+    const int32_t skip = first == 0 && u.key0 > base ? 1 : 0;
+    auto key_of = [&](int32_t i) { return base + (first + STEP * (i + skip < n ? i + skip : i + skip - n)) * 32; };
     AttnColumns<E, D> w;
     w.init(a, u, kv_head, 0);                                     // the queries are on their way while the first page is looked up
     if (n > 0) {
@@ -542,8 +555,8 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     }
     const float c = a.scale_log2;
     w.arrived();
-    const int32_t low = min(u.lim0, u.key1), before = (low - base) / 32 - wave;            // blocks from this wavefront's first on that all columns see whole
-    const int32_t full = min(n, max(0, (before + 3) / 4 - skip));
+    const int32_t low = min(u.lim0, u.key1), before = (low - base) / 32 - first;           // blocks from this wavefront's first on that all columns see whole
+    const int32_t full = min(n, max(0, (before + STEP - 1) / STEP - skip));
     int32_t i = 0;
     for (; i < full; ++i) {
         const bool more = i + 1 < n;
@@ -592,6 +605,10 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
             src.template copy<false, COPIES>(ka, key_of(i + 1), 0);
             src.template copy<true, COPIES>(va, key_of(i + 1), 0);
         }
+    }
+    if constexpr (SOLO) {
+        write_columns<E, D>(a, u, w, kv_head, 0);
+        return;
     }
     // join: every wavefront's sums at the largest m of all
     const float l = both_halves_sum(w.l);
@@ -668,13 +685,21 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
         if (!d.found) return;
         u = attn_unit_of(a.s, d);
     } else {
-        if (!attn_schedule_is(a, KIND) || unit >= as_const(a.l.header)[AH_UNITS]) return;
-        const PREFT_CONST AttnUnit *p = as_const(a.l.units) + unit;
+        if (!attn_schedule_is(a, KIND)) return;
+        // short units: one a wavefront, four a workgroup
+        const int32_t units = as_const(a.l.header)[AH_UNITS], alone = as_const(a.l.header)[AH_SHORT];
+        const int32_t i = unit < alone ? unit : alone + 4 * (unit - alone) + uniform(threadIdx.x >> 6);
+        if (i >= units) return;
+        const PREFT_CONST AttnUnit *p = as_const(a.l.units) + i;
         u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
+        if (unit >= alone) {
+            if (u.ncols > 0) attend_keys<E, D, PAGED, true>(a, u, kv_head, (lds_t)lds, join);
+            return;
+        }
     }
     if (u.ncols <= 0) return;
     if (u.ncols > ATTN_FEW_COLS) attend_columns<E, D, PAGED>(a, u, kv_head, (lds_t)lds, (int32_t *)join);
-    else attend_keys<E, D, PAGED>(a, u, kv_head, (lds_t)lds, join);
+    else attend_keys<E, D, PAGED, false>(a, u, kv_head, (lds_t)lds, join);
 }
 
 // Joins the parts of a column: M = max m_j, out = sum 2^(m_j - M) o_j / sum 2^(m_j - M) l_j, in the order of the parts.  One wavefront a column.

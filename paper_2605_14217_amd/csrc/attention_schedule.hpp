@@ -16,6 +16,7 @@ constexpr int ATTN_KEYS      = 64;    // keys of a tile
 constexpr int ATTN_TARGET    = 512;   // workgroups that run side by side: two on each of 256 compute units
 constexpr int ATTN_GROUP_ROWS = 4096; // rows of groups that are listed; the rest see their prefix by themselves
 constexpr int ATTN_MIN_PREFIX = 64;   // shorter prefixes are not worth a part of their own
+constexpr int ATTN_SHORT     = 12;    // key tiles: up to here a unit of few columns is one wavefront's, where there are many of them
 constexpr int ATTN_SCAN      = 4096;  // items whose tile offsets are kept in LDS
 constexpr int ATTN_DIRECT    = 256;   // segments of a call whose workgroups find their unit by themselves, four a lane
 
@@ -51,7 +52,7 @@ struct AttnLists {
     int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
 };
 
-constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9;
+constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9, AH_SHORT = 10;
 
 struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     __shared__ int32_t lds[32];
     __shared__ int32_t first_tile[ATTN_SCAN + 1];
     __shared__ int32_t bins[512];
-    __shared__ int32_t n_units, n_merges, n_slots;
+    __shared__ int32_t n_units, n_long,  n_merges, n_slots;
     __shared__ unsigned long long cost_sum;
     const int tid = threadIdx.x, nt = blockDim.x;
     const int32_t G = a.group, items = a.S + a.n_groups;
@@ -297,6 +298,8 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         const int32_t before = block_exclusive_scan(v0 + v1, lds, &total);
         if (tid < 256) { bins[2 * tid] = before; bins[2 * tid + 1] = before + v0; }
         if (tid == 0) n_units = total;
+        constexpr int first_short = 256 + 255 - ATTN_SHORT;
+        if (tid == first_short / 2) n_long = before + (first_short % 2 ? v0 : 0);
         __syncthreads();
     }
     for (int32_t t = tid; t < n_tiles; t += nt) {
@@ -330,7 +333,10 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     __syncthreads();
     if (tid == 0) {
         int32_t *h = a.l.header;
-        h[AH_UNITS] = min(n_units, a.l.unit_cap); h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
+        const int32_t units = min(n_units, a.l.unit_cap);
+        // enough of them that a wavefront each fills the chip: 2048 wavefronts run side by side
+        h[AH_SHORT] = (units - n_long) * a.kv_heads >= 2 * ATTN_TARGET ? min(n_long, units) : units;
+        h[AH_UNITS] = units; h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
         h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
     }
 }

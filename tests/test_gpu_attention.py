@@ -286,6 +286,25 @@ def test_many_rows_share_a_long_prefix(dtype, H, Hkv, D):
     print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
 
 
+@pytest.mark.parametrize("dtype,H,Hkv,D", [("bf16", 8, 4, 128), ("bf16", 4, 2, 64), ("f32", 2, 2, 64)])
+def test_many_short_requests(dtype, H, Hkv, D):
+    """Units enough that each is one wavefront's: decode rows, some of several, with and without groups; and short prompts."""
+    print(f"\n[case] many short requests {dtype} {H}/{Hkv}x{D}", flush=True)
+    rng = np.random.Generator(np.random.PCG64(8))
+    S = 1100 // Hkv + 40
+    kv = rng.integers(0, 150, size=S)
+    kv[::7] = rng.integers(300, 900, size=len(kv[::7]))
+    out, before, want, *_ = cached_case(dtype, H, Hkv, D, 16, rng.integers(0, 3, size=S), kv)
+    print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+    cut = [0, S // 3, S - 60]
+    out, before, want, *_ = cached_case(dtype, H, Hkv, D, 16, np.ones(S, int), 100 + kv, groups=[(cut[0], cut[1]), (cut[1], cut[2])], prefix=[96, 100])
+    print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+    n = rng.integers(0, 16, size=S)
+    n[5] = 90
+    out, before, _, _, want = prompt_case(dtype, H, Hkv, D, n, n)
+    print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+
+
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
 @pytest.mark.parametrize("dtype,H,Hkv,D", HEADS[:4])
 def test_tokens_that_only_later_rows_see(dtype, H, Hkv, D, bad):
