@@ -120,9 +120,9 @@ __device__ __forceinline__ int32_t last_at_or_before(P first, int32_t n, int32_t
 }
 
 // One workgroup: the lists are a few kilobytes, and what a step waits for is the chain of reads and barriers, not the work.
-// Wide units (more than 32 columns) come first, and units of a kind stand in the order of falling cost (counting sort over 256 cost classes): the longest
-// of a causal prompt begin first and the short ones fill the ends.  (Wide units, bound by the matrix cores, and narrow ones, bound by memory, in turns, so
-// that a compute unit has one of each: 229 us against 187 on 256 rows of 64 heads with prefixes of 8192 -- the wide ones then end late.)  Their order does not change a result: every unit has an output or part of its own.
+// Units stand in the order of falling time (counting sort over 256 classes): the longest of a causal prompt begin first and the short ones fill the ends.
+// (Wide units, bound by the matrix cores, and narrow ones, bound by memory, in turns, so that a compute unit has one of each: 229 us against 187 on 256 rows of
+// 64 heads with prefixes of 8192 -- the wide ones then end late.)  Their order does not change a result: every unit has an output or part of its own.
 __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnScheduleArgs a)
 {
     __shared__ int32_t lds[32];
@@ -215,6 +215,8 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     __syncthreads();
     const int32_t n_tiles = min(carry, a.l.tile_cap);
     // a range of keys: no shorter than the whole work over the workgroups that run side by side
+    // (Wide and narrow tiles each for themselves: 206 us against 173 on 256 rows of 64 heads with prefixes of 8192.  All workgroups are wide ones then at first, and memory
+    // waits for the narrow ones.)
     int32_t range = INT32_MAX;
     if (a.can_split) {
         const unsigned long long even = (cost_sum * (unsigned)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET;
@@ -283,7 +285,10 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         d.splits = d.n == 0 && d.g >= 0 ? 0 : ranges_of(d.n, range);      // 0: the group's part is all there is
         d.parts = d.splits > 1 || d.g >= 0 || i >= a.S;
         const int32_t each = d.splits > 0 ? (int32_t)((uint32_t)d.n / (uint32_t)d.splits) : 0;
-        d.cls = (d.u.ncols > ATTN_FEW_COLS ? 0 : 256) + 255 - (each < 128 ? each : min(255, 128 + (each - 128) / 16));
+        // by time: 64 keys of a wide unit take 2.5 times those of a narrow one; short units stand at the end
+        const bool narrow = d.u.ncols <= ATTN_FEW_COLS, brief = narrow && each <= ATTN_SHORT;
+        const int32_t time = narrow && !brief ? each * 2 / 5 : each;
+        d.cls = (brief ? 256 : 0) + 255 - (time < 128 ? time : min(255, 128 + (time - 128) / 16));
         return d;
     };
     Tile d;
@@ -298,8 +303,7 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         const int32_t before = block_exclusive_scan(v0 + v1, lds, &total);
         if (tid < 256) { bins[2 * tid] = before; bins[2 * tid + 1] = before + v0; }
         if (tid == 0) n_units = total;
-        constexpr int first_short = 256 + 255 - ATTN_SHORT;
-        if (tid == first_short / 2) n_long = before + (first_short % 2 ? v0 : 0);
+        if (tid == 128) n_long = before;
         __syncthreads();
     }
     for (int32_t t = tid; t < n_tiles; t += nt) {
