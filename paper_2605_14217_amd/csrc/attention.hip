@@ -96,9 +96,9 @@ int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
 {
     hipLaunchKernelGGL((attention_kernel<E, D, PAGED, DIRECT>), dim3((unsigned)(p.units * a.kv_heads)), dim3(256), 0, st, a);
     if (p.split) {
-        const unsigned tiles = (unsigned)(DIRECT ? p.tiles : a.l.merge_cap < 1024 ? a.l.merge_cap : 1024);
-        const unsigned z = tiles * (unsigned)a.kv_heads < 512 && (int64_t)a.T * a.group > 4 ? 8u : 1u;
-        hipLaunchKernelGGL((attention_merge_kernel<E, D, DIRECT>), dim3(tiles, (unsigned)a.kv_heads, z), dim3(256), 0, st, a, PAGED ? 2 : 1);
+        const unsigned tiles = (unsigned)(a.l.merge_cap < 1024 ? a.l.merge_cap : 1024);
+        const unsigned z = tiles * (unsigned)a.kv_heads < 256 && (int64_t)a.T * a.group > 4 ? 16u : 1u;      // workgroups that share a tile's columns
+        hipLaunchKernelGGL((attention_merge_kernel<E, D>), dim3(tiles, (unsigned)a.kv_heads, z), dim3(256), 0, st, a, PAGED ? 2 : 1);
     }
     return launched();
 }

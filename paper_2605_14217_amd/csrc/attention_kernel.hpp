@@ -676,14 +676,22 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
     AttnUnit u;
     if constexpr (DIRECT) {
         if (a.ready && !attn_schedule_is(a, KIND)) return;
-        const AttnDirect d = attn_direct<false>(a.s, unit);
+        const AttnDirect d = attn_direct(a.s, unit);
         if (!a.ready && blockIdx.x == 0 && threadIdx.x == 0) {
             int32_t *h = a.l.header;
-            h[AH_UNITS] = d.units; h[AH_MERGES] = d.joined; h[AH_TILES] = d.tiles; h[AH_KIND] = KIND;
+            h[AH_UNITS] = d.units; h[AH_MERGES] = d.joined; h[AH_TILES] = d.tiles; h[AH_JOINS] = min(d.tiles, a.l.merge_cap); h[AH_KIND] = KIND;
             h[AH_GROUPS] = 0; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
         }
         if (!d.found) return;
         u = attn_unit_of(a.s, d);
+        if (a.s.can_split && d.part == 0 && kv_head == 0 && threadIdx.x == 0) {
+            const int32_t tile = (d.it.rows * a.group + ATTN_COLS - 1) / ATTN_COLS - 1 - d.tile, to = d.tiles_before + tile;
+            AttnMerge j = {};
+            j.row0 = d.it.row0; j.col0 = tile * ATTN_COLS; j.ncols = u.ncols; j.group_cols = ATTN_COLS;
+            j.parts = d.parts > 1 ? d.parts : 0;
+            j.slot = d.slot + j.col0 * d.parts * a.kv_heads;
+            if (to < a.l.merge_cap) a.l.merges[to] = j;
+        }
     } else {
         if (!attn_schedule_is(a, KIND)) return;
         // short units: one a wavefront, four a workgroup
@@ -713,25 +721,27 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
         const int32_t width = min(ATTN_COLS, j.group_cols - tile * ATTN_COLS);
         const int64_t group = (int64_t)j.group_slot + (int64_t)tile * ATTN_COLS * a.kv_heads * j.group_parts + kv_head * width + gc % ATTN_COLS;
         const int64_t mine = (int64_t)j.slot + kv_head * j.ncols + c;
-        const int32_t parts = j.parts + j.group_parts;
+        const int32_t parts = j.parts + j.group_parts;           // at least one: see where the entries are made
         auto part = [&](int32_t k) {                               // slots are below 2^31: checked where the workspace is laid out
             const int64_t p = k < j.parts ? mine + (int64_t)k * j.ncols * a.kv_heads : group + (int64_t)(k - j.parts) * width * a.kv_heads;
             return p < 0 || p >= a.l.slot_cap ? 0 : (int32_t)p;
         };
-        // a lane has the place and the factor of a part, 64 parts at a time; their rows are then read eight at a time, with nothing to wait for in between
-        float top = ATTN_LOWEST;
-        for (int32_t k = lane; k < parts; k += 64) top = fmaxf(top, a.l.part_ml[part(k)].x);
+        // A lane has the place and the factor of a part, 64 parts at a time; their rows are then read eight at a time, with nothing to wait for in between.
+        int32_t at = part(min(lane, parts - 1));
+        float2 ml = a.l.part_ml[at];
+        float top = ml.x;
+        for (int32_t k = lane + 64; k < parts; k += 64) top = fmaxf(top, a.l.part_ml[part(k)].x);
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
         float o[D / 64] = {}, l = 0.0f;
         for (int32_t k0 = 0; k0 < parts; k0 += 64) {
-            const int32_t n = min(64, parts - k0), at = part(min(k0 + lane, parts - 1));
-            const float2 ml = a.l.part_ml[at];
+            const int32_t n = min(64, parts - k0);
+            if (k0 > 0) {
+                at = part(min(k0 + lane, parts - 1));
+                ml = a.l.part_ml[at];
+            }
             const float f = __builtin_amdgcn_exp2f(ml.x - top);
             float sum = lane < n ? ml.y * f : 0.0f;
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-            l += sum;
             for (int32_t k = 0; k < n; k += 8) {
                 float x[8][D / 64] = {};
 #pragma unroll
@@ -748,6 +758,9 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
                     for (int d = 0; d < D / 64; ++d) o[d] += x[e][d] * w;
                 }
             }
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+            l += sum;
         }
         const float inv = inverse(l);
         const int32_t q = (j.col0 + c) / G, head = kv_head * G + (j.col0 + c - q * G), row = max(0, min(j.row0 + q, a.T - 1));
@@ -757,22 +770,14 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
     }
 }
 
-template <typename E, int D, bool DIRECT>
+template <typename E, int D>
 __global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, int kind)
 {
-    if constexpr (DIRECT) {
-        if (a.ready && !attn_schedule_is(a, kind)) return;
-        const AttnDirect d = attn_direct<true>(a.s, (int32_t)blockIdx.x);
-        if (!d.found || d.parts <= 1) return;
-        AttnMerge j = {};
-        j.row0 = d.it.row0; j.col0 = d.tile * ATTN_COLS; j.ncols = min(ATTN_COLS, d.it.rows * a.group - j.col0);
-        j.parts = d.parts; j.slot = d.slot + j.col0 * d.parts * a.kv_heads;
-        j.group_cols = ATTN_COLS;
-        join_tile<E, D>(a, j, (int)blockIdx.y);
-    } else {
-        if (!attn_schedule_is(a, kind)) return;
-        const int32_t n = as_const(a.l.header)[AH_MERGES];
-        for (int32_t i = blockIdx.x; i < n; i += gridDim.x) join_tile<E, D>(a, a.l.merges[i], (int)blockIdx.y);
+    if (!attn_schedule_is(a, kind)) return;
+    const int32_t n = as_const(a.l.header)[AH_JOINS];
+    for (int32_t i = blockIdx.x; i < n; i += gridDim.x) {
+        const AttnMerge j = a.l.merges[i];
+        if (j.parts + j.group_parts > 0) join_tile<E, D>(a, j, (int)blockIdx.y);
     }
 }
 

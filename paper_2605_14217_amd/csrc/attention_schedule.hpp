@@ -52,7 +52,7 @@ struct AttnLists {
     int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
 };
 
-constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9, AH_SHORT = 10;
+constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11;      // AH_JOINS: entries of merges
 
 struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
@@ -340,19 +340,20 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         const int32_t units = min(n_units, a.l.unit_cap);
         // enough of them that a wavefront each fills the chip: 2048 wavefronts run side by side
         h[AH_SHORT] = (units - n_long) * a.kv_heads >= 2 * ATTN_TARGET ? min(n_long, units) : units;
-        h[AH_UNITS] = units; h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
+        h[AH_UNITS] = units; h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_JOINS] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
         h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
     }
 }
 
 // ---------------------------------------------------------------------------------------
-// Without a schedule kernel: a wavefront finds the unit (or the tile to join) of its workgroup from the tables by itself, in a microsecond where the
-// kernel would take six.  For calls of few segments and workgroups, without groups.  All tiles of a segment are cut into as many ranges, so that the sums over the
+// Without a schedule kernel: a wavefront finds the unit of its workgroup from the tables by itself, in a microsecond where the
+// kernel would take six, and the first unit of a tile leaves the entry of its merge.  For calls of few segments and workgroups, without groups.  All tiles of a segment are cut into as many ranges, so that the sums over the
 // segments before are all it takes.
 // ---------------------------------------------------------------------------------------
 struct AttnDirect {
     AttnItem it;
     int32_t s, tile, part, parts;      // parts 1: the unit writes the result
+    int32_t tiles_before;              // of the segments before
     int32_t slot;                      // first part column of the segment
     int32_t units, tiles, joined;      // of the call, for index 0
     bool found;
@@ -369,8 +370,7 @@ __device__ __forceinline__ int32_t wave_inclusive(int32_t v, int32_t n)
     return v;
 }
 
-// the unit `index` of the call, or with BY_TILE its tile `index`
-template <bool BY_TILE>
+// the unit `index` of the call
 __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int32_t index)
 {
     constexpr int EACH = ATTN_DIRECT / 64;
@@ -397,36 +397,38 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
         range = max(a.min_tiles, (int32_t)min(((uint64_t)(uint32_t)cost * (uint32_t)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET, (uint64_t)INT32_MAX));
     }
     AttnDirect r = {};
-    int32_t before = 0, slots = 0;
+    int32_t before = 0, slots = 0, tiles_before = 0;
 #pragma unroll
     for (int c = 0; c < EACH; ++c) {
         if (c * 64 >= a.S) continue;
         const int32_t parts = ranges_of(key_tiles(0, it[c].key1), range), units = tiles[c] * parts;
-        const int32_t mine = BY_TILE ? tiles[c] : units;
         const int32_t need = parts > 1 ? (int32_t)min((int64_t)it[c].rows * G * parts * a.kv_heads, (int64_t)a.l.slot_cap) : 0;
         const int32_t lanes = min(a.S - c * 64, 64);
-        const int32_t upto = wave_inclusive(mine, lanes), slot = a.can_split ? wave_inclusive(need, lanes) : 0;
+        const int32_t upto = wave_inclusive(units, lanes), slot = a.can_split ? wave_inclusive(need, lanes) : 0;
+        const int32_t tile = a.can_split ? wave_inclusive(tiles[c], lanes) : upto;
         const uint64_t past = __ballot(lane < lanes && before + upto > index);
         if (!r.found && past != 0) {
             const int at = __builtin_ctzll(past);
             auto of = [&](int32_t v) { return __builtin_amdgcn_readlane(v, at); };
-            const int32_t i = index - before - (of(upto) - of(mine));
+            const int32_t i = index - before - (of(upto) - of(units));
             r.found = true;
             r.s = c * 64 + at;
             r.it.row0 = of(it[c].row0); r.it.rows = of(it[c].rows); r.it.lim0 = of(it[c].lim0); r.it.key0 = 0; r.it.key1 = of(it[c].key1);
             r.parts = of(parts);
-            r.tile = BY_TILE || r.parts == 1 ? i : (int32_t)((uint32_t)i / (uint32_t)r.parts);
-            r.part = BY_TILE ? 0 : i - r.tile * r.parts;
+            r.tile = r.parts == 1 ? i : (int32_t)((uint32_t)i / (uint32_t)r.parts);
+            r.part = i - r.tile * r.parts;
+            r.tiles_before = tiles_before + of(tile) - of(tiles[c]);
             r.slot = slots + of(slot) - of(need);
         }
         before += __builtin_amdgcn_readlane(upto, lanes - 1);
         slots += __builtin_amdgcn_readlane(slot, lanes - 1);
-        if (!BY_TILE && index == 0) {
-            r.tiles += __builtin_amdgcn_readlane(wave_inclusive(tiles[c], lanes), lanes - 1);
+        tiles_before += __builtin_amdgcn_readlane(tile, lanes - 1);
+        if (index == 0) {
             r.joined += __builtin_amdgcn_readlane(wave_inclusive(parts > 1 ? tiles[c] : 0, lanes), lanes - 1);
         }
     }
     r.units = before;
+    r.tiles = tiles_before;
     return r;
 }
 
