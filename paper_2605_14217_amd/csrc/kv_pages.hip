@@ -17,7 +17,8 @@ struct PlanArgs {
     int32_t  max_pages, S, T, n_free, page_shift;
 };
 
-constexpr int PLAN_THREADS = 1024;
+// 1024 rows a workgroup of 512: of workgroups of 1024 threads a compute unit holds one, and 356 000 rows took two rounds (12.0 us).
+constexpr int PLAN_THREADS = 512, PLAN_ROWS = 2;
 
 struct PlanRequest { int32_t lo, hi, ctx, need, over; };     // rows, tokens before them, pages to begin within and beyond the table
 
@@ -34,92 +35,105 @@ __device__ __forceinline__ PlanRequest plan_request(const PlanArgs &a, int32_t s
     return r;
 }
 
+// sum over the workgroup, for every thread; `lds`: one place a wavefront
+__device__ __forceinline__ int32_t block_sum(int32_t v, int32_t *lds)
+{
+    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if (lane == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lane < waves ? lds[lane] : 0;
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return __shfl(v, 0, 64);
+}
+
 // have = ceil(ctx / page), want = ceil((ctx + n) / page), both cut at max_pages; page k of a request, have <= k < want, is
-// free_pages[off + k - have] with off = sum of want - have over the requests before it.  Latency is what bounds it: a handful of
-// bytes per request, and a chain of reads.  Every workgroup therefore sums the requests before its rows by itself (eight bytes each, from the cache, all
-// reads in flight at once) instead of waiting for another launch to do it, keeps the requests that own its rows in LDS, and writes its rows; the
-// last one sums all requests and writes kv_len and the counts.
+// free_pages[off + k - have] with off = sum of want - have over the requests before it.  (A new page has a row at its start: all sums are at most T.)
+// Latency is what bounds it: a handful of bytes per request, and a chain of reads.  Every workgroup therefore sums the requests before its rows by itself (twelve
+// bytes each, from the cache, all reads in flight at once) instead of waiting for another launch to do it, keeps the requests that own its rows in LDS, and
+// writes its rows; the last one sums all requests and writes kv_len and the counts.  32 requests, one row each: PLAN_SMALL us; 4096 requests and 356 000 rows:
+// PLAN_LARGE us, where the 4.5 MB that it moves would take 1.
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a)
 {
-    __shared__ int32_t lds[32];
-    __shared__ int64_t sums[3][PLAN_THREADS / 64];
-    __shared__ int32_t own_start[PLAN_THREADS], own_end[PLAN_THREADS], own_ctx[PLAN_THREADS], own_off[PLAN_THREADS], own_seg[PLAN_THREADS];
-    const int32_t page = 1 << a.page_shift, n_threads = (int32_t)blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t row0 = (int32_t)blockIdx.x * n_threads, row1 = min(a.T, row0 + n_threads);
+    __shared__ int32_t lds[32], sums[4][PLAN_THREADS / 64];
+    __shared__ int32_t own_start[PLAN_THREADS], own_end[PLAN_THREADS], own_ctx[PLAN_THREADS], own_off[PLAN_THREADS];
+    const int32_t page = 1 << a.page_shift, n_threads = (int32_t)blockDim.x;
+    const int32_t row0 = (int32_t)blockIdx.x * n_threads * PLAN_ROWS, row1 = min(a.T, row0 + n_threads * PLAN_ROWS);
     const bool last = blockIdx.x + 1 == gridDim.x;
     // requests that end before this workgroup's rows: their pages, and how many they are; all requests: their pages, and those that do not fit the table
-    int64_t before = 0, all = 0, over = 0;
-    int32_t first = 0;
+    int32_t off = 0, first = 0, all = 0, over = 0;
 #pragma unroll 4
     for (int32_t s = (int32_t)threadIdx.x; s < a.S; s += n_threads) {
         const PlanRequest r = plan_request(a, s);
-        if (r.hi <= row0) { before += r.need; ++first; }
+        if (r.hi <= row0) { off += r.need; ++first; }
         all += r.need;
         over += r.over;
         if (last) a.kv_len[s] = r.ctx + (r.hi - r.lo);
     }
+    if (row0 > 0) {                                    // else there are none before, but empty ones
+        off = block_sum(off, sums[0]);
+        first = block_sum(first, sums[1]);
+    } else {
+        off = 0;
+        first = 0;
+    }
+    if (last) {
+        all = block_sum(all, sums[2]);
+        over = block_sum(over, sums[3]);
+        if (threadIdx.x == 0) {
+            const int32_t taken = min(a.n_free, all);
+            a.counts[0] = taken;
+            a.counts[1] = all - taken + over;
+        }
+    }
+    int64_t slot[PLAN_ROWS];
+    int32_t at[PLAN_ROWS];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        before += __shfl_xor(before, off, 64);
-        first += __shfl_xor(first, off, 64);
-        if (last) { all += __shfl_xor(all, off, 64); over += __shfl_xor(over, off, 64); }
-    }
-    if (lane == 0) { lds[wave] = first; sums[0][wave] = before; sums[1][wave] = all; sums[2][wave] = over; }
-    __syncthreads();
-    before = all = over = 0;
-    first = 0;
-    for (int w = 0; w < n_threads / 64; ++w) { first += lds[w]; before += sums[0][w]; all += sums[1][w]; over += sums[2][w]; }
-    if (last && threadIdx.x == 0) {
-        const int64_t taken = min((int64_t)a.n_free, all);
-        a.counts[0] = (int32_t)taken;
-        a.counts[1] = (int32_t)min((int64_t)INT32_MAX, all - taken + over);
-    }
-    int64_t off = before;
-    int32_t owned = 0;
-    for (int32_t s0 = first; s0 < a.S; s0 += n_threads) {
+    for (int i = 0; i < PLAN_ROWS; ++i) { slot[i] = -1; at[i] = 0; }
+    for (int32_t s0 = first; s0 < a.S; s0 += n_threads) {          // more than once only where hundreds of requests without rows stand together
         const int32_t s = s0 + (int32_t)threadIdx.x;
         PlanRequest r = {};
+        r.lo = INT32_MAX;
         if (s < a.S) r = plan_request(a, s);
-        int32_t total, mine;
-        const int32_t here = block_exclusive_scan(r.need, lds, &total);
-        const bool owns = r.hi > r.lo && r.lo < row1 && r.hi > row0;
-        const int32_t at = owned + block_exclusive_scan(owns ? 1 : 0, lds, &mine);
-        if (owns && at < n_threads) {                  // well-formed segments do not share rows: at most one for every row
-            own_start[at] = r.lo; own_end[at] = r.hi; own_ctx[at] = r.ctx; own_seg[at] = s;
-            own_off[at] = (int32_t)min((int64_t)INT32_MAX, off + here);
-        }
-        owned = min(n_threads, owned + mine);
+        int32_t total;
+        const int32_t here = block_exclusive_scan(r.need, lds, &total);        // its barriers also end the reads of the turn before
+        own_start[threadIdx.x] = r.lo; own_end[threadIdx.x] = r.hi; own_ctx[threadIdx.x] = r.ctx; own_off[threadIdx.x] = off + here;
         off += total;
-        if (a.seg_start[min(s0 + n_threads, a.S)] >= row1) break;
-    }
-    __syncthreads();
-    const int32_t row = row0 + (int32_t)threadIdx.x;
-    if (row >= row1) return;
-    int32_t lo = 0, hi = owned;                        // the last request that starts at or before the row
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (own_start[mid] <= row) lo = mid; else hi = mid;
-    }
-    int64_t slot = -1;
-    int32_t at = 0;
-    if (owned > 0 && own_start[lo] <= row && row < own_end[lo]) {
-        at = own_ctx[lo] + (row - own_start[lo]);
-        const int32_t k = at >> a.page_shift, have = (int32_t)(((int64_t)own_ctx[lo] + page - 1) >> a.page_shift);
-        if (k < a.max_pages) {
-            int32_t *entry = a.table + (int64_t)own_seg[lo] * a.ld_table + k;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PLAN_ROWS; ++i) {
+            const int32_t row = row0 + i * n_threads + (int32_t)threadIdx.x;
+            int32_t lo = 0, hi = n_threads;                        // the last request that starts at or before the row: an empty one never is
+            while (hi - lo > 1) {
+                const int32_t mid = (lo + hi) >> 1;
+                if (own_start[mid] <= row) lo = mid; else hi = mid;
+            }
+            if (row >= row1 || own_start[lo] > row || row >= own_end[lo]) continue;
+            at[i] = own_ctx[lo] + (row - own_start[lo]);
+            const int32_t k = at[i] >> a.page_shift, have = (int32_t)(((int64_t)own_ctx[lo] + page - 1) >> a.page_shift);
+            if (k >= a.max_pages) continue;
+            int32_t *entry = a.table + (int64_t)(s0 + lo) * a.ld_table + k;
             int32_t p;
             if (k < have) {
                 p = *entry;
             } else {
                 const int64_t pick = (int64_t)own_off[lo] + (k - have);
                 p = pick < a.n_free ? a.free_pages[pick] : -1;
-                if ((at & (page - 1)) == 0) *entry = p;      // a new page has exactly one row at its start
+                if ((at[i] & (page - 1)) == 0) *entry = p;         // a new page has exactly one row at its start
             }
-            if (p >= 0) slot = ((int64_t)p << a.page_shift) + (at & (page - 1));
+            if (p >= 0) slot[i] = ((int64_t)p << a.page_shift) + (at[i] & (page - 1));
         }
+        if (a.seg_start[min(s0 + n_threads, a.S)] >= row1) break;
     }
-    a.slot_map[row] = slot;
-    a.positions[row] = at;
+#pragma unroll
+    for (int i = 0; i < PLAN_ROWS; ++i) {
+        const int32_t row = row0 + i * n_threads + (int32_t)threadIdx.x;
+        if (row >= row1) continue;
+        a.slot_map[row] = slot[i];
+        a.positions[row] = at[i];
+    }
 }
 
 struct StoreArgs {
@@ -187,9 +201,10 @@ int preft_kv_plan(int64_t *slot_map, int32_t *positions, int32_t *kv_len, int32_
     a.slot_map = slot_map; a.positions = positions; a.kv_len = kv_len; a.table = block_table; a.counts = counts;
     a.seg_start = seg_start; a.ctx_len = ctx_len; a.free_pages = free_pages;
     a.ld_table = ld_table; a.max_pages = max_pages; a.S = S; a.T = T; a.n_free = n_free; a.page_shift = shift;
-    const int32_t most = S > T ? S : T;                // a step of a few dozen rows: one small workgroup, fewer wavefronts at every barrier
+    const int32_t most = S > T ? S : T;                // a step of a few dozen rows: one small workgroup, no wavefronts to wait for at its barriers
     const int threads = most >= PLAN_THREADS ? PLAN_THREADS : (most + 63) / 64 * 64;
-    const unsigned grid = T > 0 ? (unsigned)((T + threads - 1) / threads) : 1u;
+    const int64_t rows = (int64_t)threads * PLAN_ROWS;
+    const unsigned grid = T > 0 ? (unsigned)((T + rows - 1) / rows) : 1u;
     hipLaunchKernelGGL(kv_plan_kernel, dim3(grid), dim3(threads), 0, reinterpret_cast<hipStream_t>(stream), a);
     return launched();
 }
