@@ -53,8 +53,8 @@ __device__ __forceinline__ int32_t block_sum(int32_t v, int32_t *lds)
 // free_pages[off + k - have] with off = sum of want - have over the requests before it.  (A new page has a row at its start: all sums are at most T.)
 // Latency is what bounds it: a handful of bytes per request, and a chain of reads.  Every workgroup therefore sums the requests before its rows by itself (twelve
 // bytes each, from the cache, all reads in flight at once) instead of waiting for another launch to do it, keeps the requests that own its rows in LDS, and
-// writes its rows; the last one sums all requests and writes kv_len and the counts.  32 requests, one row each: PLAN_SMALL us; 4096 requests and 356 000 rows:
-// PLAN_LARGE us, where the 4.5 MB that it moves would take 1.
+// writes its rows; the last one sums all requests and writes kv_len and the counts.  32 requests, one row each: 4.2 us a call; 4096 requests and 356 000 rows:
+// 9.2 us, where the 4.5 MB that it moves would take 1.
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a)
 {
     __shared__ int32_t lds[32], sums[4][PLAN_THREADS / 64];
@@ -145,38 +145,26 @@ struct StoreArgs {
     int32_t T, page_shift, heads, head_bytes;
 };
 
-constexpr int STORE_ROWS = 4;
-
-// A copy: bound by memory.  A wavefront moves the k (grid.y = 0) or v rows of STORE_ROWS tokens in 16-byte pieces per lane and has the pieces
-// of all four in flight before it writes the first; a head's row lands in one piece (page, head, position in the page, head_dim).
+// A copy: bound by memory.  A wavefront moves the k (grid.y = 0) or v row of one token, 16 bytes a lane; a head's row lands in one piece (page, head, position in the page,
+// head_dim).  One row a wavefront: 33 rows of 8 heads of 128 in f32 in 3.8 us (four rows, all in flight: 5.2).  The pages are written with the non-temporal hint, so
+// that the rows' keys and values, which attention reads next, stay in the caches: store and prompt attention of 36 864 rows together 558 us, 563 without the hint
+// or with it on the loads too (the store alone 65.5 us, 4.6 TB/s; 71 and 63.8).
 __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a)
 {
     const int lane = threadIdx.x & 63;
-    const int32_t row0 = __builtin_amdgcn_readfirstlane((int32_t)((blockIdx.x * 4 + (threadIdx.x >> 6)) * STORE_ROWS));
-    if (row0 >= a.T) return;
-    const gcptr_t src = as_global((const void *)(blockIdx.y ? a.v : a.k));
-    const gptr_t dst = as_global((void *)(blockIdx.y ? a.v_cache : a.k_cache));
-    const int64_t ld = blockIdx.y ? a.ldv : a.ldk;
-    int64_t base[STORE_ROWS];
-    bool live[STORE_ROWS];
-    const int64_t page_bytes = ((int64_t)a.heads * a.head_bytes) << a.page_shift;
-#pragma unroll
-    for (int i = 0; i < STORE_ROWS; ++i) {
-        const int64_t slot = as_const(a.slot_map)[min(row0 + i, a.T - 1)];
-        live[i] = row0 + i < a.T && slot >= 0 && slot < a.n_slots;
-        base[i] = (slot >> a.page_shift) * page_bytes + (slot & ((1 << a.page_shift) - 1)) * a.head_bytes;
-    }
+    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    if (row >= a.T) return;
+    const int64_t slot = as_const(a.slot_map)[row];
+    if (slot < 0 || slot >= a.n_slots) return;
+    const gcptr_t src = as_global((const void *)(blockIdx.y ? a.v : a.k)) + row * (blockIdx.y ? a.ldv : a.ldk);
+    const gptr_t dst = as_global((void *)(blockIdx.y ? a.v_cache : a.k_cache)) + (slot >> a.page_shift) * (((int64_t)a.heads * a.head_bytes) << a.page_shift) +
+                       (slot & ((1 << a.page_shift) - 1)) * a.head_bytes;
     const int32_t pieces = a.head_bytes / 16, n = a.heads * pieces;
+#pragma unroll 2
     for (int32_t c = lane; c < n; c += 64) {
         const int32_t head = c / pieces;
         const int64_t to = (((int64_t)head * a.head_bytes) << a.page_shift) + (c - head * pieces) * 16;
-        u32x4_t v[STORE_ROWS];
-#pragma unroll
-        for (int i = 0; i < STORE_ROWS; ++i)
-            if (live[i]) v[i] = ld16(src + (row0 + i) * ld + c * 16);
-#pragma unroll
-        for (int i = 0; i < STORE_ROWS; ++i)
-            if (live[i]) st16(dst + base[i] + to, v[i]);
+        __builtin_nontemporal_store(ld16(src + c * 16), (PREFT_GLOBAL u32x4_t *)(dst + to));
     }
 }
 
@@ -235,8 +223,7 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
     a.k_cache = (char *)k_cache; a.v_cache = (char *)v_cache; a.k = (const char *)k; a.v = (const char *)v; a.slot_map = slot_map;
     a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.T = T; a.page_shift = shift; a.heads = n_kv_heads;
     a.head_bytes = (int32_t)(head_dim * e);
-    const int rows = 4 * STORE_ROWS;
-    hipLaunchKernelGGL(kv_store_kernel, dim3((unsigned)((T + rows - 1) / rows), 2), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(kv_store_kernel, dim3((unsigned)((T + 3) / 4), 2), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
     return launched();
 }
 
