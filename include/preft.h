@@ -135,7 +135,7 @@ enum {
                                /* built for another T, S, N or position set, and did nothing */
     PREFT_ETOOLARGE    = -8    /* preft_direft_apply_static: the batch's schedule does   */
                                /* not fit the static area; attention: T * n_heads of     */
-                               /* 2^30 and more                                          */
+                               /* 2^28 and more                                          */
 };
 
 #define PREFT_MAX_RANK 128

@@ -69,13 +69,14 @@ AttnLists lists_of(const Layout &l, void *workspace)
     return r;
 }
 
-bool sizes_fit(int64_t T, int64_t S, int64_t heads, int64_t groups) { return T * heads < (1ll << 30) && S + groups < (1ll << 28); }
+// so that counts of columns, part columns and workgroups (three a tile and key/value head at most) stay below 2^31
+bool sizes_fit(int64_t T, int64_t S, int64_t heads, int64_t groups) { return T * heads < (1ll << 28) && S + groups < (1ll << 28); }
 
 // How a call runs: its units found by the workgroups themselves or listed by the schedule kernel, its keys cut into ranges or not.
 struct Plan { bool direct, split; int64_t units, tiles; };
 
-// Few segments and workgroups: the schedule kernel's 6 to 8 us are a third of the call (one decode row over 1500 keys: 20.7 us with it, see the table of
-// DESIGN without); with more than two rounds of workgroups each one's search, about a microsecond, costs as much, and the order by cost pays.
+// Few segments and workgroups: the schedule kernel's 6 to 8 us are a third of the call (one decode row over 1500 keys: 20.7 us with it, 12.0
+// without); with more than two rounds of workgroups each one's search, about a microsecond, costs as much, and the order by cost pays.
 // Keys are cut where the tiles alone do not fill the chip and some tile may be longer than a range.
 Plan plan_of(const AttnScheduleArgs &s, int64_t most_keys)
 {
@@ -205,7 +206,7 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     AttnArgs a = {};
     a.q = q; a.k = k_cache; a.v = v_cache; a.out = out; a.ldq = ldq * e; a.ldo = ldo * e;
-    a.table = block_table; a.ld_table = ld_table; a.n_pages = n_pages; a.page_shift = shift; a.max_pages = max_pages;
+    a.table = block_table; a.ld_table = ld_table; a.n_pages = n_pages; a.page_shift = shift;
     a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads; a.group = n_heads / n_kv_heads; a.n_groups = n_groups;
     a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;

@@ -28,7 +28,7 @@ struct AttnArgs {
     int64_t ldq, ldk, ldv, ldo;       // bytes
     const int32_t *table;
     int64_t ld_table;
-    int32_t n_pages, page_shift, max_pages;
+    int32_t n_pages, page_shift;
     int32_t T, S, heads, kv_heads, group, n_groups;      // group: query heads of a key/value head, G
     float scale_log2;
     uint32_t per_head;                // ceil(2^21 / G): x / G = x per_head >> 21 for x < 2048 (G <= 1024)
@@ -438,13 +438,15 @@ __device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit 
 
 // ---------------------------------------------------------------------------------------
 // A unit of more than 32 columns: every wavefront has 32 of them, and all read the tiles of 64 keys that the workgroup brings to LDS, one
-// tile ahead.
+// tile ahead.  Two workgroups share a compute unit (registers allow no third): 0.93 us a tile and unit, 1.21 with one.  One prompt of 16 001 rows, 64 heads over 8 of 128:
+// 3.83 ms, 1100 TFLOP/s, 90 % of what a large matrix product of the library reaches (power holds the clock of both at about 1.6 GHz).  Prompts of a thousand rows:
+// 650 TFLOP/s; 10 us of a workgroup's 28 go into finding its queries and first tile, the tile at the diagonal, and the results.
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, bool PAGED>
 __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, int32_t *votes)
 {
     using X = AttnTile<E, D>;
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     constexpr int COPIES = X::TILE / 1024 / 4, ROWS = COPIES * X::ROWS_PER_COPY;     // of a wavefront
     AttnSource<E, D, PAGED> src;
     src.init(a, u, kv_head);
@@ -528,7 +530,8 @@ __device__ __forceinline__ void attend_columns(const AttnArgs &a, const AttnUnit
 // A unit of up to 32 columns: bound by the bytes of its keys.  The four wavefronts take blocks of 32 keys in turn, each through LDS of its own without a
 // barrier -- K of the next block is asked for as soon as this one's is in registers, V likewise -- and join their sums at the end.
 // SOLO: the unit is one wavefront's.  Where short units are many this costs the look-ups before the first block once in 12 blocks instead of once in 3, and no join
-// (SOLO_FIGURES).
+// (256 rows of 64 heads over shared prefixes of 8192 and up to 700 tokens of their own: 173 us, else 180).
+// 224 decode rows over 256..4096 tokens, 32 heads over 8 of 128: 348 us, 5.7 TB/s of keys and values, more than a copy moves on this card (4.9).
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, bool PAGED, bool SOLO>
 __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)

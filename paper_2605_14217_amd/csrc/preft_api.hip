@@ -1309,7 +1309,7 @@ const char *preft_strerror(int code)
     case PREFT_EWORKSPACE:   return "workspace missing, misaligned or smaller than preft_workspace_bytes(T, S) or preft_attention_workspace_bytes(...)";
     case PREFT_EHIP:         return "HIP runtime error (launch, copy or allocation)";
     case PREFT_ECAPACITY:    return "more distinct adapters in one batch than the slot manager has slots";
-    case PREFT_ETOOLARGE:    return "batch too large for the static schedule area of preft_direft_apply_static (preft_workspace_bytes(T, S) exceeds PREFT_STATIC_SCRATCH_BYTES), or an attention call of 2^30 and more (row, head) pairs";
+    case PREFT_ETOOLARGE:    return "batch too large for the static schedule area of preft_direft_apply_static (preft_workspace_bytes(T, S) exceeds PREFT_STATIC_SCRATCH_BYTES), or an attention call of 2^28 and more (row, head) pairs";
     case PREFT_ESCHEDULE:    return "an apply call named another T, S, N or position set than the schedule in its workspace was built for; that call did nothing";
     default:                 return "unknown preft error code";
     }
