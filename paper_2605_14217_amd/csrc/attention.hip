@@ -75,16 +75,30 @@ bool sizes_fit(int64_t T, int64_t S, int64_t heads, int64_t groups) { return T *
 // How a call runs: its units found by the workgroups themselves or listed by the schedule kernel, its keys cut into ranges or not.
 struct Plan { bool direct, split; int64_t units, tiles; };
 
-// Few segments and workgroups: the schedule kernel's 6 to 8 us are a third of the call (one decode row over 1500 keys: 20.7 us with it, 12.0
-// without); with more than two rounds of workgroups each one's search, about a microsecond, costs as much, and the order by cost pays.
+// The workgroups that the keys are spread over.  n tiles of about the same work, cut into ranges of 1/spread of it all, make up to n + spread units: no more than run
+// side by side where spread = ATTN_TARGET - n (eight decode rows over 8000..30 000 keys: 124 us, spread over all 512 workgroups 147).  Wide tiles are cut no shorter than
+// min_wide, fewer key tiles the fewer of them there are; a key tile of f32 takes longer, and counts for four (one prompt of 800 rows, 14 heads: 34 us at 2 key tiles,
+// 36 at 4, 60 uncut).
+void spread(AttnScheduleArgs &s, int dtype)
+{
+    const int64_t n = (int64_t)s.l.tile_cap * s.kv_heads, least = dtype == PREFT_BF16 ? 2 : 1, wide = dtype == PREFT_BF16 ? n / 8 : n / 32, most = 8 * least;
+    s.spread = (int32_t)(n > ATTN_TARGET ? ATTN_TARGET : ATTN_TARGET - n > ATTN_TARGET / 2 ? ATTN_TARGET - n : ATTN_TARGET / 2);
+    s.min_tiles = (int32_t)least;
+    s.min_wide = (int32_t)(wide > most ? most : wide < least ? least : wide);
+}
+
+// Few segments and workgroups: the schedule kernel's launch is a third of the call (one decode row over 1500 keys: 17.0 us with it, 11.7 without; 40 chat-length
+// prompts 12.1 and 7.7); with more than two rounds of workgroups each one's search, about a microsecond, costs as much, and the order by time pays.  For decode rows,
+// whose keys are cut one by one then, it does from one round on (64 rows over 4000..16 000 keys: 487 us without the kernel, 468 with it).
 // Keys are cut where the tiles alone do not fill the chip and some tile may be longer than a range.
 Plan plan_of(const AttnScheduleArgs &s, int64_t most_keys)
 {
     Plan p;
     const int64_t key_tiles = (most_keys + ATTN_KEYS - 1) / ATTN_KEYS;
     p.tiles = s.l.tile_cap;
+    const bool narrow = (int64_t)s.T * s.group <= (int64_t)s.S * ATTN_FEW_COLS;
     p.split = s.can_split && key_tiles > 2 * s.min_tiles;
-    p.direct = s.n_groups == 0 && s.S <= ATTN_DIRECT && p.tiles * s.kv_heads <= 2 * ATTN_TARGET;
+    p.direct = s.n_groups == 0 && s.S <= ATTN_DIRECT && p.tiles * s.kv_heads <= (narrow && s.can_split ? 1 : 2) * ATTN_TARGET;
     const int64_t ranges = (ATTN_TARGET + s.kv_heads - 1) / s.kv_heads;
     p.units = !p.split ? p.tiles : p.direct ? p.tiles + 2 * ranges + 2 : 3 * p.tiles + ranges + 2;
     const int64_t most = p.tiles * ((key_tiles + s.min_tiles - 1) / s.min_tiles);
@@ -172,10 +186,12 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
     AttnScheduleArgs &s = a.s;
     s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = a.group;
     s.max_keys = T; s.l = a.l;
-    // Cut only where the prompts are long on average and their tiles do not fill the chip twice over: a prompt has tiles by its rows as it has keys, and a
-    // merge launch with nothing to join costs 4 us of the 10 that a batch of chat-length prompts takes.
-    s.can_split = (int64_t)l.tile_cap * n_kv_heads < 2 * ATTN_TARGET && T >= 512 * (int64_t)S;
-    s.min_tiles = dtype == PREFT_BF16 ? 8 : 4;
+    // Cut only where the prompts are long on average and their tiles do not fill half the chip: a prompt has tiles by its rows as it has keys, and a
+    // merge launch with nothing to join costs 4 us of the 10 that a batch of chat-length prompts takes (8 heads over 2 of 128: 4000 rows 66 us, uncut 74; 6000 rows
+    // 115 uncut, cut 132; 32 heads over 8, 1200 rows: 30 uncut, cut 75).
+    s.can_split = (int64_t)l.tile_cap * n_kv_heads <= ATTN_TARGET / 2 && T >= 512 * (int64_t)S;
+    spread(s, dtype);
+    s.min_tiles = s.min_wide;
     return run<false>(a, dtype, head_dim, mode, T, st);
 }
 
@@ -217,7 +233,7 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     const int64_t most = (int64_t)max_pages << shift;
     s.max_keys = keys ? (int32_t)(most < (1 << 30) ? most : (1 << 30)) : 0;
     s.can_split = 1;
-    s.min_tiles = dtype == PREFT_BF16 ? 2 : 1;
+    spread(s, dtype);
     return run<true>(a, dtype, head_dim, mode, s.max_keys, st);
 }
 

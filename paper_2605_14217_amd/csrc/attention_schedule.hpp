@@ -58,7 +58,7 @@ struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
     const int32_t *kv_len;                                 // null: packed whole prompts
     const int32_t *group_start, *group_prefix;
-    int32_t S, T, n_groups, heads, kv_heads, group, max_keys, can_split, min_tiles;    // group: heads / kv_heads
+    int32_t S, T, n_groups, heads, kv_heads, group, max_keys, can_split, min_tiles, min_wide, spread;    // group: heads / kv_heads; spread: workgroups that a range's length is meant for
     AttnLists l;
 };
 
@@ -87,6 +87,12 @@ __device__ __forceinline__ AttnItem attn_segment(const AttnScheduleArgs &a, int3
 
 __device__ __forceinline__ int32_t key_tiles(int32_t key0, int32_t key1) { return key1 > key0 ? (key1 - 1) / ATTN_KEYS - key0 / ATTN_KEYS + 1 : 0; }
 
+// A part of a wide tile is 64 KB written and read again, which on a full chip takes the time of some 14 key tiles: cut only where tiles are few, or this one long.
+// (16 requests of 40 rows over 100..2000 tokens: 56 us, cut by `range` 85; one prompt of 900 rows 23 us, cut by 8 key tiles 37; of 2000 rows and 8 heads 33 us cut by 8, uncut 40.)
+__device__ __forceinline__ int32_t wide_range(const AttnScheduleArgs &a, int32_t range)
+{
+    return max(a.min_wide, a.spread <= ATTN_TARGET / 2 ? min(range, INT32_MAX / 2) * 2 : range);
+}
 __device__ __forceinline__ int32_t ranges_of(int32_t tiles, int32_t range) { return tiles > range ? (int32_t)((uint32_t)(tiles - 1) / (uint32_t)range) + 1 : 1; }
 // where part k of `parts` of n tiles begins: the first n % parts have one more
 __device__ __forceinline__ int32_t part_begin(int32_t n, int32_t parts, int32_t k)
@@ -214,12 +220,12 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     if ((tid & 63) == 0) atomicAdd(&cost_sum, cost);
     __syncthreads();
     const int32_t n_tiles = min(carry, a.l.tile_cap);
-    // a range of keys: no shorter than the whole work over the workgroups that run side by side
+    // a range of keys: no shorter than the whole work over the workgroups it is meant for
     // (Wide and narrow tiles each for themselves: 206 us against 173 on 256 rows of 64 heads with prefixes of 8192.  All workgroups are wide ones then at first, and memory
     // waits for the narrow ones.)
     int32_t range = INT32_MAX;
     if (a.can_split) {
-        const unsigned long long even = (cost_sum * (unsigned)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET;
+        const unsigned long long even = (cost_sum * (unsigned)a.kv_heads + a.spread - 1) / (unsigned)a.spread;
         range = max(a.min_tiles, (int32_t)min(even, (unsigned long long)INT32_MAX));
     }
     if (a.n_groups > 0) {                                  // a group's parts stand together, tile by tile: its members find them by their columns
@@ -282,7 +288,7 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
             d.u.lim0 = __hip_atomic_load(&a.l.group_low[i - a.S], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         d.n = key_tiles(d.key0, d.key1);
-        d.splits = d.n == 0 && d.g >= 0 ? 0 : ranges_of(d.n, range);      // 0: the group's part is all there is
+        d.splits = d.n == 0 && d.g >= 0 ? 0 : ranges_of(d.n, i < a.S && d.u.ncols > ATTN_FEW_COLS ? wide_range(a, range) : range);      // 0: the group's part is all there is
         d.parts = d.splits > 1 || d.g >= 0 || i >= a.S;
         const int32_t each = d.splits > 0 ? (int32_t)((uint32_t)d.n / (uint32_t)d.splits) : 0;
         // by time: 64 keys of a wide unit take 2.5 times those of a narrow one; short units stand at the end
@@ -394,14 +400,14 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
     if (a.can_split) {
         const int32_t n = min(a.S, 64);
         cost = __builtin_amdgcn_readlane(wave_inclusive(cost, n), n - 1);
-        range = max(a.min_tiles, (int32_t)min(((uint64_t)(uint32_t)cost * (uint32_t)a.kv_heads + ATTN_TARGET - 1) / ATTN_TARGET, (uint64_t)INT32_MAX));
+        range = max(a.min_tiles, (int32_t)min(((uint64_t)(uint32_t)cost * (uint32_t)a.kv_heads + a.spread - 1) / (uint32_t)a.spread, (uint64_t)INT32_MAX));
     }
     AttnDirect r = {};
     int32_t before = 0, slots = 0, tiles_before = 0;
 #pragma unroll
     for (int c = 0; c < EACH; ++c) {
         if (c * 64 >= a.S) continue;
-        const int32_t parts = ranges_of(key_tiles(0, it[c].key1), range), units = tiles[c] * parts;
+        const int32_t parts = ranges_of(key_tiles(0, it[c].key1), it[c].rows * G > ATTN_FEW_COLS ? wide_range(a, range) : range), units = tiles[c] * parts;
         const int32_t need = parts > 1 ? (int32_t)min((int64_t)it[c].rows * G * parts * a.kv_heads, (int64_t)a.l.slot_cap) : 0;
         const int32_t lanes = min(a.S - c * 64, 64);
         const int32_t upto = wave_inclusive(units, lanes), slot = a.can_split ? wave_inclusive(need, lanes) : 0;
