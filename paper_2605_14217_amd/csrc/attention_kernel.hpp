@@ -667,7 +667,7 @@ __device__ __forceinline__ bool attn_schedule_is(const AttnArgs &a, int kind)
 }
 
 // Consecutive workgroups take the key/value heads of one unit: with 8 heads, or a multiple, every XCD keeps to its own heads' keys in its L2.
-// DIRECT: there is no list, every wavefront finds the unit by itself; the first workgroup leaves the header that a later call asks for.
+// DIRECT: there is no list, every wavefront finds the unit by itself (attn_direct_unit).
 template <typename E, int D, bool PAGED, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
 {
@@ -679,22 +679,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
     AttnUnit u;
     if constexpr (DIRECT) {
         if (a.ready && !attn_schedule_is(a, KIND)) return;
-        const AttnDirect d = attn_direct(a.s, unit);
-        if (!a.ready && blockIdx.x == 0 && threadIdx.x == 0) {
-            int32_t *h = a.l.header;
-            h[AH_UNITS] = d.units; h[AH_MERGES] = d.joined; h[AH_TILES] = d.tiles; h[AH_JOINS] = min(d.tiles, a.l.merge_cap); h[AH_KIND] = KIND;
-            h[AH_GROUPS] = 0; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
-        }
-        if (!d.found) return;
-        u = attn_unit_of(a.s, d);
-        if (a.s.can_split && d.part == 0 && kv_head == 0 && threadIdx.x == 0) {
-            const int32_t tile = (d.it.rows * a.group + ATTN_COLS - 1) / ATTN_COLS - 1 - d.tile, to = d.tiles_before + tile;
-            AttnMerge j = {};
-            j.row0 = d.it.row0; j.col0 = tile * ATTN_COLS; j.ncols = u.ncols; j.group_cols = ATTN_COLS;
-            j.parts = d.parts > 1 ? d.parts : 0;
-            j.slot = d.slot + j.col0 * d.parts * a.kv_heads;
-            if (to < a.l.merge_cap) a.l.merges[to] = j;
-        }
+        if (!attn_direct_unit(a.s, unit, kv_head, a.ready != 0, u)) return;
     } else {
         if (!attn_schedule_is(a, KIND)) return;
         // short units: one a wavefront, four a workgroup

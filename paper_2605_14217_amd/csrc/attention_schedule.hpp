@@ -462,4 +462,27 @@ __device__ __forceinline__ AttnUnit attn_unit_of(const AttnScheduleArgs &a, cons
     return u;
 }
 
+// The unit that a workgroup of a direct call finds; false: none.  The first workgroup leaves the header that a later call asks for, unless it is there already (`ready`), and
+// a tile's first unit the entry of its merge.
+__device__ __forceinline__ bool attn_direct_unit(const AttnScheduleArgs &a, int32_t unit, int32_t kv_head, bool ready, AttnUnit &u)
+{
+    const AttnDirect d = attn_direct(a, unit);
+    if (!ready && unit == 0 && kv_head == 0 && threadIdx.x == 0) {
+        int32_t *h = a.l.header;
+        h[AH_UNITS] = d.units; h[AH_MERGES] = d.joined; h[AH_TILES] = d.tiles; h[AH_JOINS] = min(d.tiles, a.l.merge_cap); h[AH_KIND] = a.kv_len ? 2 : 1;
+        h[AH_GROUPS] = 0; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
+    }
+    if (!d.found) return false;
+    u = attn_unit_of(a, d);
+    if (a.can_split && d.part == 0 && kv_head == 0 && threadIdx.x == 0) {
+        const int32_t tile = (d.it.rows * a.group + ATTN_COLS - 1) / ATTN_COLS - 1 - d.tile, to = d.tiles_before + tile;
+        AttnMerge j = {};
+        j.row0 = d.it.row0; j.col0 = tile * ATTN_COLS; j.ncols = u.ncols; j.group_cols = ATTN_COLS;
+        j.parts = d.parts > 1 ? d.parts : 0;
+        j.slot = d.slot + j.col0 * d.parts * a.kv_heads;
+        if (to < a.l.merge_cap) a.l.merges[to] = j;
+    }
+    return true;
+}
+
 }  // namespace preft

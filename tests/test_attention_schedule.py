@@ -1,0 +1,94 @@
+"""The schedule of attention calls, run on the CPU by the kernels' own code (tests/attention_schedule_driver.hip): every row of a call gets its result once, from its keys, whatever the
+batch looks like, and no index leaves its list."""
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None, reason="needs hipcc")
+F32, BF16 = 0, 1
+PROMPT, CACHED, MALFORMED = 1, 2, 10
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    exe = tmp_path_factory.mktemp("attention_schedule") / "driver"
+    build = subprocess.run(["hipcc", "--cuda-host-only", "-std=c++17", "-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+                            "-Xarch_host", "-fno-sanitize-recover=all", os.path.join(ROOT, "tests", "attention_schedule_driver.hip"), "-o", str(exe)],
+                           capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr
+    return exe
+
+
+def call(kind, dtype, heads, kv_heads, rows, prefill=None, kv=None, max_keys=0, group_start=None, prefix=None, start=None, T=None):
+    """One call of the driver's input; rows of the segments, or their offsets."""
+    if start is None:
+        start = np.concatenate([[0], np.cumsum(rows)])
+    S, prefix = len(start) - 1, [] if prefix is None else prefix
+    words = [kind, dtype, int(start[-1]) if T is None else T, S, heads, kv_heads, len(prefix), max_keys, *start, *([0] * S if prefill is None else prefill)]
+    if kind % MALFORMED == CACHED:
+        words += [*kv, *(group_start if len(prefix) else []), *prefix]
+    return " ".join(str(int(w)) for w in words)
+
+
+def answers(driver, calls):
+    """direct, split, merge, units, grid, entries of every call, after a look at the verdicts."""
+    run = subprocess.run([str(driver)], input="\n".join(calls) + "\n", capture_output=True, text=True, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"), timeout=600)
+    assert run.returncode == 0, run.stdout[-500:] + run.stderr[-3000:]
+    lines = [line.split(" ", 6) for line in run.stdout.splitlines()]
+    assert len(lines) == len(calls)
+    for asked, line in zip(calls, lines):
+        assert line[6] == "ok", (line, asked[:400])
+    return [[int(x) for x in line[:6]] for line in lines]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_groups_over_short_tables_are_joined(driver, dtype):
+    """Tables so short that no keys are cut: the rows of a group are parts all the same."""
+    calls, lengths = [], [64, 96, 128, 160, 192, 256, 272, 320]
+    for most in lengths:
+        calls.append(call(CACHED, dtype, 8, 2, [1, 1, 1, 40, 1, 1], kv=[most, most - 1, 64, 60, most, 9], max_keys=most, group_start=[0, 3, 5], prefix=[64, 64 if most > 64 else 3]))
+    got = answers(driver, calls)
+    assert {g[1] for g in got} == {0, 1}, "tables on both sides of the line are meant"
+    for most, (direct, _, merge, _, _, joins) in zip(lengths, got):
+        assert not direct and merge and joins >= 3
+
+
+def random_call(rng):
+    kv_heads = int(rng.choice([1, 2, 3, 8]))
+    heads = kv_heads * int(rng.choice([1, 1, 4, 7, 8, 40]))
+    S = int(rng.choice([1, 2, 5, 17, 60, 300]))
+    dtype = int(rng.integers(0, 2))
+    most_rows = int(rng.choice([1, 2, 8, 40, 300 if S < 20 else 8]))
+    rows = rng.integers(0, most_rows + 1, size=S)
+    if rng.random() < 0.4:
+        rows[:] = np.minimum(rows, 1)
+    if rows.sum() == 0:
+        rows[0] = 1
+    if rng.random() < 0.35:
+        prefill = rng.integers(0, rows.max() + 2, size=S)
+        if rng.random() < 0.3:
+            rows[0] = 2500 // max(1, heads // kv_heads // 8)
+            prefill[0] = rows[0]
+        return call(PROMPT, dtype, heads, kv_heads, rows, prefill)
+    max_keys = 16 * int(rng.choice([2, 8, 10, 16, 17, 40, 300, 3000]))
+    kv = np.maximum(rng.integers(0, max_keys + 1, size=S) - rng.integers(0, 2) * rng.integers(0, max_keys, size=S), 0)
+    prefill = rng.integers(0, 3, size=S) if rng.random() < 0.3 else None
+    if rng.random() < 0.5:
+        return call(CACHED, dtype, heads, kv_heads, rows, prefill, kv, max_keys)
+    g = int(rng.integers(1, 6))
+    start = np.sort(rng.integers(0, S + 1, size=g + 1))
+    if rng.random() < 0.5:
+        start[0], start[-1] = 0, S
+    return call(CACHED, dtype, heads, kv_heads, rows, prefill, kv, max_keys, start, rng.integers(0, max_keys + 1, size=g))
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_every_row_of_random_batches_is_written_once_from_its_keys(driver, seed):
+    rng = np.random.Generator(np.random.PCG64(seed))
+    got = answers(driver, [random_call(rng) for _ in range(60)])
+    assert {(g[0], g[2]) for g in got} == {(0, 0), (0, 1), (1, 0), (1, 1)}
+    assert all(units <= grid for _, _, _, units, grid, _ in got)

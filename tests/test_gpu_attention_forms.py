@@ -1,0 +1,70 @@
+"""Forms of the attention calls in which every row needs a second look: groups over short tables, replayed graphs.  Against the definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import attention_reference as ref
+import paper_2605_14217_amd as preft
+from test_gpu_attention import HEADS, cached_case, i32, normal
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("most,page,prefix", [(64, 16, 64), (96, 8, 75), (128, 64, 128), (192, 16, 100), (256, 64, 200), (272, 16, 256)])
+@pytest.mark.parametrize("dtype,H,Hkv,D", HEADS[:4])
+def test_groups_over_short_tables(dtype, H, Hkv, D, most, page, prefix):
+    """Block tables of 64 to 272 tokens, where no keys are cut: a group's rows still have their shared keys as a part of their own.  Shared prefixes at the end of a
+    page and inside one, members that end before it, a second group, prompt rows in between, and requests in no group."""
+    print(f"\n[case] short groups {dtype} {H}/{Hkv}x{D} most={most} page={page} prefix={prefix}", flush=True)
+    rows = [1, 2, 1, 1, 1, 3, 1]
+    kv = [most, most, prefix, prefix - 3, most - 1, most, 20]
+    out, before, want, args, _, (gs, gp, H, scale) = cached_case(dtype, H, Hkv, D, page, rows, kv, prefill=[0, 0, 5, 0, 0, 0, 0], groups=[(0, 4), (4, 6)],
+                                                                 prefix=[prefix, 64])
+    print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+    narrow = args[6][:, : -(-most // page)]                    # a table without room for more
+    again = torch.full_like(out, -3.0)
+    preft.preft_cached_attention(again, *args[:6], narrow, gs, gp, H, scale, 0, preft.new_attention_workspace(out.shape[0], len(rows), H, Hkv, D, 2))
+    ref.check(again.cpu(), want, torch.full_like(before, -3.0))
+
+
+@pytest.mark.parametrize("pages", [6, 40])
+def test_replayed_steps_against_the_definitions(pages):
+    """A step's two calls in a graph, replayed with other contents of the same tables between eager work; every replay against the definitions, in an output that held something
+    else before.  Tables in which nothing is cut, and longer ones."""
+    print(f"\n[case] graph and definitions, {pages} pages", flush=True)
+    H, Hkv, D, page, S = 8, 2, 128, 16, 6
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    pool = S * pages
+    kc, vc = (normal(gen, pool, Hkv, page, D).bfloat16() for _ in "kv")
+    qkv = normal(gen, 90, (H + 2 * Hkv) * D).bfloat16()
+    q, k, v = qkv[:, :H * D], qkv[:, H * D:(H + Hkv) * D], qkv[:, (H + Hkv) * D:]
+    start, long = [0, 50, 51, 52, 53, 89, 90], pages * page - 20
+    table = np.random.Generator(np.random.PCG64(0)).permutation(pool).reshape(S, pages)
+    table[2:4, :5] = table[1, :5]                              # the group's shared pages
+    dev, gs, gp = i32(table), i32([1, 4]), i32([80])
+    prefill, kv = i32([50, 0, 0, 0, 36, 0]), i32([0, long, 33, long, 0, 7])
+    seg = i32(start)
+    out = torch.zeros(90, H * D, dtype=torch.bfloat16, device="cuda")
+    w1, w2 = preft.new_attention_workspace(90, S, H, Hkv, D), preft.new_attention_workspace(90, S, H, Hkv, D, 1)
+
+    def step():
+        preft.preft_prompt_attention(out, q, k, v, seg, prefill, H, Hkv, 0.09, 0, w1)
+        preft.preft_cached_attention(out, q, seg, prefill, kv, kc, vc, dev, gs, gp, H, 0.09, 0, w2)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        n, kvl = [50 - i, 0, 0, 0, 36 - 2 * i, 0], [0, long - i, 33 + 5 * i, long - 3 * i, 0, 7 + i]
+        kv.copy_(i32(kvl))
+        prefill.copy_(i32(n))
+        q += 0.01
+        out.fill_(2.0 + i)
+        before = out.cpu()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = ref.cached(q.cpu(), start, n, kvl, kc.cpu(), vc.cpu(), table, H, 0.09)
+        want.update(ref.prompt(q.cpu(), k.cpu(), v.cpu(), start, n, H, Hkv, 0.09))
+        assert len(want) == 90
+        print(f"  replay {i}: {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
