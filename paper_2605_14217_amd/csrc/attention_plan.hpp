@@ -107,6 +107,7 @@ inline void cached_rules(AttnScheduleArgs &s, int dtype, int64_t most_keys)
 // Few segments and workgroups: the schedule kernel's launch is a third of the call (one decode row over 1500 keys: 17.0 us with it, 11.7 without; 40 chat-length
 // prompts 12.1 and 7.7); with more than two rounds of workgroups each one's search, about a microsecond, costs as much, and the order by time pays.  For decode rows,
 // whose keys are cut one by one then, it does from one round on (64 rows over 4000..16 000 keys: 487 us without the kernel, 468 with it).
+// The workgroups sum the work of all tiles in 31 bits: where tables are so long that it may not fit, the schedule kernel does it in 64.
 // Keys are cut where the tiles alone do not fill the chip and some tile may be longer than a range.
 inline Plan plan_of(const AttnScheduleArgs &s)
 {
@@ -116,7 +117,8 @@ inline Plan plan_of(const AttnScheduleArgs &s)
     const bool narrow = (int64_t)s.T * s.group <= (int64_t)s.S * ATTN_FEW_COLS;
     p.split = s.can_split && key_tiles > 2 * s.min_tiles;
     p.merge = p.split || s.n_groups > 0;
-    p.direct = s.n_groups == 0 && s.S <= ATTN_DIRECT && p.tiles * s.kv_heads <= (narrow && s.can_split ? 1 : 2) * ATTN_TARGET;
+    p.direct = s.n_groups == 0 && s.S <= ATTN_DIRECT && p.tiles * s.kv_heads <= (narrow && s.can_split ? 1 : 2) * ATTN_TARGET &&
+               p.tiles * (key_tiles + 1) <= INT32_MAX;
     const int64_t ranges = (ATTN_TARGET + s.kv_heads - 1) / s.kv_heads;
     p.units = !p.split ? p.tiles : p.direct ? p.tiles + 2 * ranges + 2 : 3 * p.tiles + ranges + 2;
     const int64_t most = p.tiles * ((key_tiles + s.min_tiles - 1) / s.min_tiles);

@@ -393,7 +393,7 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
         tiles[c] = (it[c].rows * G + ATTN_COLS - 1) / ATTN_COLS;
         if (tiles[c] > 0) {
             const int32_t low = min(it[c].key1, it[c].lim0 + (min(it[c].rows * G, ATTN_COLS) - 1) / G);
-            cost += (int32_t)min(((int64_t)tiles[c] * (key_tiles(0, low) + key_tiles(0, it[c].key1) + 1)) / 2, (int64_t)(INT32_MAX / 1024));
+            cost += (int32_t)(((int64_t)tiles[c] * (key_tiles(0, low) + key_tiles(0, it[c].key1) + 1)) / 2);      // all of them fit 31 bits: plan_of
         }
     }
     int32_t range = INT32_MAX;

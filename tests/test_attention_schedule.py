@@ -92,3 +92,19 @@ def test_every_row_of_random_batches_is_written_once_from_its_keys(driver, seed)
     got = answers(driver, [random_call(rng) for _ in range(60)])
     assert {(g[0], g[2]) for g in got} == {(0, 0), (0, 1), (1, 0), (1, 1)}
     assert all(units <= grid for _, _, _, units, grid, _ in got)
+
+
+def test_batches_over_very_long_tables(driver):
+    """Workgroups and parts are enough whatever the keys come to: many tiles over millions of tokens, and tables so long that the work of all tiles does not fit 31 bits, on both sides of
+    that line."""
+    calls = [call(CACHED, BF16, 16, 1, [8184], kv=[600_000], max_keys=600_000),              # 1023 tiles of 9375 key tiles
+             call(CACHED, F32, 16, 1, [4000], kv=[3_000_000], max_keys=3_000_000),
+             call(CACHED, BF16, 8, 8, [1500, 3, 40], kv=[2_000_000, 17, 1 << 20], max_keys=1 << 21),
+             call(CACHED, F32, 2, 1, [8000, 6000, 9000], kv=[9_000_000, 9_000_000, 100], max_keys=10_000_000),
+             call(PROMPT, BF16, 8, 2, [8000], prefill=[8000])]
+    for S in (1, 8, 126, 127, 128, 200, 300):
+        calls.append(call(CACHED, BF16, 4, 1, [1] * S, kv=[(1 << 30) - 7 * s for s in range(S)], max_keys=1 << 30))
+        calls.append(call(CACHED, F32, 4, 4, [1] * S, kv=[(1 << 30) >> (s % 31) for s in range(S)], max_keys=1 << 30))
+    got = answers(driver, calls)
+    assert {g[0] for g in got[5:]} == {0, 1}
+    assert all(units <= grid for _, _, _, units, grid, _ in got)

@@ -68,3 +68,23 @@ def test_replayed_steps_against_the_definitions(pages):
         want.update(ref.prompt(q.cpu(), k.cpu(), v.cpu(), start, n, H, Hkv, 0.09))
         assert len(want) == 90
         print(f"  replay {i}: {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+
+
+def test_a_wide_chunk_over_very_many_tokens():
+    """8184 rows of 16 heads over one key/value head and 600 000 tokens: more work than the search for units once summed.  Every row is
+    written; rows of several tiles, and at their ends."""
+    print("\n[case] 8184 rows over 600 000 tokens", flush=True)
+    H, D, page, T, kv = 16, 64, 256, 8184, 600_000
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n_pages = -(-kv // page)
+    kc, vc = (normal(gen, n_pages, 1, page, D).bfloat16() for _ in "kv")
+    q = (2.0 * normal(gen, T, H * D)).bfloat16()
+    table = torch.randperm(n_pages, generator=gen, device="cuda").int()[None]
+    out = torch.full_like(q, 7.5)
+    ws = preft.new_attention_workspace(T, 1, H, 1, D)
+    preft.preft_cached_attention(out, q, i32([0, T]), None, i32([kv]), kc, vc, table, None, None, H, 0.125, 0, ws)
+    assert not bool((out == 7.5).all(1).any())
+    K, V = (c[table[0].long()].reshape(1, -1, D).cpu().double() for c in (kc, vc))
+    for t in (0, 7, 8, 15, 2047, 4096, 8175, 8176, 8183):
+        o, bound = ref.attend_row(q[t].cpu().double().view(H, D), K[:, : kv - (T - 1 - t)], V[:, : kv - (T - 1 - t)], 0.125, q.dtype)
+        assert ((out[t].cpu().double().view(H, D) - o).abs() <= bound).all(), t
