@@ -420,7 +420,7 @@ int preft_slots_stats(const preft_slots_t *m, int64_t *stats);
  *
  * As in the apply calls everything is enqueued on `stream`, nothing is allocated or synchronised, launch sizes follow from host-visible sizes,
  * and contents of device tables are not validated: positions, pages and rows are clamped to what exists, so that a malformed table gives unspecified results,
- * never an access out of range.
+ * never an access out of range.  (An attention call writes nothing where offsets in seg_start or group_start go back.)
  *
  * preft_kv_plan: ctx_len[s] tokens of request s are in the cache, and its seg_start[s + 1] - seg_start[s] rows follow them.  For all rows t,
  *   positions[t]  the row's position in its request (for rotary embeddings),

@@ -52,7 +52,7 @@ struct AttnLists {
     int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
 };
 
-constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11;      // AH_JOINS: entries of merges
+constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11;      // AH_SHORT: first unit that is one wavefront's; AH_JOINS: entries of merges
 
 struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
@@ -63,6 +63,10 @@ struct AttnScheduleArgs {
 };
 
 struct AttnItem { int32_t row0, rows, lim0, key0, key1; };
+
+// Entry i of a table of offsets, each cut to 0..most, and the next: does it go back?  Where none does, segments (and groups) are disjoint, and every bound on lists,
+// sums and grids follows from T and S; a call with an offset that goes back has no units.  All other entries of the tables are cut to what exists.
+__device__ __forceinline__ bool goes_back_at(const int32_t *start, int32_t i, int32_t most) { return max(0, min(start[i + 1], most)) < max(0, min(start[i], most)); }
 
 __device__ __forceinline__ AttnItem attn_segment(const AttnScheduleArgs &a, int32_t s)
 {
@@ -101,6 +105,14 @@ __device__ __forceinline__ int32_t part_begin(int32_t n, int32_t parts, int32_t 
     return each * k + min(k, n - each * parts);
 }
 
+// what a later call and the join go by; joined: tiles of more than one part
+__device__ __forceinline__ void attn_header(const AttnScheduleArgs &a, int32_t units, int32_t alone, int32_t tiles, int32_t joined, int32_t joins)
+{
+    int32_t *h = a.l.header;
+    h[AH_UNITS] = units; h[AH_SHORT] = alone; h[AH_TILES] = tiles; h[AH_MERGES] = joined; h[AH_JOINS] = joins; h[AH_MISMATCH] = 0;
+    h[AH_KIND] = a.kv_len ? 2 : 1; h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_KV_HEADS] = a.kv_heads;
+}
+
 struct AttnGroup { int32_t begin, end, rows, prefix; };
 
 __device__ __forceinline__ AttnGroup attn_group(const AttnScheduleArgs &a, int32_t g)
@@ -134,13 +146,23 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     __shared__ int32_t lds[32];
     __shared__ int32_t first_tile[ATTN_SCAN + 1];
     __shared__ int32_t bins[512];
-    __shared__ int32_t n_units, n_long,  n_merges, n_slots;
+    __shared__ int32_t n_units, n_long, n_merges, n_slots, goes_back;
     __shared__ unsigned long long cost_sum;
     const int tid = threadIdx.x, nt = blockDim.x;
     const int32_t G = a.group, items = a.S + a.n_groups;
     const bool in_lds = items <= ATTN_SCAN;
-    if (tid == 0) { n_merges = 0; n_slots = 0; cost_sum = 0; }
+    if (tid == 0) { n_merges = 0; n_slots = 0; cost_sum = 0; goes_back = 0; }
     for (int b = tid; b < 512; b += nt) bins[b] = 0;
+    __syncthreads();
+    for (int32_t s = tid; s < a.S; s += nt)
+        if (goes_back_at(a.seg_start, s, a.T)) goes_back = 1;
+    for (int32_t g = tid; g < a.n_groups; g += nt)
+        if (goes_back_at(a.group_start, g, a.S)) goes_back = 1;
+    __syncthreads();
+    if (goes_back) {
+        if (tid == 0) attn_header(a, 0, 0, 0, 0, 0);
+        return;
+    }
 
     // groups: how many rows each has, and where they stand in the row list
     if (a.n_groups > 0) {
@@ -342,12 +364,9 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     }
     __syncthreads();
     if (tid == 0) {
-        int32_t *h = a.l.header;
-        const int32_t units = min(n_units, a.l.unit_cap);
-        // enough of them that a wavefront each fills the chip: 2048 wavefronts run side by side
-        h[AH_SHORT] = (units - n_long) * a.kv_heads >= 2 * ATTN_TARGET ? min(n_long, units) : units;
-        h[AH_UNITS] = units; h[AH_MERGES] = min(n_merges, a.l.merge_cap); h[AH_JOINS] = min(n_merges, a.l.merge_cap); h[AH_TILES] = n_tiles; h[AH_KIND] = a.kv_len ? 2 : 1;
-        h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
+        const int32_t units = min(n_units, a.l.unit_cap), joins = min(n_merges, a.l.merge_cap);
+        // enough short ones that a wavefront each fills the chip: 2048 wavefronts run side by side
+        attn_header(a, units, (units - n_long) * a.kv_heads >= 2 * ATTN_TARGET ? min(n_long, units) : units, n_tiles, joins, joins);
     }
 }
 
@@ -382,27 +401,33 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
     constexpr int EACH = ATTN_DIRECT / 64;
     const int lane = threadIdx.x & 63, G = a.group;
     AttnItem it[EACH];
-    int32_t tiles[EACH], cost = 0;
+    int32_t tiles[EACH];
+    uint32_t cost = 0;
+    bool back = false;
 #pragma unroll
     for (int c = 0; c < EACH; ++c) {
         it[c] = AttnItem{0, 0, 0, 0, 0};
         tiles[c] = 0;
         if (c * 64 >= a.S) continue;
         const int32_t s = c * 64 + lane;
-        if (s < a.S) it[c] = attn_segment(a, s);
+        if (s < a.S) {
+            it[c] = attn_segment(a, s);
+            back = back || goes_back_at(a.seg_start, s, a.T);
+        }
         tiles[c] = (it[c].rows * G + ATTN_COLS - 1) / ATTN_COLS;
         if (tiles[c] > 0) {
             const int32_t low = min(it[c].key1, it[c].lim0 + (min(it[c].rows * G, ATTN_COLS) - 1) / G);
-            cost += (int32_t)(((int64_t)tiles[c] * (key_tiles(0, low) + key_tiles(0, it[c].key1) + 1)) / 2);      // all of them fit 31 bits: plan_of
+            cost += (uint32_t)(((int64_t)tiles[c] * (key_tiles(0, low) + key_tiles(0, it[c].key1) + 1)) / 2);      // all of them fit 31 bits: plan_of
         }
     }
+    AttnDirect r = {};
+    if (__any(back)) return r;
     int32_t range = INT32_MAX;
     if (a.can_split) {
         const int32_t n = min(a.S, 64);
-        cost = __builtin_amdgcn_readlane(wave_inclusive(cost, n), n - 1);
-        range = max(a.min_tiles, (int32_t)min(((uint64_t)(uint32_t)cost * (uint32_t)a.kv_heads + a.spread - 1) / (uint32_t)a.spread, (uint64_t)INT32_MAX));
+        cost = (uint32_t)__builtin_amdgcn_readlane(wave_inclusive((int32_t)cost, n), n - 1);
+        range = max(a.min_tiles, (int32_t)min(((uint64_t)cost * (uint32_t)a.kv_heads + a.spread - 1) / (uint32_t)a.spread, (uint64_t)INT32_MAX));
     }
-    AttnDirect r = {};
     int32_t before = 0, slots = 0, tiles_before = 0;
 #pragma unroll
     for (int c = 0; c < EACH; ++c) {
@@ -467,11 +492,7 @@ __device__ __forceinline__ AttnUnit attn_unit_of(const AttnScheduleArgs &a, cons
 __device__ __forceinline__ bool attn_direct_unit(const AttnScheduleArgs &a, int32_t unit, int32_t kv_head, bool ready, AttnUnit &u)
 {
     const AttnDirect d = attn_direct(a, unit);
-    if (!ready && unit == 0 && kv_head == 0 && threadIdx.x == 0) {
-        int32_t *h = a.l.header;
-        h[AH_UNITS] = d.units; h[AH_MERGES] = d.joined; h[AH_TILES] = d.tiles; h[AH_JOINS] = min(d.tiles, a.l.merge_cap); h[AH_KIND] = a.kv_len ? 2 : 1;
-        h[AH_GROUPS] = 0; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_MISMATCH] = 0; h[AH_KV_HEADS] = a.kv_heads;
-    }
+    if (!ready && unit == 0 && kv_head == 0 && threadIdx.x == 0) attn_header(a, d.units, d.units, d.tiles, d.joined, min(d.tiles, a.l.merge_cap));
     if (!d.found) return false;
     u = attn_unit_of(a, d);
     if (a.can_split && d.part == 0 && kv_head == 0 && threadIdx.x == 0) {

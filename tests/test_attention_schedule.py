@@ -28,7 +28,7 @@ def call(kind, dtype, heads, kv_heads, rows, prefill=None, kv=None, max_keys=0, 
     if start is None:
         start = np.concatenate([[0], np.cumsum(rows)])
     S, prefix = len(start) - 1, [] if prefix is None else prefix
-    words = [kind, dtype, int(start[-1]) if T is None else T, S, heads, kv_heads, len(prefix), max_keys, *start, *([0] * S if prefill is None else prefill)]
+    words = [kind, dtype, int(start[-1]) if T is None else T, S, heads, kv_heads, len(prefix) if kind % MALFORMED == CACHED else 0, max_keys, *start, *([0] * S if prefill is None else prefill)]
     if kind % MALFORMED == CACHED:
         words += [*kv, *(group_start if len(prefix) else []), *prefix]
     return " ".join(str(int(w)) for w in words)
@@ -108,3 +108,63 @@ def test_batches_over_very_long_tables(driver):
     got = answers(driver, calls)
     assert {g[0] for g in got[5:]} == {0, 1}
     assert all(units <= grid for _, _, _, units, grid, _ in got)
+
+
+def goes_back(start, T):
+    at = np.clip(start, 0, T)
+    return bool((np.diff(at) < 0).any())
+
+
+def test_offsets_that_go_back_leave_nothing_to_run(driver):
+    """Segments that overlap, in both forms of the schedule, with keys to cut and without: no unit, no entry of the join, whatever the sums over them would be.  Offsets outside the batch
+    that do not go back within it are ordinary."""
+    T, big = 1000, 1 << 24
+    tables = [[0, 1000, 0, 1000], [0, 500, 200, 900, -4, 1000], [5, 5, 4, 1000, 1000], [0, 1000] * 2000 + [0], [0, 2 ** 31 - 1, -2 ** 31, 1000]]
+    calls = []
+    for start in tables:
+        S = len(start) - 1
+        for dtype in (BF16, F32):
+            calls.append(call(MALFORMED + PROMPT, dtype, 4, 2, None, [1000] * S, start=start, T=T))
+            for most in (64, 320, 100_000):
+                calls.append(call(MALFORMED + CACHED, dtype, 4, 2, None, None, [most] * S, most, start=start, T=T))
+                calls.append(call(MALFORMED + CACHED, dtype, 4, 2, None, None, [most] * S, most, [0, S // 2, S], [most, 64], start=start, T=T))
+    # rows and tiles of all segments together past 31 bits
+    calls.append(call(MALFORMED + CACHED, BF16, 8, 8, None, None, [64] * 400, 64, [0, 400], [64], start=[0, big] * 200 + [0], T=big))
+    # groups that overlap
+    for gstart in ([0, 3, 1, 4], [2, 1], [4, 0, 4]):
+        calls.append(call(MALFORMED + CACHED, BF16, 4, 2, [1, 2, 3, 1], None, [300] * 4, 320, gstart, [100] * (len(gstart) - 1)))
+    for _, _, _, units, _, joins in answers(driver, calls):
+        assert units == 0 and joins == 0
+    outside = [-7, 0, 10, 900, 900, 5000]
+    got = answers(driver, [call(MALFORMED + PROMPT, BF16, 4, 2, None, [100] * 5, start=outside, T=T),
+                           call(MALFORMED + CACHED, BF16, 4, 2, None, None, [100] * 5, 320, [-3, 2, 9], [100, 64], start=outside, T=T)])
+    assert all(g[3] > 0 for g in got)
+
+
+@pytest.mark.parametrize("seed", range(2))
+def test_random_tables_stay_within_the_lists(driver, seed):
+    """Anything in any table: no index leaves its list, and the join takes no entry that nobody wrote."""
+    rng = np.random.Generator(np.random.PCG64(100 + seed))
+    calls, back = [], []
+
+    def wild(n, most):
+        v = rng.integers(-3, most + 4, size=n)
+        odd = rng.random(n) < 0.1
+        v[odd] = rng.choice([-2 ** 31, -1, 0, 2 ** 30, 2 ** 31 - 1], size=int(odd.sum()))
+        return v
+    for _ in range(60):
+        kv_heads = int(rng.choice([1, 2, 8]))
+        S, T = int(rng.choice([1, 3, 20, 270])), int(rng.choice([1, 60, 500, 4000]))
+        start = wild(S + 1, T)
+        if rng.random() < 0.5:
+            start = np.sort(start)
+        max_keys = 16 * int(rng.choice([1, 9, 20, 400]))
+        g = int(rng.choice([0, 0, 1, 4]))
+        gstart = wild(g + 1, S) if rng.random() < 0.4 else np.sort(wild(g + 1, S))
+        kind = PROMPT if rng.random() < 0.3 else CACHED
+        calls.append(call(MALFORMED + kind, int(rng.integers(0, 2)), 4 * kv_heads, kv_heads, None, wild(S, 40), wild(S, max_keys), max_keys,
+                          gstart, wild(g, max_keys) if kind == CACHED else None, start=start, T=T))
+        back.append(goes_back(start, T) or (kind == CACHED and g > 0 and goes_back(gstart, S)))
+    for got, b in zip(answers(driver, calls), back):
+        assert got[3] <= got[4] and got[5] >= 0
+        assert not b or got[3] == 0

@@ -88,3 +88,30 @@ def test_a_wide_chunk_over_very_many_tokens():
     for t in (0, 7, 8, 15, 2047, 4096, 8175, 8176, 8183):
         o, bound = ref.attend_row(q[t].cpu().double().view(H, D), K[:, : kv - (T - 1 - t)], V[:, : kv - (T - 1 - t)], 0.125, q.dtype)
         assert ((out[t].cpu().double().view(H, D) - o).abs() <= bound).all(), t
+
+
+@pytest.mark.parametrize("groups", [0, 2])
+@pytest.mark.parametrize("S,most", [(3, 320), (5, 4000), (300, 64), (300, 1000)])
+def test_segments_that_overlap_leave_the_output_alone(S, most, groups):
+    """Offsets that go back, over tables long enough to be cut and joined and over short ones, searched for and listed: nothing is written, and the next call on the workspace is as ever."""
+    print(f"\n[case] overlapping segments S={S} most={most} groups={groups}", flush=True)
+    H, Hkv, D, page, T = 4, 2, 64, 16, 1000
+    gen = torch.Generator(device="cuda").manual_seed(S)
+    kc, vc = (normal(gen, 40, Hkv, page, D).bfloat16() for _ in "kv")
+    qkv = normal(gen, T, (H + 2 * Hkv) * D).bfloat16()
+    q, k, v = qkv[:, :H * D], qkv[:, H * D:(H + Hkv) * D], qkv[:, (H + Hkv) * D:]
+    start = [0, T] * (S // 2) + [0, 900][: S + 1 - 2 * (S // 2)]
+    assert len(start) == S + 1
+    table = torch.randint(0, 40, (S, -(-most // page)), generator=gen, device="cuda", dtype=torch.int32)
+    gs, gp = (i32([0, S // 2, S]), i32([64, 64])) if groups else (None, None)
+    ws = preft.new_attention_workspace(T, S, H, Hkv, D, groups)
+    ws.fill_(0x9d)                                             # no sensible entry of any list
+    out = torch.full((T, H * D), 7.5, dtype=torch.bfloat16, device="cuda")
+    kv = i32([most] * S)
+    preft.preft_cached_attention(out, q, i32(start), None, kv, kc, vc, table, gs, gp, H, 0.1, 0, ws)
+    preft.preft_prompt_attention(out, q, k, v, i32(start), i32([T] * S), H, Hkv, 0.1, 0, preft.new_attention_workspace(T, S, H, Hkv, D).fill_(0x9d))
+    torch.cuda.synchronize()
+    assert bool((out == 7.5).all())
+    good = np.linspace(0, T, S + 1).astype(int)
+    preft.preft_cached_attention(out, q, i32(good), None, kv, kc, vc, table, gs, gp, H, 0.1, 0, ws)
+    assert not bool((out == 7.5).all(1).any())
