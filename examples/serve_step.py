@@ -4,7 +4,8 @@ Requests of three adapters are served.  Every adapter has a system prompt that a
 adapter edits, are computed once and shared as pages.  A step is: slots for its rows (preft_kv_plan); in every layer the q, k and v projections with the
 adapters' LoRA on prompt rows (preft_lora_apply_packed), the rows' keys and values to their slots (preft_kv_store), attention, and the o projection with its LoRA.
 The first step prefills the system prompts (whole prompts: preft_prompt_attention); in the second every request sends the rest of its prompt, and in the others one token
-(preft_cached_attention, grouped by adapter, so that a system prompt's keys are read once for all its requests).
+(preft_cached_attention, grouped by adapter, so that a system prompt's keys are read once for all its requests).  In the fourth two requests without a system prompt
+join: a mixed step, whose layers make both calls on one workspace.
 
     python examples/serve_step.py            runs the steps and compares every row with the same model in 64 bits
 
@@ -71,7 +72,9 @@ class Engine:
         attn_ws = preft.new_attention_workspace(T, S, HEADS, KV_HEADS, DIM, len(prefix or []), device=dev)
         group_start = None if prefix is None else i32(groups, dev)
         group_prefix = None if prefix is None else i32(prefix, dev)
-        whole = all(c == 0 for c in context) and all(prompt)
+        # whole prompts by their own keys and values, all other rows over the pages
+        first = [n if p and c == 0 else 0 for n, p, c in zip(lengths, prompt, context)]
+        whole, rest = i32(first, dev), sum(lengths) > sum(first)
         for layer, (w, pools, (k_cache, v_cache)) in enumerate(zip(self.model.w, self.model.pools, self.caches)):
             mode = preft.PREFT_PREFILL_ONLY | (preft.PREFT_SCHEDULE_READY if layer else 0)
             ready = preft.PREFT_SCHEDULE_READY if layer else 0
@@ -81,10 +84,10 @@ class Engine:
                                           RANK, LORA_SCALE, mode, adapter_ws)
             preft.preft_kv_store(k_cache, v_cache, k, v, slot_map)
             out = torch.empty(T, WIDTH, dtype=self.dtype, device=dev)
-            if whole:
-                preft.preft_prompt_attention(out, q, k, v, seg_start, prefill, HEADS, KV_HEADS, ATTN_SCALE, ready, attn_ws)
-            else:                                           # every row, over the pages
-                preft.preft_cached_attention(out, q, seg_start, None, kv_len, k_cache, v_cache, tables, group_start, group_prefix, HEADS, ATTN_SCALE,
+            if any(first):
+                preft.preft_prompt_attention(out, q, k, v, seg_start, whole, HEADS, KV_HEADS, ATTN_SCALE, ready, attn_ws)
+            if rest:
+                preft.preft_cached_attention(out, q, seg_start, whole, kv_len, k_cache, v_cache, tables, group_start, group_prefix, HEADS, ATTN_SCALE,
                                              ready, attn_ws)
             y = out @ w["o"]
             preft.preft_lora_apply(y, out, seg_start, seg_adapter, prefill, *pools["o"], RANK, LORA_SCALE, preft.PREFT_PREFILL_ONLY | preft.PREFT_SCHEDULE_READY,
@@ -133,10 +136,24 @@ def main(dtype=torch.float32, device="cuda", new_tokens=4, requests=9, seed=1):
     context = [SYSTEM[a] for a in adapter]
     got = [engine.step(torch.cat(tokens), own, [True] * requests, adapter, context, tables, groups, SYSTEM).split(own)]
     context = [c + n for c, n in zip(context, own)]
+    late, joined = [(0, embeddings(37 + new_tokens)), (2, embeddings(70 + new_tokens))], [37, 70]       # adapter and tokens; how many are the prompt
+    got_late = []
     for t in range(new_tokens):
-        x = torch.cat([m[t:t + 1] for m in more])
-        got.append(engine.step(x, [1] * requests, [False] * requests, adapter, context, tables, groups, SYSTEM).split(1))
-        context = [c + 1 for c in context]
+        rows = [m[t:t + 1] for m in more]
+        lengths, prompt = [1] * requests, [False] * requests
+        if t == 1:                                          # they stand after the groups, in none
+            tables = torch.cat([tables, torch.full((len(late), engine.max_pages), -1, dtype=torch.int32, device=device)])
+            adapter, context = adapter + [a for a, _ in late], context + [0] * len(late)
+        if t >= 1:
+            at = context[requests:]
+            lengths += [n if t == 1 else 1 for n in joined]
+            prompt += [t == 1] * len(late)
+            rows += [x[c:c + n] for (_, x), c, n in zip(late, at, lengths[requests:])]
+        parts = engine.step(torch.cat(rows), lengths, prompt, adapter, context, tables, groups, SYSTEM).split(lengths)
+        got.append(parts[:requests])
+        if t >= 1:
+            got_late.append(parts[requests:])
+        context = [c + n for c, n in zip(context, lengths)]
     worst = 0.0
 
     def compare(a, b):
@@ -147,6 +164,9 @@ def main(dtype=torch.float32, device="cuda", new_tokens=4, requests=9, seed=1):
         all_ = torch.cat([system[adapter[r]], tokens[r], more[r]])
         want = exact(model, all_, SYSTEM[adapter[r]] + own[r], adapter[r])[SYSTEM[adapter[r]]:]
         worst = max(worst, compare(torch.cat([step[r] for step in got]), want))
+    for r, ((a, x), n) in enumerate(zip(late, joined)):
+        rows = torch.cat([step[r] for step in got_late])
+        worst = max(worst, compare(rows, exact(model, x[:len(rows)], n, a)))
     return worst
 
 

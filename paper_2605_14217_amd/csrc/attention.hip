@@ -60,7 +60,7 @@ extern "C" {
 size_t preft_attention_workspace_bytes(int32_t T, int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_groups)
 {
     if (T < 0 || S < 0 || n_groups < 0 || check_heads(n_heads, n_kv_heads, head_dim, PREFT_F32) != PREFT_OK || !sizes_fit(T, S, n_heads, n_groups)) return 0;
-    return layout_of(T, S, n_heads, n_kv_heads, head_dim, n_groups).bytes;
+    return cached_layout(T, S, n_heads, n_kv_heads, head_dim, n_groups).end;
 }
 
 int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, int32_t T,
@@ -76,8 +76,8 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
         (rc = check_rows(k, ldk, wk, dtype)) != PREFT_OK || (rc = check_rows(v, ldv, wk, dtype)) != PREFT_OK) return rc;
     if (rows_meet(out, ldo, wq, q, ldq, wq, T, dtype) || rows_meet(out, ldo, wq, k, ldk, wk, T, dtype) || rows_meet(out, ldo, wq, v, ldv, wk, T, dtype))
         return PREFT_EINVAL;
-    const Layout l = layout_of(T, S, n_heads, n_kv_heads, head_dim, 0);
-    if (!workspace || !aligned_workspace(workspace) || workspace_bytes < l.bytes) return PREFT_EWORKSPACE;
+    if (!workspace || !aligned_workspace(workspace) || workspace_bytes < cached_layout(T, S, n_heads, n_kv_heads, head_dim, 0).end) return PREFT_EWORKSPACE;
+    const Layout l = prompt_layout(T, S, n_heads, n_kv_heads, head_dim);
     const int64_t e = elem_bytes(dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     AttnArgs a = {};
@@ -116,8 +116,8 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     const int64_t cache = (int64_t)n_pages * page_size * wk * e;
     const Span o = {out, ((int64_t)(T - 1) * ldo + wq) * e};
     if (keys && (o.meets({k_cache, cache}) || o.meets({v_cache, cache}))) return PREFT_EINVAL;
-    const Layout l = layout_of(T, S, n_heads, n_kv_heads, head_dim, n_groups);
-    if (!workspace || !aligned_workspace(workspace) || workspace_bytes < l.bytes) return PREFT_EWORKSPACE;
+    const Layout l = cached_layout(T, S, n_heads, n_kv_heads, head_dim, n_groups);
+    if (!workspace || !aligned_workspace(workspace) || workspace_bytes < l.end) return PREFT_EWORKSPACE;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     AttnArgs a = {};
     a.q = q; a.k = k_cache; a.v = v_cache; a.out = out; a.ldq = ldq * e; a.ldo = ldo * e;

@@ -12,12 +12,16 @@ namespace preft {
 //                  kv_heads / TARGET.  That estimate, from the first and the last tile of a segment, is short by up to two a tile of a causal prompt (list), and
 //                  at least half of what counting every tile of a segment like its last gives (direct);
 //   part columns   a tile that is cut has at most twice n / range parts of at most 128 columns; rows of groups have one of their own and their group's.
+//
+// The workspace holds, behind the header that preft_schedule_counts reads, a header, lists and parts of each kind of call: in a mixed step both kinds find their own
+// schedule again in every layer.  The prompts' come first, since their size does not depend on the groups of the other call.
 struct Layout {
     int32_t tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
-    size_t units, merges, group_rows, tiles, rows_before, group_of, group_list, group_slot, group_low, part_ml, part_o, bytes;
+    size_t header, units, merges, group_rows, tiles, rows_before, group_of, group_list, group_slot, group_low, part_ml, part_o, end;
 };
 
-inline Layout layout_of(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
+// of one kind of call, from byte `at` on; parts: whether it has any
+inline Layout layout_from(size_t at, bool parts, int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
 {
     Layout l;
     const int64_t G = heads / kv_heads, cols = T * G;
@@ -27,9 +31,9 @@ inline Layout layout_of(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, i
     l.unit_cap = (int32_t)(3 * tiles + 2 * ((ATTN_TARGET + kv_heads - 1) / kv_heads) + 2);
     l.merge_cap = (int32_t)seg_tiles;
     l.group_row_cap = groups > 0 ? (int32_t)(T < ATTN_GROUP_ROWS ? T : ATTN_GROUP_ROWS) : 0;
-    l.slot_cap = (int32_t)(4 * ATTN_TARGET * (cols < ATTN_COLS ? cols : ATTN_COLS) + 2 * l.group_row_cap * heads);
-    size_t at = HEADER_INTS * 4;
+    l.slot_cap = parts ? (int32_t)(4 * ATTN_TARGET * (cols < ATTN_COLS ? cols : ATTN_COLS) + 2 * l.group_row_cap * heads) : 0;
     auto take = [&](size_t bytes) { const size_t p = at; at = (at + bytes + 63) & ~(size_t)63; return p; };
+    l.header = take(HEADER_INTS * 4);
     l.units = take((size_t)l.unit_cap * sizeof(AttnUnit));
     l.merges = take((size_t)l.merge_cap * sizeof(AttnMerge));
     l.group_rows = take((size_t)l.group_row_cap * sizeof(int2));
@@ -41,15 +45,33 @@ inline Layout layout_of(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, i
     l.group_low = take((size_t)groups * 4);
     l.part_ml = take((size_t)l.slot_cap * sizeof(float2));
     l.part_o = take((size_t)l.slot_cap * D * 4);
-    l.bytes = at;
+    l.end = at;
     return l;
+}
+
+// Prompts are cut only where they are long on average and their tiles do not fill half the chip: a prompt has tiles by its rows as it has keys, and a
+// merge launch with nothing to join costs 4 us of the 10 that a batch of chat-length prompts takes (8 heads over 2 of 128: 4000 rows 66 us, uncut 74; 6000 rows
+// 115 uncut, cut 132; 32 heads over 8, 1200 rows: 30 uncut, cut 75).
+inline bool prompts_are_cut(int64_t tiles, int64_t kv_heads, int64_t T, int64_t S) { return tiles * kv_heads <= ATTN_TARGET / 2 && T >= 512 * S; }
+
+inline Layout prompt_layout(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D)
+{
+    const Layout l = layout_from(HEADER_INTS * 4, false, T, S, heads, kv_heads, D, 0);
+    return prompts_are_cut(l.tile_cap, kv_heads, T, S) ? layout_from(HEADER_INTS * 4, true, T, S, heads, kv_heads, D, 0) : l;
+}
+
+// ends where the workspace does
+inline Layout cached_layout(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
+{
+    return layout_from(prompt_layout(T, S, heads, kv_heads, D).end, true, T, S, heads, kv_heads, D, groups);
 }
 
 inline AttnLists lists_of(const Layout &l, void *workspace)
 {
     char *p = (char *)workspace;
     AttnLists r;
-    r.header = (int32_t *)p;
+    r.report = (int32_t *)p;
+    r.header = (int32_t *)(p + l.header);
     r.units = (AttnUnit *)(p + l.units);
     r.merges = (AttnMerge *)(p + l.merges);
     r.group_rows = (int2 *)(p + l.group_rows);
@@ -85,13 +107,10 @@ inline void spread(AttnScheduleArgs &s, int dtype)
 }
 
 // A prompt call of T rows: what its schedule goes by.
-// Cut only where the prompts are long on average and their tiles do not fill half the chip: a prompt has tiles by its rows as it has keys, and a
-// merge launch with nothing to join costs 4 us of the 10 that a batch of chat-length prompts takes (8 heads over 2 of 128: 4000 rows 66 us, uncut 74; 6000 rows
-// 115 uncut, cut 132; 32 heads over 8, 1200 rows: 30 uncut, cut 75).
 inline void prompt_rules(AttnScheduleArgs &s, int dtype)
 {
     s.max_keys = s.T;
-    s.can_split = (int64_t)s.l.tile_cap * s.kv_heads <= ATTN_TARGET / 2 && s.T >= 512 * (int64_t)s.S;
+    s.can_split = prompts_are_cut(s.l.tile_cap, s.kv_heads, s.T, s.S);
     spread(s, dtype);
     s.min_tiles = s.min_wide;
 }

@@ -37,7 +37,8 @@ struct AttnMerge {
 };
 
 struct AttnLists {
-    int32_t   *header;     // HEADER_INTS ints, laid out as the adapter schedule's where they mean the same
+    int32_t   *report;     // what preft_schedule_counts reads: units, joined tiles and tiles of the last schedule, and the mark of refused calls
+    int32_t   *header;     // HEADER_INTS ints of this kind of call
     AttnUnit  *units;
     AttnMerge *merges;
     int2      *group_rows; // {batch row, keys it sees}
@@ -52,7 +53,12 @@ struct AttnLists {
     int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
 };
 
-constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_MISMATCH = 8, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11;      // AH_SHORT: first unit that is one wavefront's; AH_JOINS: entries of merges
+constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11;      // AH_SHORT: first unit that is one wavefront's; AH_JOINS: entries of merges
+
+// A call that found another batch's schedule marks the report with its kind; the next schedule of that kind takes the mark away.  (Anything else that stands there is what
+// the memory held before.)
+constexpr int32_t ATTN_MARK = 0x5a7e0000;
+__device__ __forceinline__ int32_t attn_marks(const int32_t *report) { return (report[HDR_MISMATCH] & ~3) == ATTN_MARK ? report[HDR_MISMATCH] & 3 : 0; }
 
 struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
@@ -108,9 +114,11 @@ __device__ __forceinline__ int32_t part_begin(int32_t n, int32_t parts, int32_t 
 // what a later call and the join go by; joined: tiles of more than one part
 __device__ __forceinline__ void attn_header(const AttnScheduleArgs &a, int32_t units, int32_t alone, int32_t tiles, int32_t joined, int32_t joins)
 {
-    int32_t *h = a.l.header;
-    h[AH_UNITS] = units; h[AH_SHORT] = alone; h[AH_TILES] = tiles; h[AH_MERGES] = joined; h[AH_JOINS] = joins; h[AH_MISMATCH] = 0;
-    h[AH_KIND] = a.kv_len ? 2 : 1; h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_KV_HEADS] = a.kv_heads;
+    int32_t *h = a.l.header, *r = a.l.report;
+    const int32_t kind = a.kv_len ? 2 : 1, marks = attn_marks(r) & ~kind;
+    r[AH_UNITS] = units; r[AH_MERGES] = joined; r[AH_TILES] = tiles; r[HDR_MISMATCH] = marks != 0 ? ATTN_MARK | marks : 0;
+    h[AH_UNITS] = units; h[AH_SHORT] = alone; h[AH_TILES] = tiles; h[AH_MERGES] = joined; h[AH_JOINS] = joins;
+    h[AH_KIND] = kind; h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_KV_HEADS] = a.kv_heads;
 }
 
 struct AttnGroup { int32_t begin, end, rows, prefix; };

@@ -28,14 +28,14 @@ static std::string check(int kind, int dtype, int32_t T, int32_t S, int32_t head
                          const std::vector<int32_t> &prefill, const std::vector<int32_t> &kv, const std::vector<int32_t> &gstart, const std::vector<int32_t> &gprefix,
                          bool malformed, std::string &facts)
 {
-    const Layout l = layout_of(T, S, heads, kv_heads, 64, groups);
+    const Layout l = kind == 1 ? prompt_layout(T, S, heads, kv_heads, 64) : cached_layout(T, S, heads, kv_heads, 64, groups);
     AttnLists x = lists_of(l, reinterpret_cast<void *>(4096));        // for its capacities
-    Block<int32_t> header(HEADER_INTS), tiles(S + groups + 1), rows_before(S + 1), group_of(S), group_list(groups), group_slot(groups), group_low(groups);
+    Block<int32_t> report(HEADER_INTS), header(HEADER_INTS), tiles(S + groups + 1), rows_before(S + 1), group_of(S), group_list(groups), group_slot(groups), group_low(groups);
     Block<AttnUnit> units(l.unit_cap);
     Block<AttnMerge> merges(l.merge_cap);
     Block<int2> group_rows(l.group_row_cap);
     x.header = header.p(); x.units = units.p(); x.merges = merges.p(); x.group_rows = group_rows.p(); x.tiles = tiles.p(); x.rows_before = rows_before.p();
-    x.group_of = group_of.p(); x.group_list = group_list.p(); x.group_slot = group_slot.p(); x.group_low = group_low.p(); x.part_o = nullptr; x.part_ml = nullptr;
+    x.group_of = group_of.p(); x.group_list = group_list.p(); x.group_slot = group_slot.p(); x.group_low = group_low.p(); x.report = report.p(); x.part_o = nullptr; x.part_ml = nullptr;
     AttnScheduleArgs s = {};
     s.seg_start = start.data(); s.seg_prefill_len = prefill.data(); s.S = S; s.T = T; s.heads = heads; s.kv_heads = kv_heads; s.group = heads / kv_heads; s.l = x;
     if (kind == 1) {

@@ -115,3 +115,91 @@ def test_segments_that_overlap_leave_the_output_alone(S, most, groups):
     good = np.linspace(0, T, S + 1).astype(int)
     preft.preft_cached_attention(out, q, i32(good), None, kv, kc, vc, table, gs, gp, H, 0.1, 0, ws)
     assert not bool((out == 7.5).all(1).any())
+
+
+def mixed_step(S, seed, groups, dtype=torch.bfloat16):
+    """Whole prompts and decode rows of one batch, layer after layer with other values: (tables of the step, layers of (q, k, v, caches))."""
+    H, Hkv, D, page = 8, 2, 64, 16
+    rng, gen = np.random.Generator(np.random.PCG64(seed)), torch.Generator(device="cuda").manual_seed(seed)
+    prompt = rng.random(S) < 0.4
+    prompt[:4] = False                                         # the group's
+    n = np.where(prompt, rng.integers(1, 90, size=S), rng.integers(1, 3, size=S))
+    kv = np.where(prompt, n, rng.integers(130, 400, size=S))
+    pages = 26
+    table = rng.permutation(S * pages).reshape(S, pages)
+    table[1:4, :8] = table[0, :8]
+    start = np.concatenate([[0], np.cumsum(n)])
+    T = int(start[-1])
+    layers = [tuple((normal(gen, *shape) * f).to(dtype) for shape, f in (((T, H * D), 2.0), ((T, Hkv * D), 1.0), ((T, Hkv * D), 1.0),
+                                                                         ((S * pages, Hkv, page, D), 1.0), ((S * pages, Hkv, page, D), 1.0))) for _ in range(3)]
+    return dict(H=H, Hkv=Hkv, D=D, S=S, T=T, start=start, prefill=np.where(prompt, n, 0), kv=kv, table=table, dev=i32(table), seg=i32(start),
+                groups=(i32([0, 4]), i32([128])) if groups else (None, None), n_groups=1 if groups else 0), layers
+
+
+@pytest.mark.parametrize("groups", [False, True])
+@pytest.mark.parametrize("S", [9, 300])
+def test_both_kinds_of_a_mixed_step_keep_their_schedules_in_one_workspace(S, groups):
+    """Every layer makes both calls; the first builds both schedules, the others find them again."""
+    print(f"\n[case] mixed step S={S} groups={groups}", flush=True)
+    s, layers = mixed_step(S, S, groups)
+    ws = preft.new_attention_workspace(s["T"], S, s["H"], s["Hkv"], s["D"], s["n_groups"])
+    ws.fill_(0x9d)
+    prefill, kv = i32(s["prefill"]), i32(s["kv"])
+    for i, (q, k, v, kc, vc) in enumerate(layers):
+        ready = preft.PREFT_SCHEDULE_READY if i else 0
+        out = torch.full_like(q, 7.5)
+        before = out.cpu()
+        preft.preft_prompt_attention(out, q, k, v, s["seg"], prefill, s["H"], s["Hkv"], 0.125, ready, ws)
+        preft.preft_cached_attention(out, q, s["seg"], prefill, kv, kc, vc, s["dev"], *s["groups"], s["H"], 0.125, ready, ws)
+        preft.preft_schedule_counts(ws)                        # raises where a call was refused
+        if S > 100 and i != 2:                                 # the last layer alone: 300 requests take the reference a while
+            assert not bool((out == 7.5).all(1).any())
+            continue
+        want = ref.prompt(q.cpu(), k.cpu(), v.cpu(), s["start"], s["prefill"], s["H"], s["Hkv"], 0.125)
+        want.update(ref.cached(q.cpu(), s["start"], s["prefill"], s["kv"], kc.cpu(), vc.cpu(), s["table"], s["H"], 0.125))
+        assert len(want) == s["T"]
+        print(f"  layer {i}: {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+
+
+def test_a_refused_call_of_either_kind_is_reported_until_its_next_schedule():
+    print("\n[case] refused calls", flush=True)
+    s, layers = mixed_step(9, 1, False)
+    q, k, v, kc, vc = layers[0]
+    T, H, Hkv = s["T"], s["H"], s["Hkv"]
+    ws = preft.new_attention_workspace(T, 9, H, Hkv, s["D"])
+    ws.fill_(0x9d)
+    out, prefill, kv = torch.full_like(q, 7.5), i32(s["prefill"]), i32(s["kv"])
+
+    def prompt(mode, rows=T):
+        preft.preft_prompt_attention(out[:rows], q[:rows], k[:rows], v[:rows], s["seg"], prefill, H, Hkv, 0.125, mode, ws)
+
+    def cached(mode, rows=T):
+        preft.preft_cached_attention(out[:rows], q[:rows], s["seg"], prefill, kv, kc, vc, s["dev"], None, None, H, 0.125, mode, ws)
+
+    def refused():
+        try:
+            preft.preft_schedule_counts(ws)
+        except preft.PreftError as e:
+            assert e.code == preft.PREFT_ESCHEDULE
+            return True
+        return False
+    READY = preft.PREFT_SCHEDULE_READY
+    prompt(0)
+    assert not refused()
+    out.fill_(7.5)
+    cached(READY)                                              # no schedule of this kind was ever built
+    assert refused() and bool((out == 7.5).all())
+    prompt(READY)
+    assert refused() and not bool((out == 7.5).all())
+    prompt(0)                                                  # the other kind's mark stays
+    assert refused()
+    cached(0)
+    assert not refused()
+    out.fill_(7.5)
+    prompt(READY, T - 1)
+    cached(READY, T - 1)
+    assert refused() and bool((out == 7.5).all())
+    cached(0)
+    assert refused()
+    prompt(0)
+    assert not refused()
