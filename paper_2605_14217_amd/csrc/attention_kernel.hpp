@@ -657,11 +657,10 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
     }
 }
 
+// false: the call names another batch than the schedule's, and leaves a mark
 __device__ __forceinline__ bool attn_schedule_is(const AttnArgs &a, int kind)
 {
-    const PREFT_CONST int32_t *h = as_const(a.l.header);
-    const bool same = h[AH_KIND] == kind && h[AH_GROUPS] == a.n_groups && h[AH_T] == a.T && h[AH_S] == a.S && h[AH_HEADS] == a.heads &&
-                      h[AH_KV_HEADS] == a.kv_heads;
+    const bool same = attn_schedule_fits(a.s);
     if (!same && threadIdx.x == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) a.l.report[HDR_MISMATCH] = ATTN_MARK | kind | attn_marks(a.l.report);
     return same;
 }

@@ -110,6 +110,7 @@ inline void spread(AttnScheduleArgs &s, int dtype)
 inline void prompt_rules(AttnScheduleArgs &s, int dtype)
 {
     s.max_keys = s.T;
+    s.dtype = dtype;
     s.can_split = prompts_are_cut(s.l.tile_cap, s.kv_heads, s.T, s.S);
     spread(s, dtype);
     s.min_tiles = s.min_wide;
@@ -119,6 +120,7 @@ inline void prompt_rules(AttnScheduleArgs &s, int dtype)
 inline void cached_rules(AttnScheduleArgs &s, int dtype, int64_t most_keys)
 {
     s.max_keys = (int32_t)(most_keys < (1 << 30) ? most_keys : (1 << 30));
+    s.dtype = dtype;
     s.can_split = 1;
     spread(s, dtype);
 }

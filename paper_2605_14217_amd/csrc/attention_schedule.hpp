@@ -53,7 +53,7 @@ struct AttnLists {
     int32_t    tile_cap, unit_cap, merge_cap, group_row_cap, slot_cap;
 };
 
-constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11;      // AH_SHORT: first unit that is one wavefront's; AH_JOINS: entries of merges
+constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_DTYPE = 8, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11, AH_KEYS = 12;      // AH_SHORT: first unit that is one wavefront's; AH_JOINS: entries of merges
 
 // A call that found another batch's schedule marks the report with its kind; the next schedule of that kind takes the mark away.  (Anything else that stands there is what
 // the memory held before.)
@@ -64,7 +64,7 @@ struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
     const int32_t *kv_len;                                 // null: packed whole prompts
     const int32_t *group_start, *group_prefix;
-    int32_t S, T, n_groups, heads, kv_heads, group, max_keys, can_split, min_tiles, min_wide, spread;    // group: heads / kv_heads; spread: workgroups that a range's length is meant for
+    int32_t S, T, n_groups, heads, kv_heads, group, max_keys, dtype, can_split, min_tiles, min_wide, spread;    // group: heads / kv_heads; spread: workgroups that a range's length is meant for
     AttnLists l;
 };
 
@@ -118,7 +118,16 @@ __device__ __forceinline__ void attn_header(const AttnScheduleArgs &a, int32_t u
     const int32_t kind = a.kv_len ? 2 : 1, marks = attn_marks(r) & ~kind;
     r[AH_UNITS] = units; r[AH_MERGES] = joined; r[AH_TILES] = tiles; r[HDR_MISMATCH] = marks != 0 ? ATTN_MARK | marks : 0;
     h[AH_UNITS] = units; h[AH_SHORT] = alone; h[AH_TILES] = tiles; h[AH_MERGES] = joined; h[AH_JOINS] = joins;
-    h[AH_KIND] = kind; h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_KV_HEADS] = a.kv_heads;
+    h[AH_KIND] = kind; h[AH_DTYPE] = a.dtype; h[AH_KEYS] = a.max_keys; h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_KV_HEADS] = a.kv_heads;
+}
+
+// Whether the header's schedule is that of a call with these sizes.  The type and the room of the block table are among them: ranges, and with them the grid and
+// whether parts are joined, go by both.  Compared as a whole: behind && it would be a chain of trips to memory.
+__device__ __forceinline__ bool attn_schedule_fits(const AttnScheduleArgs &a)
+{
+    const PREFT_CONST int32_t *h = as_const(a.l.header);
+    return ((h[AH_KIND] ^ (a.kv_len ? 2 : 1)) | (h[AH_GROUPS] ^ a.n_groups) | (h[AH_T] ^ a.T) | (h[AH_S] ^ a.S) | (h[AH_HEADS] ^ a.heads) | (h[AH_DTYPE] ^ a.dtype) |
+            (h[AH_KV_HEADS] ^ a.kv_heads) | (h[AH_KEYS] ^ a.max_keys)) == 0;
 }
 
 struct AttnGroup { int32_t begin, end, rows, prefix; };

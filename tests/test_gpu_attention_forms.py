@@ -203,3 +203,37 @@ def test_a_refused_call_of_either_kind_is_reported_until_its_next_schedule():
     assert refused()
     prompt(0)
     assert not refused()
+
+
+@pytest.mark.parametrize("S,H,Hkv", [(300, 32, 8), (300, 4, 2), (20, 8, 2)])
+@pytest.mark.parametrize("first", ["bf16", "f32"])
+def test_a_schedule_serves_calls_of_its_type_and_its_tables_room(S, H, Hkv, first):
+    """How keys are cut goes by the type and by how long the tables may be: a call with others is refused, not run on lists that do not fit its grid."""
+    print(f"\n[case] other type, narrower table, S={S} {H}/{Hkv} {first}", flush=True)
+    D, page, gen = 64, 16, torch.Generator(device="cuda").manual_seed(S)
+    types = {"bf16": torch.bfloat16, "f32": torch.float32}
+    other = "f32" if first == "bf16" else "bf16"
+    kc, vc = (normal(gen, 500, Hkv, page, D) for _ in "kv")
+    q = normal(gen, S, H * D)
+    table = torch.randint(0, 500, (S, 12), generator=gen, device="cuda", dtype=torch.int32)
+    start, kv = i32(np.arange(S + 1)), i32([192 - s % 90 for s in range(S)])
+    ws = preft.new_attention_workspace(S, S, H, Hkv, D)
+    ws.fill_(0x9d)
+
+    def run(dtype, mode, pages=12):
+        t = types[dtype]
+        out = torch.full((S, H * D), 7.5, dtype=t, device="cuda")
+        preft.preft_cached_attention(out, q.to(t), start, None, kv, kc.to(t), vc.to(t), table[:, :pages], None, None, H, 0.125, mode, ws)
+        return out
+    READY = preft.PREFT_SCHEDULE_READY
+    built = run(first, 0)
+    assert torch.equal(built, run(first, READY)) and not bool((built == 7.5).any(1).all())
+    preft.preft_schedule_counts(ws)
+    for dtype, pages in ((other, 12), (first, 11), (first, 6)):
+        run(first, 0)
+        preft.preft_schedule_counts(ws)
+        assert bool((run(dtype, READY, pages) == 7.5).all())
+        with pytest.raises(preft.PreftError) as e:
+            preft.preft_schedule_counts(ws)
+        assert e.value.code == preft.PREFT_ESCHEDULE
+    assert torch.equal(built, run(first, READY))
