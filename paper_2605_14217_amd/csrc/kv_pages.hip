@@ -36,7 +36,7 @@ __device__ __forceinline__ PlanRequest plan_request(const PlanArgs &a, int32_t s
 }
 
 // sum over the workgroup, for every thread; `lds`: one place a wavefront
-__device__ __forceinline__ int32_t block_sum(int32_t v, int32_t *lds)
+__device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t *lds)
 {
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
 #pragma unroll
@@ -50,26 +50,28 @@ __device__ __forceinline__ int32_t block_sum(int32_t v, int32_t *lds)
 }
 
 // have = ceil(ctx / page), want = ceil((ctx + n) / page), both cut at max_pages; page k of a request, have <= k < want, is
-// free_pages[off + k - have] with off = sum of want - have over the requests before it.  (A new page has a row at its start: all sums are at most T.)
+// free_pages[off + k - have] with off = sum of want - have over the requests before it.  (A new page has a row at its start: all sums are at most T.  Of
+// requests that overlap they may wrap; a pick is compared unsigned, and stays within the list.)
 // Latency is what bounds it: a handful of bytes per request, and a chain of reads.  Every workgroup therefore sums the requests before its rows by itself (twelve
 // bytes each, from the cache, all reads in flight at once) instead of waiting for another launch to do it, keeps the requests that own its rows in LDS, and
 // writes its rows; the last one sums all requests and writes kv_len and the counts.  32 requests, one row each: 4.2 us a call; 4096 requests and 356 000 rows:
 // 9.2 us, where the 4.5 MB that it moves would take 1.
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a)
 {
-    __shared__ int32_t lds[32], sums[4][PLAN_THREADS / 64];
-    __shared__ int32_t own_start[PLAN_THREADS], own_end[PLAN_THREADS], own_ctx[PLAN_THREADS], own_off[PLAN_THREADS];
+    __shared__ int32_t lds[32];
+    __shared__ uint32_t sums[4][PLAN_THREADS / 64], own_off[PLAN_THREADS];
+    __shared__ int32_t own_start[PLAN_THREADS], own_end[PLAN_THREADS], own_ctx[PLAN_THREADS];
     const int32_t page = 1 << a.page_shift, n_threads = (int32_t)blockDim.x;
     const int32_t row0 = (int32_t)blockIdx.x * n_threads * PLAN_ROWS, row1 = min(a.T, row0 + n_threads * PLAN_ROWS);
     const bool last = blockIdx.x + 1 == gridDim.x;
     // requests that end before this workgroup's rows: their pages, and how many they are; all requests: their pages, and those that do not fit the table
-    int32_t off = 0, first = 0, all = 0, over = 0;
+    uint32_t off = 0, first = 0, all = 0, over = 0;
 #pragma unroll 4
     for (int32_t s = (int32_t)threadIdx.x; s < a.S; s += n_threads) {
         const PlanRequest r = plan_request(a, s);
-        if (r.hi <= row0) { off += r.need; ++first; }
-        all += r.need;
-        over += r.over;
+        if (r.hi <= row0) { off += (uint32_t)r.need; ++first; }
+        all += (uint32_t)r.need;
+        over += (uint32_t)r.over;
         if (last) a.kv_len[s] = r.ctx + (r.hi - r.lo);
     }
     if (row0 > 0) {                                    // else there are none before, but empty ones
@@ -83,24 +85,24 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a)
         all = block_sum(all, sums[2]);
         over = block_sum(over, sums[3]);
         if (threadIdx.x == 0) {
-            const int32_t taken = min(a.n_free, all);
-            a.counts[0] = taken;
-            a.counts[1] = all - taken + over;
+            const uint32_t taken = min((uint32_t)a.n_free, all);
+            a.counts[0] = (int32_t)taken;
+            a.counts[1] = (int32_t)(all - taken + over);
         }
     }
     int64_t slot[PLAN_ROWS];
     int32_t at[PLAN_ROWS];
 #pragma unroll
     for (int i = 0; i < PLAN_ROWS; ++i) { slot[i] = -1; at[i] = 0; }
-    for (int32_t s0 = first; s0 < a.S; s0 += n_threads) {          // more than once only where hundreds of requests without rows stand together
+    for (int32_t s0 = (int32_t)first; s0 < a.S; s0 += n_threads) {          // more than once only where hundreds of requests without rows stand together
         const int32_t s = s0 + (int32_t)threadIdx.x;
         PlanRequest r = {};
         r.lo = INT32_MAX;
         if (s < a.S) r = plan_request(a, s);
         int32_t total;
         const int32_t here = block_exclusive_scan(r.need, lds, &total);        // its barriers also end the reads of the turn before
-        own_start[threadIdx.x] = r.lo; own_end[threadIdx.x] = r.hi; own_ctx[threadIdx.x] = r.ctx; own_off[threadIdx.x] = off + here;
-        off += total;
+        own_start[threadIdx.x] = r.lo; own_end[threadIdx.x] = r.hi; own_ctx[threadIdx.x] = r.ctx; own_off[threadIdx.x] = off + (uint32_t)here;
+        off += (uint32_t)total;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PLAN_ROWS; ++i) {
@@ -119,8 +121,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(PlanArgs a)
             if (k < have) {
                 p = *entry;
             } else {
-                const int64_t pick = (int64_t)own_off[lo] + (k - have);
-                p = pick < a.n_free ? a.free_pages[pick] : -1;
+                const uint32_t pick = own_off[lo] + (uint32_t)(k - have);
+                p = pick < (uint32_t)a.n_free ? a.free_pages[pick] : -1;
                 if ((at[i] & (page - 1)) == 0) *entry = p;         // a new page has exactly one row at its start
             }
             if (p >= 0) slot[i] = ((int64_t)p << a.page_shift) + (at[i] & (page - 1));
