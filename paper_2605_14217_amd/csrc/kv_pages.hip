@@ -225,7 +225,7 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
     a.k_cache = (char *)k_cache; a.v_cache = (char *)v_cache; a.k = (const char *)k; a.v = (const char *)v; a.slot_map = slot_map;
     a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.T = T; a.page_shift = shift; a.heads = n_kv_heads;
     a.head_bytes = (int32_t)(head_dim * e);
-    hipLaunchKernelGGL(kv_store_kernel, dim3((unsigned)((T + 3) / 4), 2), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(kv_store_kernel, dim3((unsigned)(((int64_t)T + 3) / 4), 2), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
     return launched();
 }
 

@@ -23,8 +23,8 @@ def driver(tmp_path_factory):
     return exe
 
 
-def ask(driver, lines):
-    run = subprocess.run([str(driver)], input="\n".join(lines) + "\n", capture_output=True, text=True, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"), timeout=300)
+def ask(driver, lines, *args):
+    run = subprocess.run([str(driver), *args], input="\n".join(lines) + "\n", capture_output=True, text=True, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"), timeout=300)
     assert run.returncode == 0, run.stdout[-500:] + run.stderr[-3000:]
     return [[int(x) for x in line.split()] for line in run.stdout.splitlines()]
 
@@ -45,3 +45,8 @@ def test_pages_of_overlapping_requests_past_31_bits(driver):
     for line, rows in ((overlapping, 1024), (short, 3000)):
         got, = ask(driver, [line])
         assert got[0] == 0 and got[4] == rows
+
+
+def test_store_of_as_many_rows_as_32_bits_count(driver):
+    rows = [1, 4, 5, 2 ** 31 - 4, 2 ** 31 - 3, 2 ** 31 - 1]
+    assert ask(driver, [str(t) for t in rows], "store") == [[0, -(-t // 4)] for t in rows]
