@@ -577,6 +577,12 @@ def _cache(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None):
     return t.data_ptr()
 
 
+def _attention_workspace(t: torch.Tensor):
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace: need a contiguous device tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def preft_kv_plan(slot_map: torch.Tensor, positions: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, counts: torch.Tensor,
                   seg_start: torch.Tensor, ctx_len: torch.Tensor, free_pages: torch.Tensor, page_size: int, stream=None) -> None:
     """Slots and positions of the batch's rows, the requests' new lengths and the new entries of their block tables.  counts (2 values): pages
@@ -638,8 +644,8 @@ def preft_prompt_attention(out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, 
     S = int(seg_prefill_len.numel())
     rc = load_library().preft_prompt_attention(
         op, ldo, qp, ldq, kp, ldk, vp, ldv, T, heads, kv_heads, dim, _table(seg_start, "seg_start", S + 1),
-        _table(seg_prefill_len, "seg_prefill_len", S), S, float(scale), _dtype_code(out), int(mode), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream(stream))
+        _table(seg_prefill_len, "seg_prefill_len", S), S, float(scale), _dtype_code(out), int(mode),
+        *_attention_workspace(workspace), _stream(stream))
     _check(rc, "preft_prompt_attention")
 
 
@@ -673,5 +679,5 @@ def preft_cached_attention(out: torch.Tensor, q: torch.Tensor, seg_start: torch.
         None if seg_prefill_len is None else _table(seg_prefill_len, "seg_prefill_len", S), _table(kv_len, "kv_len", S), S, kc, vc, n_pages, page,
         table, ld, max_pages, None if n_groups == 0 else _table(group_start, "group_start", n_groups + 1),
         None if n_groups == 0 else _table(group_prefix_len, "group_prefix_len", n_groups), n_groups, float(scale), _dtype_code(out), int(mode),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+        *_attention_workspace(workspace), _stream(stream))
     _check(rc, "preft_cached_attention")

@@ -345,6 +345,8 @@ bool as_last(PyObject *const *o, Last &l)
     const double scale = PyFloat_AsDouble(o[0]);
     if (scale == -1.0 && PyErr_Occurred()) return false;
     l.scale = (float)scale;
+    const at::Tensor *ws = tensor(o[2]);
+    if (!ws || !ws->is_cuda() || !ws->is_contiguous()) return false;
     return as_int(o[1], l.mode) && as_workspace(o[2], l.workspace, l.bytes) && as_stream(o[3], l.stream);
 }
 

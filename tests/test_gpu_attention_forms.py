@@ -237,3 +237,18 @@ def test_a_schedule_serves_calls_of_its_type_and_its_tables_room(S, H, Hkv, firs
             preft.preft_schedule_counts(ws)
         assert e.value.code == preft.PREFT_ESCHEDULE
     assert torch.equal(built, run(first, READY))
+
+
+def test_workspaces_that_are_no_device_memory_are_refused():
+    """On the host, or fewer bytes than they seem: refused before any launch, by either way into the library."""
+    print("\n[case] workspaces", flush=True)
+    s, layers = mixed_step(9, 1, False)
+    q, k, v, kc, vc = layers[0]
+    n = preft.preft_attention_workspace_bytes(s["T"], 9, s["H"], s["Hkv"], s["D"])
+    out, prefill, kv = torch.full_like(q, 7.5), i32(s["prefill"]), i32(s["kv"])
+    for ws in (torch.zeros(n, dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8, device="cuda").expand(n), torch.zeros(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            preft.preft_prompt_attention(out, q, k, v, s["seg"], prefill, s["H"], s["Hkv"], 0.125, 0, ws)
+        with pytest.raises(ValueError, match="workspace"):
+            preft.preft_cached_attention(out, q, s["seg"], prefill, kv, kc, vc, s["dev"], None, None, s["H"], 0.125, 0, ws)
+    assert bool((out == 7.5).all())
