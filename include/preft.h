@@ -456,7 +456,9 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
  * outside [group_start[0], group_start[n_groups]) are in no group.  The result is that of the call without groups, to rounding.
  *
  * Products are accumulated, and the softmax is computed, in fp32; in bf16 the weights p are rounded to bf16 for the product with v, and each output is
- * rounded once.  What a row does not see does not reach it, infinities and NaN included.  scale must be positive and finite.
+ * rounded once.  What a row does not see does not reach it, infinities and NaN included.  Of what it sees, a key whose score is -inf has the weight 0, and a row
+ * that sees no others gets zeros, like one without keys (where the formula is 0 / 0); a score that is NaN or +inf makes its head's output NaN, as in the formula.
+ * scale must be positive and finite.
  * out must not overlap q, k, v or the caches, except that column ranges of one buffer may be side by side.  Two calls with the same arguments give the same bits.
  *
  * The workspace (16-byte aligned, preft_attention_workspace_bytes) holds the schedules of both kinds of call, each with a place of its own, and the parts of rows whose keys

@@ -252,3 +252,64 @@ def test_workspaces_that_are_no_device_memory_are_refused():
         with pytest.raises(ValueError, match="workspace"):
             preft.preft_cached_attention(out, q, s["seg"], prefill, kv, kc, vc, s["dev"], None, None, s["H"], 0.125, 0, ws)
     assert bool((out == 7.5).all())
+
+
+def infinite_scores(k, q, H, Hkv, D, hidden, top=None):
+    """Scores of the keys `hidden` become -inf for every row, that of `top` +inf: q's first dimension is 1, theirs infinite."""
+    q.view(q.shape[0], H, D)[..., 0] = 1.0
+    k[hidden, ..., 0] = -float("inf")
+    if top is not None:
+        k[top, ..., 0] = float("inf")
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D", HEADS[:4])
+def test_infinite_scores_in_prompts(dtype, H, Hkv, D):
+    """Keys of score -inf weigh nothing, rows that see no others are zero, and rows that see a score of +inf are NaN."""
+    print(f"\n[case] infinite scores, prompts {dtype} {H}/{Hkv}x{D}", flush=True)
+    td = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    for T, none, top in ((200, 10, 150), (40, 33, 39), (2111, 700, None)):          # the last: long enough to be divided
+        q, k, v = (normal(gen, T, w * D).to(td) for w in (H, Hkv, Hkv))
+        infinite_scores(k.view(T, Hkv, D), q, H, Hkv, D, slice(0, none), top)
+        out = torch.full_like(q, 7.5)
+        preft.preft_prompt_attention(out, q, k, v, i32([0, T]), i32([T]), H, Hkv, D ** -0.5, 0, preft.new_attention_workspace(T, 1, H, Hkv, D))
+        got, qc, kc, vc = out.cpu().double().view(T, H, D), q.cpu().double().view(T, H, D), *(x.cpu().double().view(T, Hkv, D).transpose(0, 1) for x in (k, v))
+        assert not got[:none].any()
+        if top is not None:
+            assert got[top:].isnan().all()
+        for t in sorted({none, none + 1, (none + T) // 2, (top or T) - 1} - {none - 1}):
+            if top is not None and t >= top:
+                continue
+            o, bound = ref.attend_row(qc[t], kc[:, none:t + 1], vc[:, none:t + 1], D ** -0.5, td)
+            assert ((got[t] - o).abs() <= bound).all(), t
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D", HEADS[:4])
+def test_infinite_scores_over_pages(dtype, H, Hkv, D):
+    """The same for decode rows: requests whose first keys, or all, have the score -inf, short and divided, and groups whose shared keys do."""
+    print(f"\n[case] infinite scores, pages {dtype} {H}/{Hkv}x{D}", flush=True)
+    page, rows = 16, [1] * 7
+    kv, none = [300, 9001, 40, 9001, 260, 200, 128], [100, 5000, 40, 9001, 128, 200, 128]      # the last three share 128 tokens
+    out, before, _, args, ws, (gs, gp, H, scale) = cached_case(dtype, H, Hkv, D, page, rows, kv, groups=[(4, 7)], prefix=[128])
+    q, start, _, kvl, kc, vc, table = args
+    q = q.clone()
+    for s in range(7):
+        for i in range(-(-none[s] // page)):
+            infinite_scores(kc[int(table[s, i])].transpose(0, 1), q, H, Hkv, D, slice(0, min(page, none[s] - i * page)))
+    got = torch.full_like(q, 7.5)
+    preft.preft_cached_attention(got, q, start, None, kvl, kc, vc, table, gs, gp, H, scale, 0, ws)
+    got = got.cpu().double().view(7, H, D)
+    for s in range(7):
+        if none[s] == kv[s]:
+            assert not got[s].any(), s
+            continue
+        pages = table[s, : -(-kv[s] // page)].long()
+        K, V = (c[pages].transpose(0, 1).reshape(Hkv, -1, D)[:, none[s]:kv[s]].cpu().double() for c in (kc, vc))
+        o, bound = ref.attend_row(q[s].cpu().double().view(H, D), K, V, scale, q.dtype)
+        assert ((got[s] - o).abs() <= bound).all(), s
+    # and one score of +inf
+    infinite_scores(kc[int(table[0, 7])].transpose(0, 1), q, H, Hkv, D, slice(0, 0), 3)
+    infinite_scores(kc[int(table[4, 2])].transpose(0, 1), q, H, Hkv, D, slice(0, 0), 3)
+    out = torch.full_like(q, 7.5)
+    preft.preft_cached_attention(out, q, start, None, kvl, kc, vc, table, gs, gp, H, scale, 0, ws)
+    assert out[[0, 4, 5, 6]].isnan().all() and torch.isfinite(out[1:4]).all()
