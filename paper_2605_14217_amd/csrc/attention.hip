@@ -14,11 +14,11 @@ using namespace preft;
 template <typename E, int D, bool PAGED, bool DIRECT>
 int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
 {
-    hipLaunchKernelGGL((attention_kernel<E, D, PAGED, DIRECT>), dim3((unsigned)(p.units * a.kv_heads)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attention_kernel<E, D, PAGED, DIRECT>), dim3((unsigned)(p.units * a.s.kv_heads)), dim3(256), 0, st, a);
     if (p.merge) {
-        const unsigned tiles = (unsigned)(a.l.merge_cap < 1024 ? a.l.merge_cap : 1024);
-        const unsigned z = tiles * (unsigned)a.kv_heads < 256 && (int64_t)a.T * a.group > 4 ? 16u : 1u;      // workgroups that share a tile's columns
-        hipLaunchKernelGGL((attention_merge_kernel<E, D>), dim3(tiles, (unsigned)a.kv_heads, z), dim3(256), 0, st, a, PAGED ? 2 : 1);
+        const unsigned tiles = (unsigned)(a.s.l.merge_cap < 1024 ? a.s.l.merge_cap : 1024);
+        const unsigned z = tiles * (unsigned)a.s.kv_heads < 256 && (int64_t)a.s.T * a.s.group > 4 ? 16u : 1u;      // workgroups that share a tile's columns
+        hipLaunchKernelGGL((attention_merge_kernel<E, D>), dim3(tiles, (unsigned)a.s.kv_heads, z), dim3(256), 0, st, a, PAGED ? 2 : 1);
     }
     return launched();
 }
@@ -83,13 +83,11 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
     AttnArgs a = {};
     a.q = q; a.k = k; a.v = v; a.out = out;
     a.ldq = ldq * e; a.ldk = ldk * e; a.ldv = ldv * e; a.ldo = ldo * e;
-    a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads; a.group = n_heads / n_kv_heads;
-    a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;
-    a.l = lists_of(l, workspace);
     AttnScheduleArgs &s = a.s;
-    s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = a.group;
-    s.l = a.l;
+    s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len;
+    s.S = S; s.T = T; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = n_heads / n_kv_heads; s.l = lists_of(l, workspace);
+    a.per_head = ((1u << 21) + (uint32_t)s.group - 1) / (uint32_t)s.group;
     prompt_rules(s, dtype);
     return run<false>(a, dtype, head_dim, mode, st);
 }
@@ -122,13 +120,11 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
     AttnArgs a = {};
     a.q = q; a.k = k_cache; a.v = v_cache; a.out = out; a.ldq = ldq * e; a.ldo = ldo * e;
     a.table = block_table; a.ld_table = ld_table; a.n_pages = n_pages; a.page_shift = shift;
-    a.T = T; a.S = S; a.heads = n_heads; a.kv_heads = n_kv_heads; a.group = n_heads / n_kv_heads; a.n_groups = n_groups;
-    a.per_head = ((1u << 21) + (uint32_t)a.group - 1) / (uint32_t)a.group;
     a.scale_log2 = scale * 1.44269504088896340736f;
-    a.l = lists_of(l, workspace);
     AttnScheduleArgs &s = a.s;
     s.seg_start = seg_start; s.seg_prefill_len = seg_prefill_len; s.kv_len = kv_len; s.group_start = group_start; s.group_prefix = group_prefix_len;
-    s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = a.group; s.l = a.l;
+    s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = n_heads / n_kv_heads; s.l = lists_of(l, workspace);
+    a.per_head = ((1u << 21) + (uint32_t)s.group - 1) / (uint32_t)s.group;
     cached_rules(s, dtype, keys ? (int64_t)max_pages << shift : 0);
     return run<true>(a, dtype, head_dim, mode, st);
 }

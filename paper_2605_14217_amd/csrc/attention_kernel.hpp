@@ -23,17 +23,15 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef PREFT_LDS char *lds_t;
 
 struct AttnArgs {
+    AttnScheduleArgs s;               // sizes, tables and lists
     const void *q, *k, *v;            // k, v: packed rows, or the cache
     void *out;
     int64_t ldq, ldk, ldv, ldo;       // bytes
     const int32_t *table;
     int64_t ld_table;
     int32_t n_pages, page_shift;
-    int32_t T, S, heads, kv_heads, group, n_groups;      // group: query heads of a key/value head, G
     float scale_log2;
     uint32_t per_head;                // ceil(2^21 / G): x / G = x per_head >> 21 for x < 2048 (G <= 1024)
-    AttnLists l;
-    AttnScheduleArgs s;               // direct calls find their units from it
     int32_t ready;                    // direct calls: the header is there already
 };
 
@@ -101,7 +99,7 @@ template <typename E, int D, bool PAGED> struct AttnSource {
         if constexpr (PAGED) {
             page_shift = a.page_shift;
             n_pages = a.n_pages;
-            page_bytes = ((int64_t)a.kv_heads * X::ROW) << page_shift;
+            page_bytes = ((int64_t)a.s.kv_heads * X::ROW) << page_shift;
             k = (const char *)a.k + (((int64_t)head * X::ROW) << page_shift);
             v = (const char *)a.v + (((int64_t)head * X::ROW) << page_shift);
             table = a.table + (int64_t)u.table * a.ld_table;
@@ -172,7 +170,7 @@ template <typename E, int D> struct AttnColumns {
 
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
     {
-        const int lane = threadIdx.x & 63, half = lane >> 5, col = first + (lane & 31), G = a.group;
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = first + (lane & 31), G = a.s.group;
         valid = col < u.ncols;
         const int32_t x = u.head0 + min(col, u.ncols - 1), i = (int32_t)((uint32_t)x * a.per_head >> 21);
         head = kv_head * G + (x - i * G);
@@ -180,11 +178,11 @@ template <typename E, int D> struct AttnColumns {
             row = u.row0 + i;
             lim = u.lim0 + i;
         } else {
-            const int2 r = a.l.group_rows[min(-1 - u.row0 + i, a.l.group_row_cap - 1)];
+            const int2 r = a.s.l.group_rows[min(-1 - u.row0 + i, a.s.l.group_row_cap - 1)];
             row = r.x;
             lim = r.y;
         }
-        row = max(0, min(row, a.T - 1));
+        row = max(0, min(row, a.s.T - 1));
         lim = min(lim, u.key1);
         const gcptr_t from = as_global((const char *)a.q + (int64_t)row * a.ldq + head * X::ROW + half * 16);
 #pragma unroll
@@ -426,13 +424,13 @@ __device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit 
         }
     } else if (w.valid) {
         const int64_t part = (int64_t)u.slot + kv_head * u.ncols + first + (lane & 31);
-        const gptr_t to = as_global((void *)(a.l.part_o + part * D + half * 4));
+        const gptr_t to = as_global((void *)(a.s.l.part_o + part * D + half * 4));
 #pragma unroll
         for (int b = 0; b < X::BLOCKS; ++b)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 store4<float>(to + (b * 32 + 8 * r) * 4, w.o[b][4 * r], w.o[b][4 * r + 1], w.o[b][4 * r + 2], w.o[b][4 * r + 3]);
-        if (half == 0) a.l.part_ml[part] = make_float2(w.m, l);
+        if (half == 0) a.s.l.part_ml[part] = make_float2(w.m, l);
     }
 }
 
@@ -645,14 +643,14 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }
         if (u.slot < 0) {
-            const int32_t x = u.head0 + cc, q = (int32_t)((uint32_t)x * a.per_head >> 21), head = kv_head * a.group + (x - q * a.group);
+            const int32_t x = u.head0 + cc, q = (int32_t)((uint32_t)x * a.per_head >> 21), head = kv_head * a.s.group + (x - q * a.s.group);
             const float inv = inverse(ll);
-            const int32_t row = max(0, min(u.row0 + q, a.T - 1));   // a group's units always have parts
+            const int32_t row = max(0, min(u.row0 + q, a.s.T - 1));   // a group's units always have parts
             store4<E>(as_global((char *)a.out + (int64_t)row * a.ldo + head * X::ROW + d * X::ELEM), v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
         } else {
             const int64_t part = (int64_t)u.slot + kv_head * u.ncols + cc;
-            store4<float>(as_global((void *)(a.l.part_o + part * D + d)), v[0], v[1], v[2], v[3]);
-            if (d == 0) a.l.part_ml[part] = make_float2(mm, ll);
+            store4<float>(as_global((void *)(a.s.l.part_o + part * D + d)), v[0], v[1], v[2], v[3]);
+            if (d == 0) a.s.l.part_ml[part] = make_float2(mm, ll);
         }
     }
 }
@@ -661,7 +659,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
 __device__ __forceinline__ bool attn_schedule_is(const AttnArgs &a, int kind)
 {
     const bool same = attn_schedule_fits(a.s);
-    if (!same && threadIdx.x == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) a.l.report[HDR_MISMATCH] = ATTN_MARK | kind | attn_marks(a.l.report);
+    if (!same && threadIdx.x == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) a.s.l.report[HDR_MISMATCH] = ATTN_MARK | kind | attn_marks(a.s.l.report);
     return same;
 }
 
@@ -674,7 +672,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
     constexpr int JOIN = 4 * 32 * (D + 4) * 4, KIND = PAGED ? 2 : 1;
     __shared__ __align__(1024) char lds[X::LDS > JOIN ? X::LDS : JOIN];
     __shared__ float join[256];
-    const int32_t unit = (int32_t)blockIdx.x / a.kv_heads, kv_head = (int32_t)blockIdx.x % a.kv_heads;
+    const int32_t unit = (int32_t)blockIdx.x / a.s.kv_heads, kv_head = (int32_t)blockIdx.x % a.s.kv_heads;
     AttnUnit u;
     if constexpr (DIRECT) {
         if (a.ready && !attn_schedule_is(a, KIND)) return;
@@ -682,10 +680,10 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
     } else {
         if (!attn_schedule_is(a, KIND)) return;
         // short units: one a wavefront, four a workgroup
-        const int32_t units = as_const(a.l.header)[AH_UNITS], alone = as_const(a.l.header)[AH_SHORT];
+        const int32_t units = as_const(a.s.l.header)[AH_UNITS], alone = as_const(a.s.l.header)[AH_SHORT];
         const int32_t i = unit < alone ? unit : alone + 4 * (unit - alone) + uniform(threadIdx.x >> 6);
         if (i >= units) return;
-        const PREFT_CONST AttnUnit *p = as_const(a.l.units) + i;
+        const PREFT_CONST AttnUnit *p = as_const(a.s.l.units) + i;
         u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
         if (unit >= alone) {
             if (u.ncols > 0) attend_keys<E, D, PAGED, true>(a, u, kv_head, (lds_t)lds, join);
@@ -702,22 +700,22 @@ template <typename E, int D>
 __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j, int kv_head)
 {
     using X = AttnTile<E, D>;
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, G = a.group;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, G = a.s.group;
     for (int32_t c = blockIdx.z * 4 + wave; c < j.ncols; c += 4 * gridDim.z) {
         const int32_t gc = j.group_col0 + c, tile = gc / ATTN_COLS;
         const int32_t width = min(ATTN_COLS, j.group_cols - tile * ATTN_COLS);
-        const int64_t group = (int64_t)j.group_slot + (int64_t)tile * ATTN_COLS * a.kv_heads * j.group_parts + kv_head * width + gc % ATTN_COLS;
+        const int64_t group = (int64_t)j.group_slot + (int64_t)tile * ATTN_COLS * a.s.kv_heads * j.group_parts + kv_head * width + gc % ATTN_COLS;
         const int64_t mine = (int64_t)j.slot + kv_head * j.ncols + c;
         const int32_t parts = j.parts + j.group_parts;           // at least one: see where the entries are made
         auto part = [&](int32_t k) {                               // slots are below 2^31: checked where the workspace is laid out
-            const int64_t p = k < j.parts ? mine + (int64_t)k * j.ncols * a.kv_heads : group + (int64_t)(k - j.parts) * width * a.kv_heads;
-            return p < 0 || p >= a.l.slot_cap ? 0 : (int32_t)p;
+            const int64_t p = k < j.parts ? mine + (int64_t)k * j.ncols * a.s.kv_heads : group + (int64_t)(k - j.parts) * width * a.s.kv_heads;
+            return p < 0 || p >= a.s.l.slot_cap ? 0 : (int32_t)p;
         };
         // A lane has the place and the factor of a part, 64 parts at a time; their rows are then read eight at a time, with nothing to wait for in between.
         int32_t at = part(min(lane, parts - 1));
-        float2 ml = a.l.part_ml[at];
+        float2 ml = a.s.l.part_ml[at];
         float top = ml.x;
-        for (int32_t k = lane + 64; k < parts; k += 64) top = fmaxf(top, a.l.part_ml[part(k)].x);
+        for (int32_t k = lane + 64; k < parts; k += 64) top = fmaxf(top, a.s.l.part_ml[part(k)].x);
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
         float o[D / 64] = {}, l = 0.0f;
@@ -725,7 +723,7 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
             const int32_t n = min(64, parts - k0);
             if (k0 > 0) {
                 at = part(min(k0 + lane, parts - 1));
-                ml = a.l.part_ml[at];
+                ml = a.s.l.part_ml[at];
             }
             const float f = __builtin_amdgcn_exp2f(ml.x - top);
             float sum = lane < n ? ml.y * f : 0.0f;
@@ -734,7 +732,7 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if (k + e >= n) continue;
-                    const float *from = a.l.part_o + (int64_t)__builtin_amdgcn_readlane(at, k + e) * D + lane;
+                    const float *from = a.s.l.part_o + (int64_t)__builtin_amdgcn_readlane(at, k + e) * D + lane;
 #pragma unroll
                     for (int d = 0; d < D / 64; ++d) x[e][d] = from[d * 64];
                 }
@@ -750,7 +748,7 @@ __device__ __forceinline__ void join_tile(const AttnArgs &a, const AttnMerge &j,
             l += sum;
         }
         const float inv = inverse(l);
-        const int32_t q = (j.col0 + c) / G, head = kv_head * G + (j.col0 + c - q * G), row = max(0, min(j.row0 + q, a.T - 1));
+        const int32_t q = (j.col0 + c) / G, head = kv_head * G + (j.col0 + c - q * G), row = max(0, min(j.row0 + q, a.s.T - 1));
         E *to = (E *)((char *)a.out + (int64_t)row * a.ldo + head * X::ROW);
 #pragma unroll
         for (int d = 0; d < D / 64; ++d) to[d * 64 + lane] = (E)(o[d] * inv);
@@ -761,9 +759,9 @@ template <typename E, int D>
 __global__ __launch_bounds__(256) void attention_merge_kernel(AttnArgs a, int kind)
 {
     if (!attn_schedule_is(a, kind)) return;
-    const int32_t n = as_const(a.l.header)[AH_JOINS];
+    const int32_t n = as_const(a.s.l.header)[AH_JOINS];
     for (int32_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const AttnMerge j = a.l.merges[i];
+        const AttnMerge j = a.s.l.merges[i];
         if (j.parts + j.group_parts > 0) join_tile<E, D>(a, j, (int)blockIdx.y);
     }
 }
