@@ -659,7 +659,10 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
 __device__ __forceinline__ bool attn_schedule_is(const AttnArgs &a, int kind)
 {
     const bool same = attn_schedule_fits(a.s);
-    if (!same && threadIdx.x == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) a.s.l.report[HDR_MISMATCH] = ATTN_MARK | kind | attn_marks(a.s.l.report);
+    if (!same && threadIdx.x == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) {
+        a.s.l.report[HDR_ALL] = ATTN_REPORT;
+        a.s.l.report[ATTN_MARKS + kind] = ATTN_MARK;
+    }
     return same;
 }
 

@@ -37,7 +37,7 @@ struct AttnMerge {
 };
 
 struct AttnLists {
-    int32_t   *report;     // what preft_schedule_counts reads: units, joined tiles and tiles of the last schedule, and the mark of refused calls
+    int32_t   *report;     // what preft_schedule_counts reads: units, joined tiles and tiles of the last schedule, and the marks of refused calls
     int32_t   *header;     // HEADER_INTS ints of this kind of call
     AttnUnit  *units;
     AttnMerge *merges;
@@ -54,11 +54,6 @@ struct AttnLists {
 };
 
 constexpr int AH_UNITS = 0, AH_MERGES = 1, AH_TILES = 2, AH_KIND = 3, AH_GROUPS = 4, AH_T = 5, AH_S = 6, AH_HEADS = 7, AH_DTYPE = 8, AH_KV_HEADS = 9, AH_SHORT = 10, AH_JOINS = 11, AH_KEYS = 12;      // AH_SHORT: first unit that is one wavefront's; AH_JOINS: entries of merges
-
-// A call that found another batch's schedule marks the report with its kind; the next schedule of that kind takes the mark away.  (Anything else that stands there is what
-// the memory held before.)
-constexpr int32_t ATTN_MARK = 0x5a7e0000;
-__device__ __forceinline__ int32_t attn_marks(const int32_t *report) { return (report[HDR_MISMATCH] & ~3) == ATTN_MARK ? report[HDR_MISMATCH] & 3 : 0; }
 
 struct AttnScheduleArgs {
     const int32_t *seg_start, *seg_prefill_len;            // seg_prefill_len may be null in a cached call
@@ -115,8 +110,8 @@ __device__ __forceinline__ int32_t part_begin(int32_t n, int32_t parts, int32_t 
 __device__ __forceinline__ void attn_header(const AttnScheduleArgs &a, int32_t units, int32_t alone, int32_t tiles, int32_t joined, int32_t joins)
 {
     int32_t *h = a.l.header, *r = a.l.report;
-    const int32_t kind = a.kv_len ? 2 : 1, marks = attn_marks(r) & ~kind;
-    r[AH_UNITS] = units; r[AH_MERGES] = joined; r[AH_TILES] = tiles; r[HDR_MISMATCH] = marks != 0 ? ATTN_MARK | marks : 0;
+    const int32_t kind = a.kv_len ? 2 : 1;
+    r[AH_UNITS] = units; r[AH_MERGES] = joined; r[AH_TILES] = tiles; r[HDR_ALL] = ATTN_REPORT; r[ATTN_MARKS + kind] = 0;
     h[AH_UNITS] = units; h[AH_SHORT] = alone; h[AH_TILES] = tiles; h[AH_MERGES] = joined; h[AH_JOINS] = joins;
     h[AH_KIND] = kind; h[AH_DTYPE] = a.dtype; h[AH_KEYS] = a.max_keys; h[AH_GROUPS] = a.n_groups; h[AH_T] = a.T; h[AH_S] = a.S; h[AH_HEADS] = a.heads; h[AH_KV_HEADS] = a.kv_heads;
 }
@@ -170,31 +165,31 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     const bool in_lds = items <= ATTN_SCAN;
     if (tid == 0) { n_merges = 0; n_slots = 0; cost_sum = 0; goes_back = 0; }
     for (int b = tid; b < 512; b += nt) bins[b] = 0;
-    __syncthreads();
-    for (int32_t s = tid; s < a.S; s += nt)
-        if (goes_back_at(a.seg_start, s, a.T)) goes_back = 1;
-    for (int32_t g = tid; g < a.n_groups; g += nt)
-        if (goes_back_at(a.group_start, g, a.S)) goes_back = 1;
-    __syncthreads();
-    if (goes_back) {
-        if (tid == 0) attn_header(a, 0, 0, 0, 0, 0);
-        return;
-    }
+    // Whether offsets go back is known after the first loop over them; its sums wrap where they do.  All threads then leave: true for them all.
+    bool back = false;
+    auto nothing_to_run = [&]() {
+        if (back) goes_back = 1;                           // set to 0 before a barrier of the loop
+        __syncthreads();
+        if (goes_back && tid == 0) attn_header(a, 0, 0, 0, 0, 0);
+        return goes_back != 0;
+    };
 
     // groups: how many rows each has, and where they stand in the row list
     if (a.n_groups > 0) {
-        int32_t carry = 0;
+        uint32_t rows_carry = 0;
         for (int32_t s0 = 0; s0 < a.S; s0 += nt) {
             const int32_t s = s0 + tid;
             int32_t total;
             const int32_t rows = s < a.S ? attn_segment(a, s).rows : 0;
+            back = back || (s < a.S && goes_back_at(a.seg_start, s, a.T));
             const int32_t before = block_exclusive_scan(rows, lds, &total);
-            if (s < a.S) a.l.rows_before[s] = carry + before;
-            carry += total;
+            if (s < a.S) a.l.rows_before[s] = (int32_t)(rows_carry + (uint32_t)before);
+            rows_carry += (uint32_t)total;
         }
-        if (tid == 0) a.l.rows_before[a.S] = carry;
-        __syncthreads();
-        carry = 0;
+        if (tid == 0) a.l.rows_before[a.S] = (int32_t)rows_carry;
+        for (int32_t g = tid; g < a.n_groups; g += nt) back = back || goes_back_at(a.group_start, g, a.S);
+        if (nothing_to_run()) return;
+        int32_t carry = 0;
         for (int32_t g0 = 0; g0 < a.n_groups; g0 += nt) {
             const int32_t g = g0 + tid;
             int32_t rows = 0, total;
@@ -214,13 +209,14 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
     }
 
     // items: column tiles, and the work of all
-    int32_t carry = 0;
+    uint32_t carry = 0;
     unsigned long long cost = 0;
     for (int32_t i0 = 0; i0 < items; i0 += nt) {
         const int32_t i = i0 + tid;
         int32_t tiles = 0, total;
         if (i < a.S) {
             AttnItem it = attn_segment(a, i);
+            back = back || goes_back_at(a.seg_start, i, a.T);
             if (a.n_groups > 0) {
                 const int32_t g = last_at_or_before(a.group_start, a.n_groups, i);
                 const AttnGroup m = attn_group(a, g);
@@ -250,15 +246,16 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         }
         const int32_t before = block_exclusive_scan(tiles, lds, &total);
         if (i < items) {
-            if (in_lds) first_tile[i] = carry + before;
-            else a.l.tiles[i] = carry + before;
+            const int32_t first = (int32_t)(carry + (uint32_t)before);
+            if (in_lds) first_tile[i] = first;
+            else a.l.tiles[i] = first;
         }
-        carry += total;
+        carry += (uint32_t)total;
     }
     for (int off = 32; off > 0; off >>= 1) cost += __shfl_xor(cost, off, 64);
     if ((tid & 63) == 0) atomicAdd(&cost_sum, cost);
-    __syncthreads();
-    const int32_t n_tiles = min(carry, a.l.tile_cap);
+    if (nothing_to_run()) return;
+    const int32_t n_tiles = min((int32_t)carry, a.l.tile_cap);
     // a range of keys: no shorter than the whole work over the workgroups it is meant for
     // (Wide and narrow tiles each for themselves: 206 us against 173 on 256 rows of 64 heads with prefixes of 8192.  All workgroups are wide ones then at first, and memory
     // waits for the narrow ones.)

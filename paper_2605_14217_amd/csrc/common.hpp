@@ -33,6 +33,14 @@ constexpr int SORT_MAX_N  = 4096;   // pools up to this many slots get their sho
 constexpr int HEADER_INTS = 16;
 constexpr int HDR_CHUNKS = 0, HDR_SHORT_ROWS = 1, HDR_ACTIVE = 2, HDR_ALL = 3, HDR_GTILES = 4, HDR_T = 5, HDR_S = 6,
               HDR_N = 7, HDR_MISMATCH = 8;
+// The same words of an attention workspace: [0..2] counts, [3] says that it is one, and for each kind of call (1, 2) a word that is ATTN_MARK where a call found
+// another batch's schedule, until the next schedule of that kind.  (Any other value is what the memory held before.)
+constexpr int32_t ATTN_REPORT = 0x5a7e0000, ATTN_MARK = 0x5a7e0001;
+constexpr int ATTN_MARKS = 8;
+inline bool schedule_refused(const int32_t *header)
+{
+    return header[HDR_ALL] == ATTN_REPORT ? header[ATTN_MARKS + 1] == ATTN_MARK || header[ATTN_MARKS + 2] == ATTN_MARK : header[HDR_MISMATCH] != 0;
+}
 constexpr int PREFT_MAX_RANK_DEV = 128;   // must equal PREFT_MAX_RANK of the public header
 
 struct ScheduleView {

@@ -1296,7 +1296,7 @@ int preft_schedule_counts(const void *workspace, int32_t *counts, void *stream)
         return PREFT_EHIP;
     if (hipStreamSynchronize(st) != hipSuccess) return PREFT_EHIP;
     counts[0] = header[HDR_CHUNKS]; counts[1] = header[HDR_SHORT_ROWS]; counts[2] = header[HDR_ACTIVE];
-    return header[HDR_MISMATCH] ? PREFT_ESCHEDULE : PREFT_OK;
+    return schedule_refused(header) ? PREFT_ESCHEDULE : PREFT_OK;
 }
 
 const char *preft_strerror(int code)
@@ -1310,7 +1310,7 @@ const char *preft_strerror(int code)
     case PREFT_EHIP:         return "HIP runtime error (launch, copy or allocation)";
     case PREFT_ECAPACITY:    return "more distinct adapters in one batch than the slot manager has slots";
     case PREFT_ETOOLARGE:    return "batch too large for the static schedule area of preft_direft_apply_static (preft_workspace_bytes(T, S) exceeds PREFT_STATIC_SCRATCH_BYTES), or an attention call of 2^28 and more (row, head) pairs";
-    case PREFT_ESCHEDULE:    return "an apply call named another T, S, N or position set than the schedule in its workspace was built for; that call did nothing";
+    case PREFT_ESCHEDULE:    return "a call named another batch than the schedule in its workspace was built for (apply: T, S, N or position set; attention: T, S, heads, groups, type or room of the block tables); that call did nothing";
     default:                 return "unknown preft error code";
     }
 }

@@ -94,6 +94,16 @@ def test_every_row_of_random_batches_is_written_once_from_its_keys(driver, seed)
     assert all(units <= grid for _, _, _, units, grid, _ in got)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_requests_than_the_schedule_keeps_in_lds(driver, dtype):
+    rng = np.random.Generator(np.random.PCG64(7))
+    S = 4500
+    rows, kv = rng.integers(0, 3, size=S), rng.integers(0, 700, size=S)
+    answers(driver, [call(CACHED, dtype, 4, 1, rows, rng.integers(0, 2, size=S), kv, 704),
+                     call(CACHED, dtype, 8, 2, rows, None, kv, 704, [0, 100, 300, S - 900], [300, 64, 500]),
+                     call(PROMPT, dtype, 8, 2, rows, rows)])
+
+
 def test_batches_over_very_long_tables(driver):
     """Workgroups and parts are enough whatever the keys come to: many tiles over millions of tokens, and tables so long that the work of all tiles does not fit 31 bits, on both sides of
     that line."""

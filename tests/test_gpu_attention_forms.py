@@ -313,3 +313,15 @@ def test_infinite_scores_over_pages(dtype, H, Hkv, D):
     out = torch.full_like(q, 7.5)
     preft.preft_cached_attention(out, q, start, None, kvl, kc, vc, table, gs, gp, H, scale, 0, ws)
     assert out[[0, 4, 5, 6]].isnan().all() and torch.isfinite(out[1:4]).all()
+
+
+def test_more_requests_than_the_schedule_keeps_in_lds():
+    """4500 requests: the offsets of their tiles stand in memory; with and without groups."""
+    print("\n[case] 4500 requests", flush=True)
+    rng = np.random.Generator(np.random.PCG64(6))
+    S = 4500
+    kv = rng.integers(0, 60, size=S)
+    kv[::50] = rng.integers(100, 400, size=len(kv[::50]))
+    for groups, prefix, more in ((None, None, 0), ([(0, 60), (60, 2000)], [96, 72], 100)):
+        out, before, want, *_ = cached_case("bf16", 7, 1, 64, 16, rng.integers(0, 3, size=S) if groups is None else np.ones(S, int), more + kv, groups=groups, prefix=prefix)
+        print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
