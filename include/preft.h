@@ -432,7 +432,7 @@ int preft_slots_stats(const preft_slots_t *m, int64_t *stats);
  * With S = 0 (then T must be 0) nothing is written.
  *
  * preft_kv_store: k and v [T, n_kv_heads * head_dim] to the slots of slot_map[T]; rows whose slot is outside the cache (-1) are skipped.  Two rows with
- * one slot: either is kept.  k, v and the caches must not overlap.
+ * one slot: each 16 bytes of it are one's or the other's.  k, v and the caches must not overlap.
  */
 int preft_kv_plan(int64_t *slot_map, int32_t *positions, int32_t *kv_len, int32_t *block_table, int64_t ld_table,
                   int32_t max_pages, int32_t *counts, const int32_t *seg_start, const int32_t *ctx_len,
@@ -452,21 +452,24 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
  * With r of them in segment s, row i = 0..r-1 sees the first kv_len[s] - (r - 1 - i) tokens of the request, in the pages of its block table (the rows' own keys
  * are stored before).  A row that sees no token gets zeros.
  * Groups (n_groups may be 0, the tables then NULL): segments group_start[g] .. group_start[g + 1] - 1 have their first group_prefix_len[g] tokens in the same
- * pages, or in copies that hold the same values; their keys are then read once for the rows of all of them, from the first member's table.  group_start[n_groups + 1] does not decrease; segments
- * outside [group_start[0], group_start[n_groups]) are in no group.  The result is that of the call without groups, to rounding.
+ * pages, or in copies that hold the same values; their keys are then read once for the rows of all of them, from the first member's table, which has to name the pages of
+ * the whole prefix (also where that member itself has fewer tokens, or no row).  group_start[n_groups + 1] does not decrease; segments
+ * outside [group_start[0], group_start[n_groups]) are in no group.  The result is that of the call without groups, to rounding.  Reading once pays, and is done, for prefixes of
+ * 64 tokens and more that two rows or more share, and for groups whose rows are among the first 4096 rows of such groups; the rows of other groups read all of their keys themselves.
  *
  * Products are accumulated, and the softmax is computed, in fp32; in bf16 the weights p are rounded to bf16 for the product with v, and each output is
- * rounded once.  What a row does not see does not reach it, infinities and NaN included.  Of what it sees, a key whose score is -inf has the weight 0, and a row
- * that sees no others gets zeros, like one without keys (where the formula is 0 / 0); a score that is NaN or +inf makes its head's output NaN, as in the formula.
- * scale must be positive and finite.
+ * rounded once (together 0.18 to 0.23 % of the outputs' norm on random data, of which rounding the outputs alone is 0.15 to 0.17 %).  What a row does not see does not reach it,
+ * infinities and NaN included.  Of what it sees, a key whose score is -inf has the weight 0, and a row that sees no others gets zeros, like one without keys (where the formula
+ * is 0 / 0); a score that is NaN or +inf makes its head's output NaN, as in the formula.  scale must be positive and finite.
  * out must not overlap q, k, v or the caches, except that column ranges of one buffer may be side by side.  Two calls with the same arguments give the same bits.
  *
  * The workspace (16-byte aligned, preft_attention_workspace_bytes) holds the schedules of both kinds of call, each with a place of its own, and the parts of rows whose keys
- * are divided among workgroups.  One workspace serves all layers of a step, in which either kind is called, or both one after the other.
- * The schedule depends on the tables, T, S, the numbers of heads and groups, the kind of call, its type, and max_pages * page_size: with mode PREFT_SCHEDULE_READY (else 0) a call takes the one that the
- * last call of its kind left in the workspace, as the layers of a step do.  A call that names other sizes than that schedule's does nothing and
- * marks the workspace until the next schedule of its kind, which preft_schedule_counts reports as PREFT_ESCHEDULE.  (Its counts are those of work units, of joined tiles and of
- * all tiles of the schedule that was built last.)
+ * are divided among workgroups.  One workspace serves all layers of a step, in which either kind is called, or both one after the other.  Most of it is room for parts: 2048 times
+ * min(T * n_heads / n_kv_heads, 128) columns of head_dim floats (up to 130 MiB at head_dim 128), and as much again for prompts of 512 rows and more on average that are few enough to be divided.
+ * The schedule depends on the tables, T, S, the numbers of heads and groups, the kind of call, its type, and max_pages * page_size: with mode PREFT_SCHEDULE_READY (else 0) a call
+ * takes the one that the last call of its kind left in the workspace, as the layers of a step do.  A call that names others than that schedule's does nothing and marks the
+ * workspace until the next schedule of its kind, which preft_schedule_counts reports as PREFT_ESCHEDULE.  (Its counts are those of work units, of joined tiles and of all tiles of
+ * the schedule that was built last.)
  * preft_attention_workspace_bytes returns 0 for sizes that the calls refuse.
  */
 size_t preft_attention_workspace_bytes(int32_t T, int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -325,3 +325,25 @@ def test_more_requests_than_the_schedule_keeps_in_lds():
     for groups, prefix, more in ((None, None, 0), ([(0, 60), (60, 2000)], [96, 72], 100)):
         out, before, want, *_ = cached_case("bf16", 7, 1, 64, 16, rng.integers(0, 3, size=S) if groups is None else np.ones(S, int), more + kv, groups=groups, prefix=prefix)
         print(f"  {ref.check(out.cpu(), want, before):.3f} of the bound", flush=True)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D", HEADS[:4])
+def test_rows_that_see_a_key_of_infinities_are_nan(dtype, H, Hkv, D):
+    """A key that is -inf in every dimension: its score adds infinities of both signs, so that rows that see it are NaN, and the others are as by the definition."""
+    print(f"\n[case] key of -inf, {dtype} {H}/{Hkv}x{D}", flush=True)
+    td = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    T, at = 150, 70
+    q, k, v = (normal(gen, T, w * D).to(td) for w in (H, Hkv, Hkv))
+    kc, vc = (x.view(1, T, Hkv, D)[:, :144].reshape(9, 16, Hkv, D).transpose(1, 2).contiguous() for x in (k, v))
+    table = torch.arange(9, device="cuda", dtype=torch.int32)[None]
+    want = ref.prompt(q.cpu(), k.cpu(), v.cpu(), [0, at], [at], H, Hkv, D ** -0.5)
+    k[at], v[at] = -float("inf"), -float("inf")
+    kc[at // 16, :, at % 16], vc[at // 16, :, at % 16] = -float("inf"), -float("inf")
+    out, paged = torch.full_like(q, 7.5), torch.full_like(q[:144], 7.5)
+    preft.preft_prompt_attention(out, q, k, v, i32([0, T]), i32([T]), H, Hkv, D ** -0.5, 0, preft.new_attention_workspace(T, 1, H, Hkv, D))
+    preft.preft_cached_attention(paged, q[:144], i32([0, 144]), None, i32([144]), kc, vc, table, None, None, H, D ** -0.5, 0,
+                                 preft.new_attention_workspace(144, 1, H, Hkv, D))
+    for got in (out, paged):
+        print(f"  {ref.check(got[:at].cpu(), want, got[:at].cpu()):.3f} of the bound", flush=True)
+        assert got[at:].isnan().all()
