@@ -7,7 +7,7 @@
 namespace preft {
 
 // Bounds on the lists, for tables that are well-formed:
-//   column tiles   T G / 128 + one part-filled tile a segment, and the same of groups;
+//   column tiles   T G / 128 + one part-filled tile a segment, and the same of groups; of segments and groups, no more than rows have any;
 //   units          a tile of n key tiles is cut into ceil(n / range) < 1 + n / range ranges, and range is at least the estimate of all tiles' n times
 //                  kv_heads / TARGET.  That estimate, from the first and the last tile of a segment, is short by up to two a tile of a causal prompt (list), and
 //                  at least half of what counting every tile of a segment like its last gives (direct);
@@ -26,7 +26,7 @@ inline Layout layout_from(size_t at, bool parts, int64_t T, int64_t S, int64_t h
     Layout l;
     const int64_t G = heads / kv_heads, cols = T * G;
     const int64_t seg_tiles = cols / ATTN_COLS + (S < T ? S : T);
-    const int64_t tiles = groups > 0 ? 2 * seg_tiles + groups : seg_tiles;
+    const int64_t tiles = groups > 0 ? 2 * seg_tiles + (groups < T ? groups : T) : seg_tiles;
     l.tile_cap = (int32_t)tiles;
     l.unit_cap = (int32_t)(3 * tiles + 2 * ((ATTN_TARGET + kv_heads - 1) / kv_heads) + 2);
     l.merge_cap = (int32_t)seg_tiles;

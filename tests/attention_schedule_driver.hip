@@ -3,7 +3,7 @@
 // Lists are heap blocks of exactly their capacity, filled with garbage, so that with a sanitizer an access past one ends the run, and an entry that nobody wrote
 // is seen.  Standard input: KIND DTYPE T S HEADS KV_HEADS GROUPS MAX_KEYS, then seg_start[S + 1], seg_prefill_len[S] and, where KIND is 2, kv_len[S], group_start[GROUPS + 1]
 // (if GROUPS) and group_prefix_len[GROUPS].  KIND 1: prompts, 2: over pages; 11 and 12: the same on tables that are malformed, where rows may have any result, but every index has to stay
-// within bounds.  One line for each call: direct, split, join launch, units, units of the grid, entries of the join, and "ok" or what is wrong.
+// within bounds.  KIND 22: no tables follow; whether the sizes fit, the workgroups that a call over pages launches, and the capacities of its tiles, units, merges and parts.  One line for each call: direct, split, join launch, units, units of the grid, entries of the join, and "ok" or what is wrong.
 #include "emulated_hip.hpp"
 
 #include "../paper_2605_14217_amd/csrc/attention_plan.hpp"
@@ -171,6 +171,15 @@ int main()
                 if (std::scanf("%d", &x) != 1) std::exit(2);
             return v;
         };
+        if (kind == 22) {
+            AttnScheduleArgs s = {};
+            const Layout l = cached_layout(T, S, heads, kv_heads, 64, groups);
+            s.S = (int32_t)S; s.T = (int32_t)T; s.n_groups = (int32_t)groups; s.heads = (int32_t)heads; s.kv_heads = (int32_t)kv_heads; s.group = (int32_t)(heads / kv_heads);
+            s.l = lists_of(l, reinterpret_cast<void *>(4096));
+            cached_rules(s, dtype, max_keys);
+            std::printf("%d %lld %d %d %d %d ok\n", sizes_fit(T, S, heads, groups), (long long)(plan_of(s).units * kv_heads), l.tile_cap, l.unit_cap, l.merge_cap, l.slot_cap);
+            continue;
+        }
         const auto start = read(S + 1), prefill = read(S);
         const bool malformed = kind > 10;
         kind %= 10;

@@ -178,3 +178,14 @@ def test_random_tables_stay_within_the_lists(driver, seed):
     for got, b in zip(answers(driver, calls), back):
         assert got[3] <= got[4] and got[5] >= 0
         assert not b or got[3] == 0
+
+
+def test_sizes_that_are_taken_keep_grids_and_lists_in_32_bits(driver):
+    """The largest calls by every size that counts, many more groups than rows among them: workgroups and capacities stay countable."""
+    sizes = [(T, S, heads, kv_heads, groups) for T, heads in ((1, 1), (10, 1024), (1 << 17, 1024), ((1 << 18) - 1, 1024), ((1 << 28) - 1, 1), (1 << 20, 128)) for kv_heads in {1, heads}
+             for S, groups in ((1, 0), (1, (1 << 28) - 2), (T, min(T, (1 << 28) - T - 1) // 2), (min(T, (1 << 28) - 1), 0), (5, 10_000_000))]
+    lines = [f"22 {dtype} {T} {S} {heads} {kv_heads} {groups} {most}" for T, S, heads, kv_heads, groups in sizes for dtype in (BF16, F32) for most in (64, 1 << 30)]
+    taken = [g for g in answers(driver, lines) if g[0]]
+    assert len(taken) > len(lines) // 2
+    for _, workgroups, *caps in taken:
+        assert 0 < workgroups < 2 ** 32 and all(0 < c < 2 ** 31 for c in caps)
