@@ -465,8 +465,8 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
  *
  * The workspace (16-byte aligned, preft_attention_workspace_bytes) holds the schedules of both kinds of call, each with a place of its own, and the parts of rows whose keys
  * are divided among workgroups.  One workspace serves all layers of a step, in which either kind is called, or both one after the other.  Most of it is room for parts: 2048 times
- * min(T * n_heads / n_kv_heads, 128) columns of head_dim floats (up to 130 MiB at head_dim 128), and as much again for prompts of 512 rows and more on average that are few enough to be divided.
- * The schedule depends on the tables, T, S, the numbers of heads and groups, the kind of call, its type, and max_pages * page_size: with mode PREFT_SCHEDULE_READY (else 0) a call
+ * min(T * n_heads / n_kv_heads, 128) columns of head_dim floats (up to 130 MiB at head_dim 128), and 65 MiB for prompts of 512 rows and more on average that are few enough to be divided.
+ * The schedule depends on the tables, T, S, the numbers of heads and groups, the kind of call, its type, and max_pages * page_size, but not on head_dim: with mode PREFT_SCHEDULE_READY (else 0) a call
  * takes the one that the last call of its kind left in the workspace, as the layers of a step do.  A call that names others than that schedule's does nothing and marks the
  * workspace until the next schedule of its kind, which preft_schedule_counts reports as PREFT_ESCHEDULE.  (Its counts are those of work units, of joined tiles and of all tiles of
  * the schedule that was built last.)

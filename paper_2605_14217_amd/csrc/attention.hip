@@ -77,7 +77,7 @@ int preft_prompt_attention(void *out, int64_t ldo, const void *q, int64_t ldq, c
     if (rows_meet(out, ldo, wq, q, ldq, wq, T, dtype) || rows_meet(out, ldo, wq, k, ldk, wk, T, dtype) || rows_meet(out, ldo, wq, v, ldv, wk, T, dtype))
         return PREFT_EINVAL;
     if (!workspace || !aligned_workspace(workspace) || workspace_bytes < cached_layout(T, S, n_heads, n_kv_heads, head_dim, 0).end) return PREFT_EWORKSPACE;
-    const Layout l = prompt_layout(T, S, n_heads, n_kv_heads, head_dim);
+    const Layout l = prompt_layout(T, S, n_heads, n_kv_heads);
     const int64_t e = elem_bytes(dtype);
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     AttnArgs a = {};

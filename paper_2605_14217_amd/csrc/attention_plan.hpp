@@ -20,8 +20,8 @@ struct Layout {
     size_t header, units, merges, group_rows, tiles, rows_before, group_of, group_list, group_slot, group_low, part_ml, part_o, end;
 };
 
-// of one kind of call, from byte `at` on; parts: whether it has any
-inline Layout layout_from(size_t at, bool parts, int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
+// of one kind of call, from byte `at` on; slots: part columns, but those of groups' rows
+inline Layout layout_from(size_t at, int64_t slots, int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
 {
     Layout l;
     const int64_t G = heads / kv_heads, cols = T * G;
@@ -31,7 +31,7 @@ inline Layout layout_from(size_t at, bool parts, int64_t T, int64_t S, int64_t h
     l.unit_cap = (int32_t)(3 * tiles + 2 * ((ATTN_TARGET + kv_heads - 1) / kv_heads) + 2);
     l.merge_cap = (int32_t)seg_tiles;
     l.group_row_cap = groups > 0 ? (int32_t)(T < ATTN_GROUP_ROWS ? T : ATTN_GROUP_ROWS) : 0;
-    l.slot_cap = parts ? (int32_t)(4 * ATTN_TARGET * (cols < ATTN_COLS ? cols : ATTN_COLS) + 2 * l.group_row_cap * heads) : 0;
+    l.slot_cap = (int32_t)(slots + 2 * l.group_row_cap * heads);
     auto take = [&](size_t bytes) { const size_t p = at; at = (at + bytes + 63) & ~(size_t)63; return p; };
     l.header = take(HEADER_INTS * 4);
     l.units = take((size_t)l.unit_cap * sizeof(AttnUnit));
@@ -54,16 +54,20 @@ inline Layout layout_from(size_t at, bool parts, int64_t T, int64_t S, int64_t h
 // 115 uncut, cut 132; 32 heads over 8, 1200 rows: 30 uncut, cut 75).
 inline bool prompts_are_cut(int64_t tiles, int64_t kv_heads, int64_t T, int64_t S) { return tiles * kv_heads <= ATTN_TARGET / 2 && T >= 512 * S; }
 
-inline Layout prompt_layout(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D)
+// Parts have room for the largest heads, so that the other kind's schedule stands in one place: layers whose heads differ in size take the same.
+inline Layout prompt_layout(int64_t T, int64_t S, int64_t heads, int64_t kv_heads)
 {
-    const Layout l = layout_from(HEADER_INTS * 4, false, T, S, heads, kv_heads, D, 0);
-    return prompts_are_cut(l.tile_cap, kv_heads, T, S) ? layout_from(HEADER_INTS * 4, true, T, S, heads, kv_heads, D, 0) : l;
+    const Layout l = layout_from(HEADER_INTS * 4, 0, T, S, heads, kv_heads, ATTN_MAX_DIM, 0);
+    if (!prompts_are_cut(l.tile_cap, kv_heads, T, S)) return l;
+    // n tiles of all heads, up to TARGET / 2 of them, and spread = TARGET - n: n + 2 spread = 2 TARGET - n units at most (they are searched for, not listed)
+    return layout_from(HEADER_INTS * 4, 2 * ATTN_TARGET * ATTN_COLS, T, S, heads, kv_heads, ATTN_MAX_DIM, 0);
 }
 
 // ends where the workspace does
 inline Layout cached_layout(int64_t T, int64_t S, int64_t heads, int64_t kv_heads, int64_t D, int64_t groups)
 {
-    return layout_from(prompt_layout(T, S, heads, kv_heads, D).end, true, T, S, heads, kv_heads, D, groups);
+    const int64_t cols = T * (heads / kv_heads);
+    return layout_from(prompt_layout(T, S, heads, kv_heads).end, 4 * ATTN_TARGET * (cols < ATTN_COLS ? cols : ATTN_COLS), T, S, heads, kv_heads, D, groups);
 }
 
 inline AttnLists lists_of(const Layout &l, void *workspace)

@@ -13,6 +13,7 @@ namespace preft {
 constexpr int ATTN_COLS      = 128;   // columns of a unit (four wavefronts of 32)
 constexpr int ATTN_FEW_COLS  = 32;    // up to here the four wavefronts of a unit share the keys instead
 constexpr int ATTN_KEYS      = 64;    // keys of a tile
+constexpr int ATTN_MAX_DIM   = 128;   // largest head size
 constexpr int ATTN_TARGET    = 512;   // workgroups that run side by side: two on each of 256 compute units
 constexpr int ATTN_GROUP_ROWS = 4096; // rows of groups that are listed; the rest see their prefix by themselves
 constexpr int ATTN_MIN_PREFIX = 64;   // shorter prefixes are not worth a part of their own

@@ -28,7 +28,7 @@ static std::string check(int kind, int dtype, int32_t T, int32_t S, int32_t head
                          const std::vector<int32_t> &prefill, const std::vector<int32_t> &kv, const std::vector<int32_t> &gstart, const std::vector<int32_t> &gprefix,
                          bool malformed, std::string &facts)
 {
-    const Layout l = kind == 1 ? prompt_layout(T, S, heads, kv_heads, 64) : cached_layout(T, S, heads, kv_heads, 64, groups);
+    const Layout l = kind == 1 ? prompt_layout(T, S, heads, kv_heads) : cached_layout(T, S, heads, kv_heads, 64, groups);
     AttnLists x = lists_of(l, reinterpret_cast<void *>(4096));        // for its capacities
     Block<int32_t> report(HEADER_INTS), header(HEADER_INTS), tiles(S + groups + 1), rows_before(S + 1), group_of(S), group_list(groups), group_slot(groups), group_low(groups);
     Block<AttnUnit> units(l.unit_cap);
@@ -177,7 +177,10 @@ int main()
             s.S = (int32_t)S; s.T = (int32_t)T; s.n_groups = (int32_t)groups; s.heads = (int32_t)heads; s.kv_heads = (int32_t)kv_heads; s.group = (int32_t)(heads / kv_heads);
             s.l = lists_of(l, reinterpret_cast<void *>(4096));
             cached_rules(s, dtype, max_keys);
-            std::printf("%d %lld %d %d %d %d ok\n", sizes_fit(T, S, heads, groups), (long long)(plan_of(s).units * kv_heads), l.tile_cap, l.unit_cap, l.merge_cap, l.slot_cap);
+            const Layout wide = cached_layout(T, S, heads, kv_heads, 128, groups);
+            const bool one_place = l.header == wide.header && l.units == wide.units && l.group_low == wide.group_low;
+            std::printf("%d %lld %d %d %d %d %s\n", sizes_fit(T, S, heads, groups), (long long)(plan_of(s).units * kv_heads), l.tile_cap, l.unit_cap, l.merge_cap, l.slot_cap,
+                        one_place ? "ok" : "schedules of other head sizes stand elsewhere");
             continue;
         }
         const auto start = read(S + 1), prefill = read(S);

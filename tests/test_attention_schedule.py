@@ -189,3 +189,25 @@ def test_sizes_that_are_taken_keep_grids_and_lists_in_32_bits(driver):
     assert len(taken) > len(lines) // 2
     for _, workgroups, *caps in taken:
         assert 0 < workgroups < 2 ** 32 and all(0 < c < 2 ** 31 for c in caps)
+
+
+def test_schedules_stand_in_one_place_whatever_the_head_size(driver):
+    """Layers whose heads differ in size take one schedule: nothing before the lists depends on head_dim, prompts that are cut included."""
+    answers(driver, [f"22 {BF16} {T} {S} {heads} {kv_heads} {groups} 4096" for T, S in ((1, 1), (600, 1), (1200, 2), (4000, 1), (20_000, 3)) for heads, kv_heads in ((4, 1), (8, 2), (32, 8))
+                     for groups in (0, 3)])
+
+
+def test_prompts_that_are_cut_have_room_for_their_parts(driver):
+    """Few long prompts, of every number of tiles that is cut, even and uneven."""
+    rng, calls = np.random.Generator(np.random.PCG64(12)), []
+    while len(calls) < 40:
+        kv_heads, G, S = int(rng.choice([1, 2, 4, 8])), int(rng.choice([1, 2, 4, 7])), int(rng.choice([1, 1, 2, 3]))
+        most = min(2500, (256 // kv_heads - S) * 128 // G)                # tiles that fill no more than half the chip
+        if most <= 512 * S:
+            continue
+        T = int(rng.integers(512 * S, most))
+        cut = np.sort(rng.integers(0, T + 1, size=S - 1)) if rng.random() < 0.7 else np.linspace(0, T, S + 1).astype(int)[1:-1]
+        start = np.concatenate([[0], cut, [T]])
+        calls.append(call(PROMPT, int(rng.integers(0, 2)), kv_heads * G, kv_heads, None, np.diff(start) - rng.integers(0, 3, size=S), start=start, T=T))
+    got = answers(driver, calls)
+    assert sum(g[2] for g in got) >= 20 and all(units <= grid for _, _, _, units, grid, _ in got)

@@ -5,7 +5,7 @@ import torch
 
 import attention_reference as ref
 import paper_2605_14217_amd as preft
-from test_gpu_attention import HEADS, cached_case, i32, normal
+from test_gpu_attention import HEADS, cached_case, i32, normal, starts
 
 pytestmark = pytest.mark.gpu
 
@@ -347,3 +347,27 @@ def test_rows_that_see_a_key_of_infinities_are_nan(dtype, H, Hkv, D):
     for got in (out, paged):
         print(f"  {ref.check(got[:at].cpu(), want, got[:at].cpu()):.3f} of the bound", flush=True)
         assert got[at:].isnan().all()
+
+
+def test_layers_with_heads_of_two_sizes_share_their_schedules():
+    """Prompts that are divided and decode rows of one step, in layers of heads of 64, 128 and 64 again, on one workspace for the larger: the first layer builds both schedules."""
+    print("\n[case] heads of two sizes", flush=True)
+    H, Hkv, page, n, kv = 4, 1, 16, [1600, 1, 2], [1600, 700, 3000]
+    start, T, prefill = starts(n), 1603, [1600, 0, 0]
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    table = np.arange(3 * 188).reshape(3, 188)
+    ws = preft.new_attention_workspace(T, 3, H, Hkv, 128)
+    ws.fill_(0x9d)
+    for i, D in enumerate((64, 128, 64)):
+        q, k, v = (normal(gen, T, w * D).bfloat16() for w in (H, Hkv, Hkv))
+        kc, vc = (normal(gen, 3 * 188, Hkv, page, D).bfloat16() for _ in "kv")
+        out, ready = torch.full_like(q, 7.5), preft.PREFT_SCHEDULE_READY if i else 0
+        preft.preft_prompt_attention(out, q, k, v, i32(start), i32(prefill), H, Hkv, D ** -0.5, ready, ws)
+        preft.preft_cached_attention(out, q, i32(start), i32(prefill), i32(kv), kc, vc, i32(table), None, None, H, D ** -0.5, ready, ws)
+        preft.preft_schedule_counts(ws)                        # raises where a call was refused
+        want = ref.cached(q.cpu(), start, prefill, kv, kc.cpu(), vc.cpu(), table, H, D ** -0.5)
+        for t in (0, 63, 64, 900, 1599):
+            want[t] = ref.attend_row(q[t].cpu().double().view(H, D), *(x[:t + 1].cpu().double().view(t + 1, Hkv, D).transpose(0, 1) for x in (k, v)), D ** -0.5, q.dtype)
+        for t, (o, bound) in want.items():
+            assert ((out[t].cpu().double().view(H, D) - o).abs() <= bound).all(), (i, t)
+        assert not bool((out == 7.5).all(1).any())
