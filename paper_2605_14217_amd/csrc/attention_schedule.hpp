@@ -355,7 +355,7 @@ __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnSchedu
         int32_t slot = -1;
         if (d.i >= a.S) slot = a.l.group_slot[d.i - a.S] + d.col0 * a.kv_heads * d.splits;
         else if (d.parts) slot = atomicAdd(&n_slots, d.splits * step);
-        const bool fits = !d.parts || (slot >= 0 && (int64_t)slot + (int64_t)d.splits * step <= a.l.slot_cap);   // not so: the tables are malformed
+        const bool fits = !d.parts || (slot >= 0 && (int64_t)slot + (int64_t)d.splits * step <= a.l.slot_cap);   // always so: the bounds in attention_plan.hpp
         const int32_t first = d.key0 / ATTN_KEYS;
         for (int32_t k = 0; k < d.splits; ++k) {
             AttnUnit u = d.u;
@@ -497,7 +497,7 @@ __device__ __forceinline__ AttnUnit attn_unit_of(const AttnScheduleArgs &a, cons
     u.slot = -1;
     if (d.parts > 1) {
         u.slot = d.slot + col0 * d.parts * a.kv_heads + d.part * u.ncols * a.kv_heads;
-        if (u.slot < 0 || (int64_t)u.slot + (int64_t)u.ncols * a.kv_heads > a.l.slot_cap) u.ncols = 0;      // malformed tables
+        if (u.slot < 0 || (int64_t)u.slot + (int64_t)u.ncols * a.kv_heads > a.l.slot_cap) u.ncols = 0;      // never so: the bounds in attention_plan.hpp
     }
     return u;
 }
