@@ -1,0 +1,516 @@
+"""Between the projections and attention of an engine step, with 4-bit pages: the calls that these operators answer for.
+
+``rotate`` norms the heads of queries and keys and turns them by their position, in one pass over both.  ``append`` does
+that on the way into the key/value pages, values beside it.  ``append4`` does it into pages that hold 4-bit numbers with one
+power of two for every 32 of them (and reads the rows back as the values they stand for, as a program does that moves
+a request to other pages).  ``cached4`` is attention over such pages: decode rows, tokens checked ahead, chunks of a prompt.
+
+``listed`` names usual calls from the smallest to the largest and ``draw`` makes more of the same kinds.  Lengths are the
+quantiles of a uniform law, so that the work of a case does not depend on the seed; order, pages and all values do.
+With ``own`` false ``run`` computes the operators from their formulas with elementary torch operations, in 32 bits, and in 64
+bits before numbers are put on the 16 values of 4 bits, where the last bit decides between neighbours.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda:0"
+
+# op       rotate, append, append4 or cached4
+# prompts  requests with lo..hi new rows each;   decode: requests with `rows` new rows each
+# ctx_lo..ctx_hi  tokens of a request before the new rows; groups of requests share their first `prefix` tokens (cached4)
+# pad      rows of padding behind the last request: no position, no slot
+# norm     heads of q and k are normed, with weights;   rot: elements of a head that are turned;   pairs: halves or adjacent
+# keep     append: the rows of k are wanted too, beside the pages (whole prompts attend to them)
+BASE = dict(op="cached4", dtype="bf16", heads=32, kv_heads=8, dim=128, prompts=0, lo=0, hi=0, decode=0, rows=1, ctx_lo=0,
+            ctx_hi=0, groups=0, prefix=0, page=64, pad=0, norm=True, rot=128, pairs="halves", keep=False)
+
+
+def _case(name, **kw):
+    c = dict(BASE, **kw)
+    c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # a decode step of a small batch before its projections' heads go to attention
+        _case("rotate_decode_8b", op="rotate", decode=33, ctx_lo=100, ctx_hi=4000),
+        # the prompts of an ordinary mixed step at 70B width, far into long contexts
+        _case("rotate_prompts_70b", op="rotate", heads=64, prompts=9, lo=300, hi=3500, ctx_lo=0, ctx_hi=100000),
+        # one new token of a single request: latency
+        _case("append_one_8b", op="append", decode=1, ctx_lo=1500, ctx_hi=1500, page=16),
+        # proposed tokens of a small model in 32 bits, half of each head turned, neighbours paired, no norms, a padded batch
+        _case("append_ahead_f32", op="append", dtype="f32", heads=14, kv_heads=2, dim=64, decode=9, rows=5, ctx_lo=30, ctx_hi=1111,
+              page=16, pad=3, norm=False, rot=32, pairs="adjacent"),
+        # the ordinary mixed step of an 8B layer: 32 prompts of 256..2048 rows, whose keys are attended to as rows, and 224 decode rows
+        _case("append_mixed_8b", op="append", prompts=32, lo=256, hi=2048, decode=224, ctx_lo=0, ctx_hi=2000, keep=True, norm=False),
+        # decode rows of the ordinary step, to 4-bit pages
+        _case("append4_decode_8b", op="append4", decode=224, ctx_lo=256, ctx_hi=4096, page=16, pad=32, norm=False),
+        # ... and long prompts at 70B width
+        _case("append4_prompts_70b", op="append4", heads=64, prompts=7, lo=500, hi=3000, decode=100, ctx_lo=0, ctx_hi=30000),
+        # a single request, one token: latency
+        _case("cached4_one_8b", decode=1, ctx_lo=1500, ctx_hi=1500, page=16),
+        # proposed tokens checked in 32 bits on a small model
+        _case("cached4_ahead_f32", dtype="f32", heads=14, kv_heads=2, dim=64, decode=9, rows=5, ctx_lo=30, ctx_hi=1111, page=16),
+        # decode rows of the ordinary step of an 8B layer, each with a context of its own
+        _case("cached4_decode_8b", decode=224, ctx_lo=256, ctx_hi=4096),
+        # 256 requests of 8 adapters with a long system prompt each, at 70B width: prompts are shared, answers are short
+        _case("cached4_prefix_70b", heads=64, decode=256, ctx_lo=16, ctx_hi=700, groups=8, prefix=8192),
+        # further chunks of four long prompts
+        _case("cached4_chunks_8b", prompts=4, lo=900, hi=2100, ctx_lo=5000, ctx_hi=15000),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    while True:
+        c = dict(BASE)
+        c["op"] = rng.choice(["rotate", "append", "append", "append4", "append4", "cached4", "cached4", "cached4"])
+        c["dtype"] = "f32" if rng.random() < 0.25 else "bf16"
+        c["heads"], c["kv_heads"], c["dim"] = rng.choice([(32, 8, 128), (32, 8, 128), (64, 8, 128), (14, 2, 64), (8, 8, 64),
+                                                          (16, 16, 128), (12, 4, 64), (16, 1, 128)])
+        c["page"] = rng.choice([8, 16, 16, 32, 64, 64, 128])
+        c["rot"] = c["dim"]
+        if c["op"] != "cached4":
+            c["norm"] = rng.random() < 0.5
+            c["rot"] = rng.choice([c["dim"], c["dim"], c["dim"] // 2, 16, 48])
+            c["pairs"] = rng.choice(["halves", "halves", "adjacent"])
+            c["keep"] = c["op"] != "rotate" and rng.random() < 0.5
+            c["pad"] = rng.choice([0, 0, 1, 7, 40])
+        if c["op"] != "cached4" or rng.random() < 0.3:
+            c["prompts"] = _log_int(rng, 1, 64 if c["op"] != "cached4" else 6)
+            c["lo"] = _log_int(rng, 1, 2048)
+            c["hi"] = max(c["lo"], _log_int(rng, 4, 8192))
+        if c["prompts"] == 0 or rng.random() < 0.5:
+            c["decode"] = _log_int(rng, 1, 512)
+            c["rows"] = rng.choice([1, 1, 1, 2, 5, 8])
+        c["ctx_lo"] = rng.choice([0, _log_int(rng, 1, 4000)])
+        c["ctx_hi"] = c["ctx_lo"] + _log_int(rng, 1, 16000 if c["op"] == "cached4" else 120000)
+        if c["op"] == "cached4" and c["prompts"] == 0 and c["decode"] > 1 and rng.random() < 0.4:
+            c["groups"] = _log_int(rng, 1, min(c["decode"], 24))
+            c["prefix"] = c["page"] * max(1, _log_int(rng, 128, 16384) // c["page"])
+            c["ctx_hi"] = c["ctx_lo"] + _log_int(rng, 1, 1000)
+        n, ctx, _ = _lengths(c)
+        w = work(c)
+        if w["flops"] > 1.2e12 or w["bytes"] > 1.0e9:
+            continue
+        # what the plain form lays out whole: padded scores, or padded keys and values
+        if c["op"] == "cached4":
+            most = int((n + ctx).max()) + c["prefix"]
+            if len(n) * most * max(c["kv_heads"] * c["dim"], int(n.max()) * c["heads"]) > 4.0e9:
+                continue
+        return c
+
+
+def _lengths(c):
+    """New rows of each request, tokens of its own before them, and whether it is a prompt: by the case alone."""
+    u = (np.arange(c["prompts"]) + 0.5) / max(c["prompts"], 1)
+    n = np.maximum(np.rint(c["lo"] + u * (c["hi"] - c["lo"])), 1)
+    n = np.concatenate([n, np.full(c["decode"], c["rows"])]).astype(np.int64)
+    v = (np.arange(len(n)) * 0.6180339887498949 + 0.5) % 1.0
+    ctx = np.rint(c["ctx_lo"] + v * (c["ctx_hi"] - c["ctx_lo"])).astype(np.int64)
+    return n, ctx, np.arange(len(n)) < c["prompts"]
+
+
+def work(case):
+    c = case
+    n, ctx, _ = _lengths(c)
+    e = 4 if c["dtype"] == "f32" else 2
+    T, q_row, kv_row = int(n.sum()), c["heads"] * c["dim"], c["kv_heads"] * c["dim"]
+    four = 17.0 / 32                                      # bytes of a 4-bit number and its share of the scale
+    if c["op"] != "cached4":
+        # every row: q in and out, k in (and out), the sines and cosines of its position, which requests at the same one share
+        at = len(np.unique(np.concatenate([np.arange(a, a + m) for a, m in zip(ctx, n)])))
+        moved = T * (2 * q_row * e + kv_row * e + 4) + at * c["rot"] * 4
+        flops = T * (q_row + kv_row) * (3 * c["rot"] / c["dim"] + (4 if c["norm"] else 0))
+        if c["op"] == "rotate":
+            return {"bytes": moved + T * kv_row * e, "flops": flops}
+        moved += T * (kv_row * e + 8) + (T * kv_row * e if c["keep"] else 0)            # v in, slots, keys as rows
+        if c["op"] == "append":
+            return {"bytes": moved + T * 2 * kv_row * e, "flops": flops}
+        # to 4-bit pages; and out of them: the rows' slots again, their bytes in, values out
+        return {"bytes": moved + T * 2 * kv_row * four + T * (8 + 2 * kv_row * (four + e)), "flops": flops + 4.0 * T * 2 * kv_row}
+    pairs = float((n * (c["prefix"] + ctx + (n + 1) / 2.0)).sum())
+    keys = float((ctx + n).sum()) + c["prefix"] * max(c["groups"], 0)
+    tables = 4.0 * (2 * len(n) + 1 + keys / c["page"])
+    return {"bytes": keys * 2 * kv_row * four + T * e * 2 * q_row + tables, "flops": 4.0 * c["dim"] * c["heads"] * pairs}
+
+
+def _i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+
+
+def prepare(case, seed):
+    c = dict(case)
+    rng = np.random.Generator(np.random.PCG64(seed))
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(int(seed))
+    dtype = torch.float32 if c["dtype"] == "f32" else torch.bfloat16
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=gen, device=DEV, dtype=dtype)
+
+    n, ctx, prompt = _lengths(c)
+    order = rng.permutation(len(n))                       # requests stand in the batch in any order
+    n, ctx = n[order], ctx[order]
+    S, T, page, heads, kv_row = len(n), int(n.sum()), c["page"], c["heads"] * c["dim"], c["kv_heads"] * c["dim"]
+    start = np.concatenate([[0], np.cumsum(n)])
+    s = {"case": c, "S": S, "T": T + c["pad"], "most_new": int(n.max()), "host": (n, ctx, start)}
+
+    # block tables: a request's pages are anywhere in the pool, which has some to spare; whole pages of a shared prefix come first
+    shared, want = c["prefix"] // page, -(-(ctx + n) // page)
+    new = ctx // page if c["op"] != "cached4" else np.zeros_like(ctx)       # the first page that the call touches
+    most = int((want - new).max())
+    pages = rng.permutation(int((want - new).sum()) + shared * c["groups"] + 7).astype(np.int64)
+    table = np.full((S, shared + most + 3), -1, dtype=np.int64)
+    first = shared * c["groups"] + np.concatenate([[0], np.cumsum(want - new)])[:-1]
+    k = np.arange(table.shape[1] - shared)
+    mine = k[None, :] < (want - new)[:, None]
+    table[:, shared:] = np.where(mine, pages[np.where(mine, first[:, None] + k, 0)], -1)
+    if c["groups"]:
+        cut = np.round(np.linspace(0, S, c["groups"] + 1)).astype(np.int64)
+        group = np.repeat(np.arange(c["groups"]), np.diff(cut))
+        table[:, :shared] = pages[group[:, None] * shared + np.arange(shared)[None, :]]
+        s["group_start"], s["group_prefix_len"] = _i32(cut), _i32(np.full(c["groups"], shared * page))
+
+    if c["op"] == "cached4":
+        s["q"] = randn(T, heads)
+        s["k_cache"], s["v_cache"] = (_four_bit_pages(c, len(pages), gen) for _ in "kv")
+        s["block_table"], s["kv_len"], s["seg_start"] = _i32(table), _i32(c["prefix"] + ctx + n), _i32(start)
+        s["most_pages"], s["scale"] = shared + int(want.max()), 1.0 / math.sqrt(c["dim"])
+        s["out"] = torch.zeros(T, heads, dtype=dtype, device=DEV)
+        if own:                                           # the scratch memory that a serving program keeps for its steps
+            import paper_2605_14217_amd as preft
+            s["workspace"] = preft.new_attention_workspace(T, S, c["heads"], c["kv_heads"], c["dim"], c["groups"], device=DEV)
+        return s
+
+    # queries, keys and values are columns of the fused projection's output
+    qkv = randn(s["T"], heads + 2 * kv_row)
+    s["q"], s["k"], s["v"] = qkv[:, :heads], qkv[:, heads:heads + kv_row], qkv[:, heads + kv_row:]
+    request = np.repeat(np.arange(S), n)
+    at = ctx[request] + np.arange(T) - start[request]
+    none = np.full(c["pad"], -1, dtype=np.int64)
+    s["positions"] = _i32(np.concatenate([at, none]))
+    s["q_weight"], s["k_weight"] = ((1 + 0.2 * randn(c["dim"])) if c["norm"] else None for _ in "qk")
+    s["eps"] = 1e-6
+    # cosines and sines of all positions that the program serves, made once
+    reach = -(-int((ctx + n).max()) // 4096) * 4096
+    angle = torch.arange(reach, device=DEV, dtype=torch.float64)[:, None] * 500000.0 ** (-torch.arange(0, c["rot"], 2, device=DEV, dtype=torch.float64) / c["rot"])
+    s["rotation"] = torch.cat([angle.cos(), angle.sin()], 1).float()
+    s["q_out"] = torch.zeros(s["T"], heads, dtype=dtype, device=DEV)
+    s["k_out"] = torch.zeros(s["T"], kv_row, dtype=dtype, device=DEV) if c["keep"] or c["op"] == "rotate" else None
+    if c["op"] != "rotate":
+        slot = table[request, at // page - new[request]] * page + at % page
+        slot[rng.random(T) < 0.01] = -1                   # now and then a row that is not to be stored
+        s["slot_map"] = torch.from_numpy(np.concatenate([slot, none])).to(DEV)
+    if c["op"] == "append":
+        # one page more than the slots name: the plain form puts rows without a slot there
+        s["pool"] = [torch.zeros(len(pages) + 1, c["kv_heads"], page, c["dim"], dtype=dtype, device=DEV) for _ in "kv"]
+        s["k_cache"], s["v_cache"] = (p[:-1] for p in s["pool"])
+    if c["op"] == "append4":
+        s["pool"] = [torch.zeros(len(pages) + 1, c["kv_heads"], page, c["dim"] * 17 // 32, dtype=torch.uint8, device=DEV) for _ in "kv"]
+        s["k_cache"], s["v_cache"] = (p[:-1] for p in s["pool"])
+        s["k_back"], s["v_back"] = (torch.zeros(s["T"], kv_row, dtype=dtype, device=DEV) for _ in "kv")
+    return s
+
+
+def run(state):
+    s = state
+    op = s["case"]["op"]
+    if own:
+        return _OWN[op](s)
+    return _PLAIN[op](s)
+
+
+# ---- the framework's calls --------------------------------------------------------------------------------------
+
+def _pairs(s):
+    import paper_2605_14217_amd as preft
+    return preft.PREFT_PAIRS_HALVES if s["case"]["pairs"] == "halves" else preft.PREFT_PAIRS_ADJACENT
+
+
+def _own_rotate(s):
+    import paper_2605_14217_amd as preft
+    c = s["case"]
+    preft.preft_qk_rotate(s["q_out"], s["q"], s["k_out"], s["k"], s["positions"], s["rotation"], c["heads"], c["kv_heads"],
+                          s["q_weight"], s["k_weight"], s["eps"], _pairs(s))
+    return {"q": s["q_out"], "k": s["k_out"]}
+
+
+def _own_append(s):
+    import paper_2605_14217_amd as preft
+    c = s["case"]
+    preft.preft_kv_append(s["k_cache"], s["v_cache"], s["q_out"], s["q"], s["k_out"], s["k"], s["v"], s["slot_map"], s["positions"],
+                          s["rotation"], c["heads"], s["q_weight"], s["k_weight"], s["eps"], _pairs(s))
+    return _outputs(s, k_cache=s["k_cache"], v_cache=s["v_cache"])
+
+
+def _own_append4(s):
+    import paper_2605_14217_amd as preft
+    c = s["case"]
+    preft.preft_kv_append_mx4(s["k_cache"], s["v_cache"], s["q_out"], s["q"], s["k_out"], s["k"], s["v"], s["slot_map"], s["positions"],
+                              s["rotation"], c["heads"], s["q_weight"], s["k_weight"], s["eps"], _pairs(s))
+    preft.preft_kv_fetch_mx4(s["k_back"], s["v_back"], s["slot_map"], s["k_cache"], s["v_cache"])
+    return _outputs(s, k_back=s["k_back"], v_back=s["v_back"])
+
+
+def _own_cached4(s):
+    import paper_2605_14217_amd as preft
+    preft.preft_cached_attention_mx4(s["out"], s["q"], s["seg_start"], None, s["kv_len"], s["k_cache"], s["v_cache"], s["block_table"],
+                                     s.get("group_start"), s.get("group_prefix_len"), s["case"]["heads"], s["scale"], 0, s["workspace"])
+    return s["out"]
+
+
+def _outputs(s, **more):
+    out = {"q": s["q_out"], **more}
+    if s["k_out"] is not None:
+        out["k"] = s["k_out"]
+    return out
+
+
+# ---- the plain forms --------------------------------------------------------------------------------------------
+
+def _turned(s, x, weight, heads, kind):
+    """Heads of rows x, normed and turned, rounded once to the rows' type.  kind: what it is computed in."""
+    c = s["case"]
+    h = x.to(kind).reshape(s["T"], heads, c["dim"])
+    if weight is not None:
+        h = h * torch.rsqrt((h * h).mean(-1, keepdim=True) + s["eps"]) * weight.to(kind)
+    half = c["rot"] // 2
+    table = s["rotation"][s["positions"].clamp(min=0).long()].to(kind)[:, None]
+    cos, sin = table[..., :half], table[..., half:]
+    if c["pairs"] == "halves":
+        a, b = h[..., :half], h[..., half:c["rot"]]
+        h = torch.cat([a * cos - b * sin, b * cos + a * sin, h[..., c["rot"]:]], -1)
+    else:
+        a, b = h[..., 0:c["rot"]:2], h[..., 1:c["rot"]:2]
+        h = torch.cat([torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2), h[..., c["rot"]:]], -1)
+    return h.reshape(s["T"], -1).to(x.dtype)
+
+
+def _rows(s, kind):
+    """q and k as the step uses them; rows of padding stay what they were."""
+    c = s["case"]
+    real = (s["positions"] >= 0)[:, None]
+    q = _turned(s, s["q"], s["q_weight"], c["heads"], kind)
+    k = _turned(s, s["k"], s["k_weight"], c["kv_heads"], kind)
+    s["q_out"].copy_(torch.where(real, q, s["q_out"]))
+    if s["k_out"] is not None:
+        s["k_out"].copy_(torch.where(real, k, s["k_out"]))
+    return k
+
+
+def _plain_rotate(s):
+    _rows(s, torch.float32)
+    return {"q": s["q_out"], "k": s["k_out"]}
+
+
+def _slots(s):
+    """Page and place of every row; those without a slot go to the page behind the last."""
+    slot = torch.where(s["slot_map"] >= 0, s["slot_map"], s["k_cache"].shape[0] * s["case"]["page"])
+    return slot // s["case"]["page"], slot % s["case"]["page"]
+
+
+def _plain_append(s):
+    c = s["case"]
+    k = _rows(s, torch.float32)
+    at, off = _slots(s)
+    s["pool"][0][at, :, off] = k.view(-1, c["kv_heads"], c["dim"])
+    s["pool"][1][at, :, off] = s["v"].reshape(-1, c["kv_heads"], c["dim"])
+    return _outputs(s, k_cache=s["k_cache"], v_cache=s["v_cache"])
+
+
+# A page of a head: page * dim / 2 bytes of numbers, two a byte, the first in the low bits; then page * dim / 32 exponents of powers of two,
+# 127 more than they are.  A number: sign, and 0, .5, 1, 1.5, 2, 3, 4 or 6.  A power of two is the least at which the largest number
+# of its 32 is below 7, as far as there are such: from 2^-125 to 2^125.
+VALUES = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def _to_four(x):
+    """Rows [..., dim] -> bytes [..., dim / 2] and exponents [..., dim / 32]."""
+    b = x.float().unflatten(-1, (-1, 32))
+    top = b.abs().amax(-1)
+    e = (((top.view(torch.int32) + 0x200000) >> 23) - 129).clamp(-125, 125)         # from seven quarters of a power of two on: the next
+    y = b.abs().double() * ((127 - e) << 23).view(torch.float32).double()[..., None]
+    step = torch.where(y < 2, 0.5, torch.where(y < 4, 1.0, 2.0))
+    y = (torch.round(y / step) * step).clamp(max=6.0)                           # to nearest; in the middle to even
+    code = torch.where(y < 2, y * 2, torch.where(y < 4, y + 2, y / 2 + 4)).to(torch.int32) + (torch.signbit(b).int() << 3)
+    code = code.flatten(-2)
+    return (code[..., 0::2] + (code[..., 1::2] << 4)).to(torch.uint8), (e + 127).to(torch.uint8)
+
+
+def _from_four(codes, exponents):
+    """Bytes [..., dim / 2] and exponents [..., dim / 32] -> values in 32 bits [..., dim]."""
+    value = torch.tensor(VALUES + [-v for v in VALUES], device=DEV)
+    code = torch.stack([codes & 15, codes >> 4], -1).flatten(-2).int()
+    return (value[code].unflatten(-1, (-1, 32)) * (exponents.int() << 23).view(torch.float32)[..., None]).flatten(-2)
+
+
+def _parts(c, cache):
+    """The numbers [pages, heads, page, dim / 2] and the exponents [pages, heads, page, dim / 32] of a cache, as views."""
+    flat, cut = cache.view(cache.shape[0], c["kv_heads"], -1), c["page"] * c["dim"] // 2
+    return flat[..., :cut].unflatten(-1, (c["page"], -1)), flat[..., cut:].unflatten(-1, (c["page"], -1))
+
+
+def _four_bit_pages(c, n, gen):
+    """Pages of random keys or values."""
+    cache = torch.empty(n, c["kv_heads"], c["page"], c["dim"] * 17 // 32, dtype=torch.uint8, device=DEV)
+    codes, exponents = _parts(c, cache)
+    step = max(1, (1 << 26) // (c["kv_heads"] * c["page"] * c["dim"]))
+    for i in range(0, n, step):
+        x = torch.randn(min(step, n - i), c["kv_heads"], c["page"], c["dim"], generator=gen, device=DEV)
+        a, b = _to_four(x)
+        codes[i:i + step] = a
+        exponents[i:i + step] = b
+    return cache
+
+
+def _plain_append4(s):
+    c = s["case"]
+    k = _rows(s, torch.float64)
+    at, off = _slots(s)
+    real = (s["slot_map"] >= 0)[:, None]
+    keys = _back(s, s["pool"][0], k, at, off)
+    values = _back(s, s["pool"][1], s["v"], at, off)
+    s["k_back"].copy_(torch.where(real, keys, s["k_back"]))
+    s["v_back"].copy_(torch.where(real, values, s["v_back"]))
+    return _outputs(s, k_back=s["k_back"], v_back=s["v_back"])
+
+
+def _back(s, pool, x, at, off):
+    """Rows x to their slots, and out of them again."""
+    c = s["case"]
+    a, b = _to_four(x.reshape(-1, c["kv_heads"], c["dim"]))
+    codes, exponents = _parts(c, pool)
+    codes[at, :, off] = a
+    exponents[at, :, off] = b
+    return _from_four(codes[at, :, off], exponents[at, :, off]).flatten(1).to(x.dtype)
+
+
+def _plain_cached4(s):
+    c = s["case"]
+    start = s["seg_start"].long()
+    n = start[1:] - start[:-1]
+    i = torch.arange(s["most_new"], device=DEV)
+    there = i < n[:, None]
+    row = torch.where(there, start[:-1, None] + i, 0)
+    pages = s["block_table"][:, : s["most_pages"]].long().clamp(min=0)
+    k, v = _gathered(s, s["k_cache"], pages), _gathered(s, s["v_cache"], pages)
+    S, R, K, G = s["S"], s["most_new"], k.shape[2], c["heads"] // c["kv_heads"]
+    limit = s["kv_len"].long()[:, None] - n[:, None] + i + 1
+    seen = (torch.arange(K, device=DEV) < limit[..., None]) & there[..., None]
+    q = s["q"][row].float().view(S, R, c["kv_heads"], G, c["dim"]).permute(0, 2, 3, 1, 4).reshape(S, c["kv_heads"], G * R, c["dim"])
+    p = torch.matmul(q, k.transpose(2, 3).contiguous())
+    p = p.mul_(s["scale"]).view(S, c["kv_heads"], G, R, K).masked_fill_(~seen[:, None, None], -math.inf)
+    p = p.sub_(p.amax(-1, keepdim=True).clamp_(min=-3e38)).exp_()
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.view(S, c["kv_heads"], G * R, K), v).view(S, c["kv_heads"], G, R, c["dim"])
+    o = (o / total.clamp(min=1e-37)).permute(0, 3, 1, 2, 4).reshape(S, R, c["heads"] * c["dim"])
+    out = torch.zeros(s["T"] + 1, c["heads"] * c["dim"], dtype=s["q"].dtype, device=DEV)
+    out[torch.where(there, row, s["T"])] = o.to(s["q"].dtype)
+    return out[:-1]
+
+
+def _gathered(s, cache, pages):
+    """Values [S, kv_heads, keys, dim] of every request's pages."""
+    codes, exponents = _parts(s["case"], cache)
+    return _from_four(codes[pages], exponents[pages]).transpose(1, 2).flatten(2, 3).contiguous()
+
+
+_OWN = {"rotate": _own_rotate, "append": _own_append, "append4": _own_append4, "cached4": _own_cached4}
+_PLAIN = {"rotate": _plain_rotate, "append": _plain_append, "append4": _plain_append4, "cached4": _plain_cached4}
+
+
+# ---- the definitions, in 64 bits ----------------------------------------------------------------------------------
+
+def exact(case, seed):
+    c = case
+    s = prepare(case, seed)
+    if c["op"] == "cached4":
+        return _exact_cached4(c, s)
+    real = (s["positions"] >= 0).nonzero()[:, 0]
+    q, k = _exact_heads(c, s, s["q"], s["q_weight"], real), _exact_heads(c, s, s["k"], s["k_weight"], real)
+    out = {"q": torch.zeros(s["T"], q.shape[1], dtype=torch.float64, device=DEV).index_copy_(0, real, q)}
+    if s["k_out"] is not None:
+        out["k"] = torch.zeros(s["T"], k.shape[1], dtype=torch.float64, device=DEV).index_copy_(0, real, k)
+    if c["op"] == "rotate":
+        return out
+    slot = s["slot_map"][real]
+    kept = (slot >= 0).nonzero()[:, 0]
+    keys, values = k[kept], s["v"].double()[real][kept]
+    if c["op"] == "append":
+        for name, x in (("k_cache", keys), ("v_cache", values)):
+            pool = torch.zeros(s["k_cache"].shape[0] * c["page"], c["kv_heads"], c["dim"], dtype=torch.float64, device=DEV)
+            pool[slot[kept]] = x.view(-1, c["kv_heads"], c["dim"])
+            out[name] = pool.view(-1, c["page"], c["kv_heads"], c["dim"]).transpose(1, 2).contiguous()
+        return out
+    # numbers of the rows' type go onto the grid of 4 bits
+    for name, x in (("k_back", keys.to(s["k"].dtype).double()), ("v_back", values)):
+        out[name] = torch.zeros(s["T"], x.shape[1], dtype=torch.float64, device=DEV).index_copy_(0, real[kept], _exact_grid(x))
+    return out
+
+
+def _exact_heads(c, s, x, weight, real):
+    h = x[real].double().view(len(real), -1, c["dim"])
+    if weight is not None:
+        h = h / torch.sqrt(torch.sum(h ** 2, -1, keepdim=True) / c["dim"] + s["eps"]) * weight.double()
+    t = s["rotation"].double()[s["positions"][real].long()]
+    z = torch.complex(t[:, : c["rot"] // 2], t[:, c["rot"] // 2:])[:, None]
+    turn = h[..., : c["rot"]]
+    pair = turn.view(*turn.shape[:2], 2, -1).transpose(2, 3) if c["pairs"] == "halves" else turn.view(*turn.shape[:2], -1, 2)
+    pair = torch.view_as_real(torch.view_as_complex(pair.contiguous()) * z)
+    h = h.clone()
+    h[..., : c["rot"]] = (pair.transpose(2, 3) if c["pairs"] == "halves" else pair).reshape(turn.shape)
+    return h.flatten(1)
+
+
+def _exact_grid(x):
+    """The nearest of the 15 values at each 32 numbers' power of two; of two as near the one whose code is even."""
+    b = x.reshape(-1, 32)
+    m, e = torch.frexp(b.abs().amax(1))                   # top = m 2^e with 1/2 <= m < 1
+    e = torch.where(m >= 0.875, e + 1, e) - 3
+    unit = torch.exp2(torch.where(b.abs().amax(1) == 0, torch.full_like(e, -125), e).clamp(-125, 125).double())[:, None]
+    y, best, near = b.abs() / unit, torch.zeros_like(b), torch.full_like(b, math.inf)
+    for value in [0.0, 1.0, 2.0, 4.0, 0.5, 1.5, 3.0, 6.0]:                        # even codes first: they keep what they are as near to
+        d = (y - value).abs()
+        best = torch.where(d < near, value, best)
+        near = torch.minimum(near, d)
+    return (torch.copysign(best, b) * unit).view(x.shape)
+
+
+def _exact_cached4(c, s):
+    n, ctx, start = s["host"]
+    G = c["heads"] // c["kv_heads"]
+    value = torch.tensor([v * f for f in (1.0, -1.0) for v in VALUES], dtype=torch.float64, device=DEV)
+    flat = [x.view(x.shape[0], c["kv_heads"], -1) for x in (s["k_cache"], s["v_cache"])]
+    cut = c["page"] * c["dim"] // 2
+    out = torch.zeros(s["T"], c["heads"], c["dim"], dtype=torch.float64, device=DEV)
+    q = s["q"].view(s["T"], c["heads"], c["dim"])
+    for r in range(s["S"]):
+        at, rows, keys = int(start[r]), int(n[r]), c["prefix"] + int(ctx[r]) + int(n[r])
+        pages = s["block_table"][r, : -(-keys // c["page"])].long()
+        both = []
+        for f in flat:
+            page = f[pages].transpose(0, 1)               # heads, pages, bytes
+            byte = page[..., :cut].reshape(c["kv_heads"], -1, c["dim"] // 2).int()
+            x = value[torch.stack([byte % 16, byte // 16], -1).reshape(c["kv_heads"], -1, c["dim"])]
+            unit = torch.exp2(page[..., cut:].reshape(c["kv_heads"], -1, c["dim"] // 32).double() - 127)
+            both.append((x * unit.repeat_interleave(32, -1))[:, :keys])
+        hidden = torch.ones(rows, keys, dtype=torch.bool, device=DEV).triu(keys - rows + 1)
+        for h in range(c["heads"]):
+            x = (q[at:at + rows, h].double() @ both[0][h // G].t().contiguous()) / math.sqrt(c["dim"])
+            out[at:at + rows, h] = torch.softmax(x.masked_fill_(hidden, -math.inf), dim=1) @ both[1][h // G]
+    return out.view(s["T"], -1)
+
+
+if __name__ == "__main__":
+    for case in listed() + [draw(random.Random(k)) for k in range(6)]:
+        print(case.get("name", "drawn"), case, work(case))
