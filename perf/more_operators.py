@@ -256,15 +256,15 @@ def _own_append(s):
 def _own_append4(s):
     import paper_2605_14217_amd as preft
     c = s["case"]
-    preft.preft_kv_append_mx4(s["k_cache"], s["v_cache"], s["q_out"], s["q"], s["k_out"], s["k"], s["v"], s["slot_map"], s["positions"],
+    preft.preft_kv_append_mx(s["k_cache"], s["v_cache"], s["q_out"], s["q"], s["k_out"], s["k"], s["v"], s["slot_map"], s["positions"],
                               s["rotation"], c["heads"], s["q_weight"], s["k_weight"], s["eps"], _pairs(s))
-    preft.preft_kv_fetch_mx4(s["k_back"], s["v_back"], s["slot_map"], s["k_cache"], s["v_cache"])
+    preft.preft_kv_fetch_mx(s["k_back"], s["v_back"], s["slot_map"], s["k_cache"], s["v_cache"])
     return _outputs(s, k_back=s["k_back"], v_back=s["v_back"])
 
 
 def _own_cached4(s):
     import paper_2605_14217_amd as preft
-    preft.preft_cached_attention_mx4(s["out"], s["q"], s["seg_start"], None, s["kv_len"], s["k_cache"], s["v_cache"], s["block_table"],
+    preft.preft_cached_attention_mx(s["out"], s["q"], s["seg_start"], None, s["kv_len"], s["k_cache"], s["v_cache"], s["block_table"],
                                      s.get("group_start"), s.get("group_prefix_len"), s["case"]["heads"], s["scale"], 0, s["workspace"])
     return s["out"]
 
