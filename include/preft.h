@@ -443,6 +443,64 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
                    int32_t n_kv_heads, int32_t head_dim, const int64_t *slot_map, int dtype, void *stream);
 
 /*
+ * Between the q, k, v projections and attention: the heads of queries and keys are normed and turned by their position, and keys and values go to the pages.
+ *
+ *   preft_qk_rotate      rows in, rows out;
+ *   preft_kv_append      the same, and in the same pass keys and values to their slots (preft_kv_store without a launch and a trip to memory between);
+ *   preft_kv_append_mx  the same into pages of 4-bit numbers, which preft_cached_attention_mx reads;
+ *   preft_kv_fetch_mx   rows of keys and values out of such pages.
+ *
+ * Every head h of q, and every head of k, becomes
+ *   n = w * h / sqrt(mean(h^2) + eps)      with the weights w = q_weight or k_weight [head_dim], of the rows' type; NULL: n = h;
+ *   n[i], n[j] <- n[i] c - n[j] s, n[j] c + n[i] s      for the rotary_dim / 2 pairs i, j of its first rotary_dim elements; pairs says which they are:
+ *                                          PREFT_PAIRS_HALVES  p and p + rotary_dim / 2;  PREFT_PAIRS_ADJACENT  2 p and 2 p + 1;
+ * with the cosine c = rotation[position][p] and the sine s = rotation[position][rotary_dim / 2 + p], a table [n_positions, rotary_dim] in fp32, 16-byte aligned, that the caller makes
+ * once (any base, any stretching of positions).  rotary_dim: a multiple of 16, up to head_dim; 0 turns nothing (positions and rotation may then be NULL).  positions [T]: as
+ * preft_kv_plan writes them; those past the table count as its last.  A row whose position is negative is padding: nothing of it is written, in rows or pages.
+ * Computed in 64 bits from the inputs and the table, and rounded once to the rows' type (through fp32), so that a number on the border of two 4-bit numbers falls where the
+ * formula puts it.  Infinities and NaN stay within their head.
+ *
+ * q_out may be q and k_out may be k, with the same ld (in place); any other overlap is refused, except that column ranges of one buffer may be side by side.  n_heads and n_kv_heads are
+ * independent here, 0..PREFT_MAX_HEADS each (0: no such heads, the pointers are not looked at); head_dim 64 or 128; types, ld and alignment as below for attention.  Weights: 16-byte aligned.
+ *
+ * preft_kv_append, preft_kv_append_mx: k as above and v as it is go to the slots of slot_map [T]; rows whose slot is outside the cache (-1) are not stored.  The new rows of k
+ * are also written to k_out where that is not NULL (whole prompts attend to them).  Two rows with one slot: any 16 bytes (of 4-bit pages: any number, or power) are one's or the other's.
+ *
+ * 4-bit pages: a number is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6; 32 consecutive numbers of a head share a power of two (the 4-bit format of the OCP Microscaling
+ * specification: E2M1 elements, E8M0 scales).  It is the least power 2^e, -125 <= e <= 125, at which the largest of the 32 is below 7; the numbers are rounded to nearest,
+ * in the middle to even, and no larger than 6.  So a number is off by at most a fifth of itself or a quarter of the power.  Where one of the 32 is infinite or NaN, all are NaN.  What is
+ * rounded is k as preft_kv_append would store it.
+ * A cache is n_pages * n_kv_heads * page_size * (head_dim / 2 + head_dim / 32) bytes, one for keys and one for values, 16-byte aligned: page after page, of a page head after head,
+ * and of a head first the numbers of its page_size tokens (head_dim / 2 bytes each, two numbers a byte, the first in the low bits; the top bit of the four is the sign, the others are the place in the list
+ * above), then the powers of its tokens (head_dim / 32 bytes each, e + 127; 255: NaN).  That is 17/64 of the bytes of bf16 pages.
+ *
+ * preft_kv_fetch_mx: rows of k and v [T, n_kv_heads * head_dim] become the values in the slots of slot_map [T]; rows whose slot is outside the cache stay as they are.  (Every value is
+ * a bf16 number.)
+ */
+enum { PREFT_PAIRS_HALVES = 0, PREFT_PAIRS_ADJACENT = 1 };
+
+int preft_qk_rotate(void *q_out, int64_t ldqo, const void *q, int64_t ldq, void *k_out, int64_t ldko, const void *k, int64_t ldk,
+                    int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                    const void *q_weight, const void *k_weight, float eps, const int32_t *positions,
+                    const float *rotation, int32_t n_positions, int32_t rotary_dim, int pairs, int dtype, void *stream);
+
+int preft_kv_append(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_size,
+                    void *q_out, int64_t ldqo, const void *q, int64_t ldq, void *k_out, int64_t ldko, const void *k, int64_t ldk,
+                    const void *v, int64_t ldv, int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                    const int64_t *slot_map, const void *q_weight, const void *k_weight, float eps, const int32_t *positions,
+                    const float *rotation, int32_t n_positions, int32_t rotary_dim, int pairs, int dtype, void *stream);
+
+int preft_kv_append_mx(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_size,
+                        void *q_out, int64_t ldqo, const void *q, int64_t ldq, void *k_out, int64_t ldko, const void *k, int64_t ldk,
+                        const void *v, int64_t ldv, int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                        const int64_t *slot_map, const void *q_weight, const void *k_weight, float eps, const int32_t *positions,
+                        const float *rotation, int32_t n_positions, int32_t rotary_dim, int pairs, int dtype, void *stream);
+
+int preft_kv_fetch_mx(void *k, int64_t ldk, void *v, int64_t ldv, int32_t T, int32_t n_kv_heads, int32_t head_dim,
+                       const int64_t *slot_map, const void *k_cache, const void *v_cache, int32_t n_pages, int32_t page_size,
+                       int dtype, void *stream);
+
+/*
  * out[t, h] = sum_j p_j v[j, h'] / sum_j p_j,  p_j = exp(scale q[t, h] . k[j, h']), over the keys j that row t sees.
  *
  * preft_prompt_attention: the rows of a whole prompt, the first seg_prefill_len[s] of segment s; row i sees rows 0..i of its segment.

@@ -1,5 +1,6 @@
 """MI355X-native prefill-only adapter apply (segmented multi-adapter LoRA, DiReFT and LoReFT), and the attention
-side of the same engine step (pages of the key/value cache, prompt attention, attention over the pages).
+side of the same engine step (head norms and rotation, pages of the key/value cache, of activations or of 4-bit numbers, prompt attention,
+attention over the pages).
 
 The compute lives in ``libpreft.so`` (hand-written HIP for gfx950, C ABI declared in
 ``include/preft.h``); this package is the thin Python binding with the same names.
@@ -17,4 +18,5 @@ from .binding import (  # noqa: F401
     preft_slots_pool, preft_slots_resident, preft_slots_stats, PREFT_ECAPACITY,
     preft_kv_plan, preft_kv_store, preft_prompt_attention, preft_cached_attention, preft_attention_workspace_bytes,
     new_attention_workspace,
+    PREFT_PAIRS_HALVES, PREFT_PAIRS_ADJACENT, preft_qk_rotate, preft_kv_append, preft_kv_append_mx, preft_kv_fetch_mx, new_rotation, new_mx_cache,
 )

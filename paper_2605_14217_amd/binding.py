@@ -22,6 +22,8 @@ PREFT_ALL_TOKENS = 1
 PREFT_SCHEDULE_READY = 0x100
 PREFT_F32 = 0
 PREFT_BF16 = 1
+PREFT_PAIRS_HALVES = 0
+PREFT_PAIRS_ADJACENT = 1
 PREFT_ECAPACITY = -6
 PREFT_ESCHEDULE = -7
 PREFT_ETOOLARGE = -8
@@ -75,7 +77,8 @@ ABI_SYMBOLS = ("preft_workspace_bytes", "preft_workspace_bytes_z", "preft_schedu
                "preft_direft_apply", "preft_direft_apply_static", "preft_direft_apply_layers",
                "preft_loreft_prepare", "preft_loreft_apply", "preft_slots_create", "preft_slots_destroy",
                "preft_slots_store", "preft_slots_acquire", "preft_slots_pool", "preft_slots_resident",
-               "preft_slots_stats", "preft_kv_plan", "preft_kv_store", "preft_attention_workspace_bytes",
+               "preft_slots_stats", "preft_kv_plan", "preft_kv_store", "preft_qk_rotate", "preft_kv_append", "preft_kv_append_mx",
+               "preft_kv_fetch_mx", "preft_attention_workspace_bytes",
                "preft_prompt_attention", "preft_cached_attention", "preft_schedule_counts", "preft_strerror", "preft_version")
 
 _lib = None
@@ -146,6 +149,14 @@ def load_library(path: Optional[str] = None):
     lib.preft_kv_plan.argtypes = [vp, vp, vp, vp, i64, i32, vp, vp, vp, i32, i32, vp, i32, i32, vp]
     lib.preft_kv_store.restype = c.c_int
     lib.preft_kv_store.argtypes = [vp, vp, i32, i32, vp, i64, vp, i64, i32, i32, i32, vp, c.c_int, vp]
+    heads = [vp, vp, c.c_float, vp, vp, i32, i32, c.c_int, c.c_int, vp]              # weights .. stream
+    lib.preft_qk_rotate.restype = c.c_int
+    lib.preft_qk_rotate.argtypes = [vp, i64] * 4 + [i32] * 4 + heads
+    for f in (lib.preft_kv_append, lib.preft_kv_append_mx):
+        f.restype = c.c_int
+        f.argtypes = [vp, vp, i32, i32] + [vp, i64] * 5 + [i32] * 4 + [vp] + heads
+    lib.preft_kv_fetch_mx.restype = c.c_int
+    lib.preft_kv_fetch_mx.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, i32, i32, c.c_int, vp]
     lib.preft_attention_workspace_bytes.restype = sz
     lib.preft_attention_workspace_bytes.argtypes = [i32] * 6
     lib.preft_prompt_attention.restype = c.c_int
@@ -184,6 +195,8 @@ def _load_marshal(lib):
         lib.preft_direft_apply_layers)))
     _marshal.bind_attention(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.preft_kv_plan, lib.preft_kv_store, lib.preft_prompt_attention, lib.preft_cached_attention)))
+    _marshal.bind_heads(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.preft_qk_rotate, lib.preft_kv_append, lib.preft_kv_append_mx, lib.preft_kv_fetch_mx)))
     return _marshal
 
 
@@ -681,3 +694,152 @@ def preft_cached_attention(out: torch.Tensor, q: torch.Tensor, seg_start: torch.
         None if n_groups == 0 else _table(group_prefix_len, "group_prefix_len", n_groups), n_groups, float(scale), _dtype_code(out), int(mode),
         *_attention_workspace(workspace), _stream(stream))
     _check(rc, "preft_cached_attention")
+
+
+# ----------------------------------------------------------------------------------------
+# heads of queries and keys on the way to attention, and pages of 4-bit numbers
+# ----------------------------------------------------------------------------------------
+def new_rotation(n_positions: int, inv_freq, scale: float = 1.0, device="cuda") -> torch.Tensor:
+    """The table of the calls below, [n_positions, 2 * len(inv_freq)] in fp32: the cosines, then the sines, of position * inv_freq in radians (worked out in
+    64 bits), times `scale` (a stretched context's attention factor)."""
+    freq = torch.as_tensor(inv_freq, dtype=torch.float64, device=device)
+    angle = torch.arange(int(n_positions), dtype=torch.float64, device=device)[:, None] * freq
+    return (float(scale) * torch.cat([angle.cos(), angle.sin()], 1)).float()
+
+
+def new_mx_cache(n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A cache of keys, or of values, in pages of 4-bit numbers: bytes [n_pages, n_kv_heads, page_size, head_dim / 2 + head_dim / 32].  (Within a head of a page the
+    numbers of all tokens come first, then their powers: the last two dimensions are one area.)"""
+    if head_dim not in (64, 128):
+        raise ValueError("head_dim: 64 or 128")
+    return torch.zeros(int(n_pages), int(n_kv_heads), int(page_size), head_dim // 2 + head_dim // 32, dtype=torch.uint8, device=device)
+
+
+def _mx4_cache(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None):
+    """Address and head_dim."""
+    if t.dim() != 4 or not t.is_cuda or not t.is_contiguous() or t.dtype is not torch.uint8 or t.shape[3] * 32 % 17 != 0:
+        raise ValueError(f"{name}: need a contiguous uint8 device tensor as new_mx_cache makes it")
+    if like is not None and t.shape != like.shape:
+        raise ValueError("k_cache and v_cache must agree in shape")
+    return t.data_ptr(), t.shape[3] * 32 // 17
+
+
+def _turned(T: int, dim: int, dtype, positions, rotation, q_weight, k_weight):
+    """The weights and the rotation of a call, as the C ABI has them around eps: ((q_weight, k_weight), (positions, rotation, n_positions, rotary_dim))."""
+    weights = []
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and (w.dtype is not dtype or w.numel() != dim or not w.is_cuda or not w.is_contiguous()):
+            raise ValueError(f"{name}: need a contiguous device tensor of {dim} entries and the dtype of the rows")
+        weights.append(None if w is None else w.data_ptr())
+    if rotation is None:
+        return weights, (None, None, 0, 0)
+    if rotation.dim() != 2 or rotation.dtype is not _FP32 or not rotation.is_cuda or not rotation.is_contiguous():
+        raise ValueError("rotation: need a contiguous float32 device tensor [n_positions, rotary_dim]")
+    if positions is None:
+        raise ValueError("positions: needed with a rotation")
+    return weights, (_table(positions, "positions", T), rotation.data_ptr(), rotation.shape[0], rotation.shape[1])
+
+
+def _head_rows(out, x, name: str, n_heads: int, dim: int, T: Optional[int], dtype, optional: bool = False):
+    """(out, ldo, x, ldx) of heads x and what they become; zeros where x is None, and no out where it is optional."""
+    if x is None:
+        if out is not None:
+            raise ValueError(f"{name}_out without {name}")
+        return None, 0, None, 0
+    p, ld, rows, width = _matrix(x, name)
+    if width != n_heads * dim or (T is not None and rows != T) or x.dtype is not dtype:
+        raise ValueError(f"{name}: need {n_heads} heads of {dim}, in the rows and the dtype of the others")
+    if out is None and optional:
+        return None, 0, p, ld
+    po, ldo, rows_o, width_o = _matrix(out, name + "_out")
+    if rows_o != rows or width_o != width or out.dtype is not dtype:
+        raise ValueError(f"{name}_out and {name} must agree in shape and dtype")
+    return po, ldo, p, ld
+
+
+def preft_qk_rotate(q_out: Optional[torch.Tensor], q: Optional[torch.Tensor], k_out: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                    positions: Optional[torch.Tensor], rotation: Optional[torch.Tensor], n_heads: int, n_kv_heads: int,
+                    q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    pairs: int = PREFT_PAIRS_HALVES, stream=None) -> None:
+    """Norms (where there are weights) and turns the heads of q [T, n_heads * head_dim] and k [T, n_kv_heads * head_dim] by their position, into q_out and k_out, which
+    may be q and k themselves.  rotation: see new_rotation (None: no turning).  q or k may be None, with its out.  A row of a negative position stays as it is."""
+    if _native is not None:
+        rc = _native.qk_rotate(q_out, q, k_out, k, positions, rotation, n_heads, n_kv_heads, q_weight, k_weight, eps, pairs, _native_stream(stream))
+        if rc is not None:
+            return _check(rc, "preft_qk_rotate")
+    some, heads = (q, n_heads) if q is not None else (k, n_kv_heads)
+    if some is None:
+        raise ValueError("q or k: need one of them")
+    heads = int(heads)
+    T, width = _matrix(some, "q" if q is not None else "k")[2:]
+    if heads < 1 or width % heads != 0:
+        raise ValueError("n_heads, n_kv_heads: need heads of the same size in every row")
+    dim, dtype = width // heads, some.dtype
+    code = _dtype_code(some)
+    n_heads, n_kv_heads = 0 if q is None else int(n_heads), 0 if k is None else int(n_kv_heads)
+    rows = _head_rows(q_out, q, "q", n_heads, dim, T, dtype) + _head_rows(k_out, k, "k", n_kv_heads, dim, T, dtype)
+    weights, turned = _turned(T, dim, dtype, positions, rotation, q_weight, k_weight)
+    rc = load_library().preft_qk_rotate(*rows, T, n_heads, n_kv_heads, dim, *weights, float(eps), *turned, int(pairs), code, _stream(stream))
+    _check(rc, "preft_qk_rotate")
+
+
+def preft_kv_append(k_cache: torch.Tensor, v_cache: torch.Tensor, q_out: Optional[torch.Tensor], q: Optional[torch.Tensor], k_out: Optional[torch.Tensor],
+                    k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, positions: Optional[torch.Tensor], rotation: Optional[torch.Tensor], n_heads: int,
+                    q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    pairs: int = PREFT_PAIRS_HALVES, stream=None) -> None:
+    """preft_qk_rotate and preft_kv_store in one pass: the new keys, and v as it is, to the slots of slot_map; a row whose slot is -1 is not stored.  k_out None: the new keys
+    are wanted in the pages only.  q None (with its out): keys only."""
+    _append("preft_kv_append", False, k_cache, v_cache, q_out, q, k_out, k, v, slot_map, positions, rotation, n_heads, q_weight, k_weight, eps, pairs, stream)
+
+
+def preft_kv_append_mx(k_cache: torch.Tensor, v_cache: torch.Tensor, q_out: Optional[torch.Tensor], q: Optional[torch.Tensor], k_out: Optional[torch.Tensor],
+                        k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, positions: Optional[torch.Tensor], rotation: Optional[torch.Tensor], n_heads: int,
+                        q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                        pairs: int = PREFT_PAIRS_HALVES, stream=None) -> None:
+    """preft_kv_append into pages of 4-bit numbers (new_mx_cache)."""
+    _append("preft_kv_append_mx", True, k_cache, v_cache, q_out, q, k_out, k, v, slot_map, positions, rotation, n_heads, q_weight, k_weight, eps, pairs, stream)
+
+
+def _append(entry: str, mx4: bool, k_cache, v_cache, q_out, q, k_out, k, v, slot_map, positions, rotation, n_heads, q_weight, k_weight, eps, pairs, stream) -> None:
+    if _native is not None:
+        rc = _native.kv_append(mx4, k_cache, v_cache, q_out, q, k_out, k, v, slot_map, positions, rotation, n_heads, q_weight, k_weight, eps, pairs,
+                               _native_stream(stream))
+        if rc is not None:
+            return _check(rc, entry)
+    if mx4:
+        (kc, dim), (vc, _) = _mx4_cache(k_cache, "k_cache"), _mx4_cache(v_cache, "v_cache", k_cache)
+    else:
+        kc, vc, dim = _cache(k_cache, "k_cache"), _cache(v_cache, "v_cache", k_cache), k_cache.shape[3]
+    n_pages, kv_heads, page, _ = k_cache.shape
+    vp, ldv, T, width = _matrix(v, "v")
+    if width != kv_heads * dim or (not mx4 and v.dtype is not k_cache.dtype):
+        raise ValueError("k and v must agree in rows and dtype, and with the caches in heads and head size (and dtype, where they are not of 4 bits)")
+    n_heads = 0 if q is None else int(n_heads)
+    code = _dtype_code(v)
+    if k is None:
+        raise ValueError("k: need a 2-D device tensor with unit column stride")
+    rows = _head_rows(q_out, q, "q", n_heads, dim, T, v.dtype) + _head_rows(k_out, k, "k", kv_heads, dim, T, v.dtype, optional=True)
+    weights, turned = _turned(T, dim, v.dtype, positions, rotation, q_weight, k_weight)
+    if slot_map.dtype is not _INT64 or slot_map.numel() != T or not slot_map.is_cuda or not slot_map.is_contiguous():
+        raise ValueError(f"slot_map: need a contiguous int64 device tensor of {T} entries")
+    rc = getattr(load_library(), entry)(kc, vc, n_pages, page, *rows, vp, ldv, T, n_heads, kv_heads, dim, slot_map.data_ptr(), *weights, float(eps), *turned,
+                                        int(pairs), code, _stream(stream))
+    _check(rc, entry)
+
+
+def preft_kv_fetch_mx(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, stream=None) -> None:
+    """Rows of k and v ([T, n_kv_heads * head_dim]) become the values in the slots of slot_map, out of pages of 4-bit numbers; a row whose slot is -1 stays as it is."""
+    if _native is not None:
+        rc = _native.kv_fetch(k, v, slot_map, k_cache, v_cache, _native_stream(stream))
+        if rc is not None:
+            return _check(rc, "preft_kv_fetch_mx")
+    (kc, dim), (vc, _) = _mx4_cache(k_cache, "k_cache"), _mx4_cache(v_cache, "v_cache", k_cache)
+    n_pages, heads, page, _ = k_cache.shape
+    kp, ldk, T, width = _matrix(k, "k")
+    vp, ldv, T2, width2 = _matrix(v, "v")
+    if T2 != T or width != heads * dim or width2 != width or k.dtype is not v.dtype:
+        raise ValueError("k and v must agree in rows and dtype, and with the caches in heads and head size")
+    if slot_map.dtype is not _INT64 or slot_map.numel() != T or not slot_map.is_cuda or not slot_map.is_contiguous():
+        raise ValueError(f"slot_map: need a contiguous int64 device tensor of {T} entries")
+    rc = load_library().preft_kv_fetch_mx(kp, ldk, vp, ldv, T, heads, dim, slot_map.data_ptr(), kc, vc, n_pages, page, _dtype_code(k), _stream(stream))
+    _check(rc, "preft_kv_fetch_mx")

@@ -23,6 +23,9 @@ decltype(&preft_kv_plan) g_plan;
 decltype(&preft_kv_store) g_store;
 decltype(&preft_prompt_attention) g_prompt;
 decltype(&preft_cached_attention) g_cached;
+decltype(&preft_qk_rotate) g_rotate;
+decltype(&preft_kv_append) g_append, g_append4;
+decltype(&preft_kv_fetch_mx) g_fetch;
 
 const at::Tensor *tensor(PyObject *o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
 
@@ -399,7 +402,141 @@ PyObject *cached_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
     });
 }
 
-// the addresses of the four calls above
+// contiguous byte tensors [n_pages, n_kv_heads, page_size, head_dim / 2 + head_dim / 32]
+bool as_mx4_cache(PyObject *ko, PyObject *vo, Cache &c)
+{
+    const at::Tensor *k = tensor(ko), *v = tensor(vo);
+    if (!k || !v || k->dim() != 4 || !k->is_cuda() || !v->is_cuda() || !k->is_contiguous() || !v->is_contiguous() || k->sizes() != v->sizes() ||
+        k->scalar_type() != at::kByte || v->scalar_type() != at::kByte || k->size(3) * 32 % 17 != 0) return false;
+    for (int i = 0; i < 4; ++i)
+        if (k->size(i) > INT32_MAX / 32) return false;
+    c = {k->data_ptr(), v->data_ptr(), (int32_t)k->size(0), (int32_t)k->size(1), (int32_t)k->size(2), (int32_t)(k->size(3) * 32 / 17), at::kByte};
+    return true;
+}
+
+// heads and what they become; None and None: none
+struct HeadRows { Matrix out, in; };
+
+bool as_head_rows(PyObject *out, PyObject *in, int32_t heads, int32_t dim, int32_t T, at::ScalarType type, bool optional, HeadRows &r)
+{
+    r = {};
+    if (in == Py_None) return out == Py_None;
+    if (!as_matrix(in, r.in) || r.in.cols != (int64_t)heads * dim || r.in.rows != T || r.in.type != type) return false;
+    if (out == Py_None && optional) return true;
+    return as_matrix(out, r.out) && r.out.cols == r.in.cols && r.out.rows == T && r.out.type == type;
+}
+
+// (positions or None, rotation or None) and (q_weight or None, k_weight or None, eps, pairs, stream)
+struct Turned { int32_t *positions; const float *rotation; int32_t n, rot, pairs; const void *weights[2]; float eps; void *stream; };
+
+bool as_turned(PyObject *const *o, PyObject *const *w, int32_t T, int32_t dim, at::ScalarType type, Turned &t)
+{
+    t = {};
+    if (o[1] != Py_None) {
+        const at::Tensor *r = tensor(o[1]);
+        if (!r || r->dim() != 2 || r->scalar_type() != at::kFloat || !r->is_cuda() || !r->is_contiguous() || r->size(0) > INT32_MAX || r->size(1) > INT32_MAX ||
+            !as_table(o[0], T, t.positions)) return false;
+        t.rotation = static_cast<const float *>(r->data_ptr());
+        t.n = (int32_t)r->size(0);
+        t.rot = (int32_t)r->size(1);
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (w[i] == Py_None) continue;
+        const at::Tensor *x = tensor(w[i]);
+        if (!x || x->scalar_type() != type || x->numel() != dim || !x->is_cuda() || !x->is_contiguous()) return false;
+        t.weights[i] = x->data_ptr();
+    }
+    const double eps = PyFloat_AsDouble(w[2]);
+    if (eps == -1.0 && PyErr_Occurred()) return false;
+    t.eps = (float)eps;
+    return as_int(w[3], t.pairs) && as_stream(w[4], t.stream);
+}
+
+// (q_out, q, k_out, k, positions or None, rotation or None, n_heads, n_kv_heads, q_weight or None, k_weight or None, eps, pairs, stream); q or k may be None
+PyObject *qk_rotate(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        int32_t heads, kv_heads;
+        if (n != 13 || !g_rotate || !as_int(o[6], heads) || !as_int(o[7], kv_heads)) return false;
+        const bool has_q = o[1] != Py_None;
+        Matrix some;
+        if (!as_matrix(has_q ? o[1] : o[3], some)) return false;
+        const int32_t of = has_q ? heads : kv_heads;
+        if (of < 1 || some.cols % of != 0) return false;
+        const int32_t dim = some.cols / of;
+        HeadRows q, k;
+        Turned t;
+        if (!as_head_rows(o[0], o[1], heads, dim, some.rows, some.type, false, q) || !as_head_rows(o[2], o[3], kv_heads, dim, some.rows, some.type, false, k) ||
+            !as_turned(o + 4, o + 8, some.rows, dim, some.type, t)) return false;
+        if (!has_q) heads = 0;
+        if (o[3] == Py_None) kv_heads = 0;
+        rc = without_gil([&] {
+            return g_rotate(q.out.p, q.out.ld, q.in.p, q.in.ld, k.out.p, k.out.ld, k.in.p, k.in.ld, some.rows, heads, kv_heads, dim, t.weights[0], t.weights[1],
+                            t.eps, t.positions, t.rotation, t.n, t.rot, t.pairs, dtype_of(some.type), t.stream);
+        });
+        return true;
+    });
+}
+
+// (4-bit pages, k_cache, v_cache, q_out, q, k_out, k, v, slot_map, positions or None, rotation or None, n_heads, q_weight or None, k_weight or None, eps, pairs, stream);
+// q_out and q, or k_out, may be None
+PyObject *kv_append(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        if (n != 17) return false;
+        const bool mx4 = o[0] == Py_True;
+        const auto entry = mx4 ? g_append4 : g_append;
+        Cache c;
+        Matrix v;
+        HeadRows q, k;
+        Turned t;
+        int32_t heads;
+        int64_t *slots;
+        if (!entry || !(mx4 ? as_mx4_cache(o[1], o[2], c) : as_cache(o[1], o[2], c)) || !as_matrix(o[7], v) || v.cols != (int64_t)c.heads * c.dim ||
+            (!mx4 && v.type != c.type) || !as_int(o[11], heads) || o[6] == Py_None || !as_head_rows(o[3], o[4], heads, c.dim, v.rows, v.type, false, q) ||
+            !as_head_rows(o[5], o[6], c.heads, c.dim, v.rows, v.type, true, k) || !as_table(o[8], v.rows, slots) ||
+            !as_turned(o + 9, o + 12, v.rows, c.dim, v.type, t)) return false;
+        if (o[4] == Py_None) heads = 0;
+        rc = without_gil([&] {
+            return entry(c.k, c.v, c.n_pages, c.page, q.out.p, q.out.ld, q.in.p, q.in.ld, k.out.p, k.out.ld, k.in.p, k.in.ld, v.p, v.ld, v.rows, heads, c.heads,
+                         c.dim, slots, t.weights[0], t.weights[1], t.eps, t.positions, t.rotation, t.n, t.rot, t.pairs, dtype_of(v.type), t.stream);
+        });
+        return true;
+    });
+}
+
+// (k, v, slot_map, k_cache, v_cache, stream)
+PyObject *kv_fetch(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        Cache c;
+        Matrix k, v;
+        int64_t *slots;
+        void *stream;
+        if (n != 6 || !g_fetch || !as_matrix(o[0], k) || !as_matrix(o[1], v) || !as_mx4_cache(o[3], o[4], c) || k.rows != v.rows || k.cols != v.cols ||
+            k.cols != (int64_t)c.heads * c.dim || k.type != v.type || !as_table(o[2], k.rows, slots) || !as_stream(o[5], stream)) return false;
+        rc = without_gil([&] { return g_fetch(k.p, k.ld, v.p, v.ld, k.rows, c.heads, c.dim, slots, c.k, c.v, c.n_pages, c.page, dtype_of(k.type), stream); });
+        return true;
+    });
+}
+
+// the addresses of preft_qk_rotate, preft_kv_append, preft_kv_append_mx and preft_kv_fetch_mx
+PyObject *bind_heads(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    void *p[4];
+    if (n != 4) { PyErr_SetString(PyExc_TypeError, "four addresses"); return nullptr; }
+    for (int i = 0; i < 4; ++i) {
+        p[i] = PyLong_AsVoidPtr(o[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    g_rotate = reinterpret_cast<decltype(g_rotate)>(p[0]);
+    g_append = reinterpret_cast<decltype(g_append)>(p[1]);
+    g_append4 = reinterpret_cast<decltype(g_append4)>(p[2]);
+    g_fetch = reinterpret_cast<decltype(g_fetch)>(p[3]);
+    Py_RETURN_NONE;
+}
+
+// the addresses of preft_kv_plan, preft_kv_store, preft_prompt_attention and preft_cached_attention
 PyObject *bind_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
 {
     void *p[4];
@@ -455,6 +592,10 @@ PyMethodDef methods[] = {
     {"kv_store", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_store)), METH_FASTCALL, nullptr},
     {"prompt_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(prompt_attention)), METH_FASTCALL, nullptr},
     {"cached_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cached_attention)), METH_FASTCALL, nullptr},
+    {"qk_rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(qk_rotate)), METH_FASTCALL, nullptr},
+    {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_append)), METH_FASTCALL, nullptr},
+    {"kv_fetch", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_fetch)), METH_FASTCALL, nullptr},
+    {"bind_heads", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_heads)), METH_FASTCALL, nullptr},
     {"bind_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(bind_attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
