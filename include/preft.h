@@ -547,6 +547,20 @@ int preft_cached_attention(void *out, int64_t ldo, const void *q, int64_t ldq, i
                            float scale, int dtype, int mode, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * preft_cached_attention over pages of 4-bit numbers (preft_kv_append_mx): its arguments, rows, groups, workspace and schedules, with caches of the layout given there, and the formula of
+ * their values.  q and out are of type dtype; products, sums and the softmax are in fp32 (of PREFT_F32 queries and weights too: they are not rounded).  Where 32 elements of a value row are NaN, so
+ * are these of the rows that see it; infinities are not in such pages.  Power bytes that no append writes are read as they are, but 253 and 254, whose values may be infinite or NaN.
+ * A schedule is of one type of pages: layers of either kind beside each other take a workspace each.
+ */
+int preft_cached_attention_mx(void *out, int64_t ldo, const void *q, int64_t ldq, int32_t T,
+                           int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const int32_t *seg_start, const int32_t *seg_prefill_len, const int32_t *kv_len, int32_t S,
+                           const void *k_cache, const void *v_cache, int32_t n_pages, int32_t page_size,
+                           const int32_t *block_table, int64_t ld_table, int32_t max_pages,
+                           const int32_t *group_start, const int32_t *group_prefix_len, int32_t n_groups,
+                           float scale, int dtype, int mode, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Copies the schedule counters of a workspace to the host: counts[0] = multi-row work
  * units (chunks of up to 128 rows of one segment), counts[1] = rows of short segments (at most
  * 4 active rows, e.g. decode tokens), which run as gathered tiles, counts[2] = active rows.

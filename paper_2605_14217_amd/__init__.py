@@ -18,5 +18,5 @@ from .binding import (  # noqa: F401
     preft_slots_pool, preft_slots_resident, preft_slots_stats, PREFT_ECAPACITY,
     preft_kv_plan, preft_kv_store, preft_prompt_attention, preft_cached_attention, preft_attention_workspace_bytes,
     new_attention_workspace,
-    PREFT_PAIRS_HALVES, PREFT_PAIRS_ADJACENT, preft_qk_rotate, preft_kv_append, preft_kv_append_mx, preft_kv_fetch_mx, new_rotation, new_mx_cache,
+    PREFT_PAIRS_HALVES, PREFT_PAIRS_ADJACENT, preft_qk_rotate, preft_kv_append, preft_kv_append_mx, preft_kv_fetch_mx, preft_cached_attention_mx, new_rotation, new_mx_cache,
 )

@@ -78,7 +78,7 @@ ABI_SYMBOLS = ("preft_workspace_bytes", "preft_workspace_bytes_z", "preft_schedu
                "preft_loreft_prepare", "preft_loreft_apply", "preft_slots_create", "preft_slots_destroy",
                "preft_slots_store", "preft_slots_acquire", "preft_slots_pool", "preft_slots_resident",
                "preft_slots_stats", "preft_kv_plan", "preft_kv_store", "preft_qk_rotate", "preft_kv_append", "preft_kv_append_mx",
-               "preft_kv_fetch_mx", "preft_attention_workspace_bytes",
+               "preft_kv_fetch_mx", "preft_cached_attention_mx", "preft_attention_workspace_bytes",
                "preft_prompt_attention", "preft_cached_attention", "preft_schedule_counts", "preft_strerror", "preft_version")
 
 _lib = None
@@ -165,6 +165,8 @@ def load_library(path: Optional[str] = None):
     lib.preft_cached_attention.restype = c.c_int
     lib.preft_cached_attention.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp, i64, i32, vp, vp, i32,
                                            c.c_float, c.c_int, c.c_int, vp, sz, vp]
+    lib.preft_cached_attention_mx.restype = c.c_int
+    lib.preft_cached_attention_mx.argtypes = lib.preft_cached_attention.argtypes
     lib.preft_schedule_counts.restype = c.c_int
     lib.preft_schedule_counts.argtypes = [vp, c.POINTER(i32), vp]
     lib.preft_strerror.restype = c.c_char_p
@@ -196,7 +198,8 @@ def _load_marshal(lib):
     _marshal.bind_attention(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.preft_kv_plan, lib.preft_kv_store, lib.preft_prompt_attention, lib.preft_cached_attention)))
     _marshal.bind_heads(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-        lib.preft_qk_rotate, lib.preft_kv_append, lib.preft_kv_append_mx, lib.preft_kv_fetch_mx)))
+        lib.preft_qk_rotate, lib.preft_kv_append, lib.preft_kv_append_mx, lib.preft_kv_fetch_mx,
+        lib.preft_cached_attention_mx)))
     return _marshal
 
 
@@ -668,17 +671,36 @@ def preft_cached_attention(out: torch.Tensor, q: torch.Tensor, seg_start: torch.
                            workspace: torch.Tensor, stream=None) -> None:
     """Attention of the rows after the first seg_prefill_len of every segment (None: of every row) over the pages of their requests: row i of r
     sees the first kv_len - (r - 1 - i) tokens.  group_start and group_prefix_len: runs of segments that share their first tokens (None: none do)."""
+    _cached("preft_cached_attention", False, out, q, seg_start, seg_prefill_len, kv_len, k_cache, v_cache, block_table, group_start, group_prefix_len, n_heads, scale, mode,
+            workspace, stream)
+
+
+def preft_cached_attention_mx(out: torch.Tensor, q: torch.Tensor, seg_start: torch.Tensor, seg_prefill_len: Optional[torch.Tensor],
+                              kv_len: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                              group_start: Optional[torch.Tensor], group_prefix_len: Optional[torch.Tensor], n_heads: int, scale: float, mode: int,
+                              workspace: torch.Tensor, stream=None) -> None:
+    """preft_cached_attention over pages of 4-bit numbers (new_mx_cache, preft_kv_append_mx)."""
+    _cached("preft_cached_attention_mx", True, out, q, seg_start, seg_prefill_len, kv_len, k_cache, v_cache, block_table, group_start, group_prefix_len, n_heads, scale,
+            mode, workspace, stream)
+
+
+def _cached(entry: str, mx4: bool, out, q, seg_start, seg_prefill_len, kv_len, k_cache, v_cache, block_table, group_start, group_prefix_len, n_heads, scale, mode, workspace,
+            stream) -> None:
     if _native is not None:
-        rc = _native.cached_attention(out, q, seg_start, seg_prefill_len, kv_len, k_cache, v_cache, block_table, group_start, group_prefix_len,
-                                      n_heads, scale, mode, workspace, _native_stream(stream))
+        call = _native.cached_attention_mx if mx4 else _native.cached_attention
+        rc = call(out, q, seg_start, seg_prefill_len, kv_len, k_cache, v_cache, block_table, group_start, group_prefix_len,
+                  n_heads, scale, mode, workspace, _native_stream(stream))
         if rc is not None:
-            return _check(rc, "preft_cached_attention")
+            return _check(rc, entry)
     op, ldo, T, width = _matrix(out, "out")
     qp, ldq, T1, width1 = _matrix(q, "q")
-    kc, vc = _cache(k_cache, "k_cache"), _cache(v_cache, "v_cache", k_cache)
-    n_pages, kv_heads, page, dim = k_cache.shape
+    if mx4:
+        (kc, dim), (vc, _) = _mx4_cache(k_cache, "k_cache"), _mx4_cache(v_cache, "v_cache", k_cache)
+    else:
+        kc, vc, dim = _cache(k_cache, "k_cache"), _cache(v_cache, "v_cache", k_cache), k_cache.shape[3]
+    n_pages, kv_heads, page, _ = k_cache.shape
     heads = int(n_heads)
-    if T1 != T or q.dtype is not out.dtype or k_cache.dtype is not out.dtype:
+    if T1 != T or q.dtype is not out.dtype or (not mx4 and k_cache.dtype is not out.dtype):
         raise ValueError("out, q and the caches must agree in rows and dtype")
     if width != heads * dim or width1 != width:
         raise ValueError("out and q must have n_heads heads of the caches' size")
@@ -687,13 +709,13 @@ def preft_cached_attention(out: torch.Tensor, q: torch.Tensor, seg_start: torch.
     if (group_start is None) != (group_prefix_len is None):
         raise ValueError("group_start and group_prefix_len go together")
     n_groups = 0 if group_prefix_len is None else int(group_prefix_len.numel())
-    rc = load_library().preft_cached_attention(
+    rc = getattr(load_library(), entry)(
         op, ldo, qp, ldq, T, heads, kv_heads, dim, _table(seg_start, "seg_start", S + 1),
         None if seg_prefill_len is None else _table(seg_prefill_len, "seg_prefill_len", S), _table(kv_len, "kv_len", S), S, kc, vc, n_pages, page,
         table, ld, max_pages, None if n_groups == 0 else _table(group_start, "group_start", n_groups + 1),
         None if n_groups == 0 else _table(group_prefix_len, "group_prefix_len", n_groups), n_groups, float(scale), _dtype_code(out), int(mode),
         *_attention_workspace(workspace), _stream(stream))
-    _check(rc, "preft_cached_attention")
+    _check(rc, entry)
 
 
 # ----------------------------------------------------------------------------------------

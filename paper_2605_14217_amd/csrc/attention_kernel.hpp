@@ -171,7 +171,17 @@ template <typename E, int D> struct AttnColumns {
 
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
     {
-        const int lane = threadIdx.x & 63, half = lane >> 5, col = first + (lane & 31), G = a.s.group;
+        place(a, u, kv_head, first);
+        const int half = (threadIdx.x & 63) >> 5;
+        const gcptr_t from = as_global((const char *)a.q + (int64_t)row * a.ldq + head * X::ROW + half * 16);
+#pragma unroll
+        for (int s = 0; s < X::STEPS; ++s) q[s] = ld16(from + s * 32);
+    }
+
+    // everything but the queries
+    __device__ __forceinline__ void place(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
+    {
+        const int lane = threadIdx.x & 63, col = first + (lane & 31), G = a.s.group;
         valid = col < u.ncols;
         const int32_t x = u.head0 + min(col, u.ncols - 1), i = (int32_t)((uint32_t)x * a.per_head >> 21);
         head = kv_head * G + (x - i * G);
@@ -185,9 +195,6 @@ template <typename E, int D> struct AttnColumns {
         }
         row = max(0, min(row, a.s.T - 1));
         lim = min(lim, u.key1);
-        const gcptr_t from = as_global((const char *)a.q + (int64_t)row * a.ldq + head * X::ROW + half * 16);
-#pragma unroll
-        for (int s = 0; s < X::STEPS; ++s) q[s] = ld16(from + s * 32);
 #pragma unroll
         for (int b = 0; b < X::BLOCKS; ++b)
 #pragma unroll
@@ -393,8 +400,8 @@ template <typename E> __device__ __forceinline__ void store4(gptr_t p, float a, 
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }   // a row that sees no key is zero
 
 // The results of a wavefront's 32 columns, or their part.
-template <typename E, int D>
-__device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit &u, AttnColumns<E, D> &w, int kv_head, int first)
+template <typename E, int D, typename Columns>
+__device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit &u, Columns &w, int kv_head, int first)
 {
     using X = AttnTile<E, D>;
     const int lane = threadIdx.x & 63, half = lane >> 5;
@@ -432,6 +439,57 @@ __device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit 
             for (int r = 0; r < 4; ++r)
                 store4<float>(to + (b * 32 + 8 * r) * 4, w.o[b][4 * r], w.o[b][4 * r + 1], w.o[b][4 * r + 2], w.o[b][4 * r + 3]);
         if (half == 0) a.s.l.part_ml[part] = make_float2(w.m, l);
+    }
+}
+
+// The four wavefronts' sums of a unit's up to 32 columns together: results, or their part.  LDS is free once all are here.
+template <typename E, int D, typename Columns>
+__device__ __forceinline__ void join_waves(const AttnArgs &a, const AttnUnit &u, Columns &w, int kv_head, lds_t lds, float *join)
+{
+    using X = AttnTile<E, D>;
+    constexpr int PITCH = D + 4;                                  // floats between columns when they are joined: spreads the banks
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, tid = threadIdx.x;
+    // every wavefront's sums at the largest m of all
+    const float l = both_halves_sum(w.l);
+    if (half == 0) { join[wave * 32 + lane] = w.m; join[128 + wave * 32 + lane] = l; }
+    __syncthreads();                                              // and nobody reads K or V any more
+    const int col = lane & 31;
+    const float top = fmaxf(fmaxf(join[col], join[32 + col]), fmaxf(join[64 + col], join[96 + col]));
+    const float f = __builtin_amdgcn_exp2f(w.m - top);
+    PREFT_LDS float *o = (PREFT_LDS float *)lds;
+    if (col < u.ncols) {
+#pragma unroll
+        for (int b = 0; b < X::BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const f32x4_t v = {w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f};
+                *(PREFT_LDS f32x4_t *)(o + (wave * 32 + col) * PITCH + b * 32 + 8 * r + 4 * half) = v;
+            }
+    }
+    __syncthreads();
+    for (int i = tid; i < u.ncols * (D / 4); i += 256) {
+        const int cc = i / (D / 4), d = i % (D / 4) * 4;
+        const float m0 = join[cc], m1 = join[32 + cc], m2 = join[64 + cc], m3 = join[96 + cc];
+        const float mm = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+        const float ll = join[128 + cc] * __builtin_amdgcn_exp2f(m0 - mm) + join[160 + cc] * __builtin_amdgcn_exp2f(m1 - mm) +
+                         join[192 + cc] * __builtin_amdgcn_exp2f(m2 - mm) + join[224 + cc] * __builtin_amdgcn_exp2f(m3 - mm);
+        f32x4_t v = *(PREFT_LDS f32x4_t *)(o + cc * PITCH + d);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+            const f32x4_t x = *(PREFT_LDS f32x4_t *)(o + (k * 32 + cc) * PITCH + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[e];
+        }
+        if (u.slot < 0) {
+            const int32_t x = u.head0 + cc, q = (int32_t)((uint32_t)x * a.per_head >> 21), head = kv_head * a.s.group + (x - q * a.s.group);
+            const float inv = inverse(ll);
+            const int32_t row = max(0, min(u.row0 + q, a.s.T - 1));   // a group's units always have parts
+            store4<E>(as_global((char *)a.out + (int64_t)row * a.ldo + head * X::ROW + d * X::ELEM), v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        } else {
+            const int64_t part = (int64_t)u.slot + kv_head * u.ncols + cc;
+            store4<float>(as_global((void *)(a.s.l.part_o + part * D + d)), v[0], v[1], v[2], v[3]);
+            if (d == 0) a.s.l.part_ml[part] = make_float2(mm, ll);
+        }
     }
 }
 
@@ -537,8 +595,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
 {
     using X = AttnTile<E, D>;
     constexpr int HALF = X::TILE / 2, COPIES = HALF / 1024;
-    constexpr int PITCH = D + 4;                                  // floats between columns when they are joined: spreads the banks
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, tid = threadIdx.x;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     AttnSource<E, D, PAGED> src;
     src.init(a, u, kv_head);
     const lds_t kt = lds + wave * 2 * HALF, vt = kt + HALF;
@@ -612,48 +669,7 @@ __device__ __forceinline__ void attend_keys(const AttnArgs &a, const AttnUnit &u
         write_columns<E, D>(a, u, w, kv_head, 0);
         return;
     }
-    // join: every wavefront's sums at the largest m of all
-    const float l = both_halves_sum(w.l);
-    if (half == 0) { join[wave * 32 + lane] = w.m; join[128 + wave * 32 + lane] = l; }
-    __syncthreads();                                              // and nobody reads K or V any more
-    const int col = lane & 31;
-    const float top = fmaxf(fmaxf(join[col], join[32 + col]), fmaxf(join[64 + col], join[96 + col]));
-    const float f = __builtin_amdgcn_exp2f(w.m - top);
-    PREFT_LDS float *o = (PREFT_LDS float *)lds;
-    if (col < u.ncols) {
-#pragma unroll
-        for (int b = 0; b < X::BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4_t v = {w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f};
-                *(PREFT_LDS f32x4_t *)(o + (wave * 32 + col) * PITCH + b * 32 + 8 * r + 4 * half) = v;
-            }
-    }
-    __syncthreads();
-    for (int i = tid; i < u.ncols * (D / 4); i += 256) {
-        const int cc = i / (D / 4), d = i % (D / 4) * 4;
-        const float m0 = join[cc], m1 = join[32 + cc], m2 = join[64 + cc], m3 = join[96 + cc];
-        const float mm = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-        const float ll = join[128 + cc] * __builtin_amdgcn_exp2f(m0 - mm) + join[160 + cc] * __builtin_amdgcn_exp2f(m1 - mm) +
-                         join[192 + cc] * __builtin_amdgcn_exp2f(m2 - mm) + join[224 + cc] * __builtin_amdgcn_exp2f(m3 - mm);
-        f32x4_t v = *(PREFT_LDS f32x4_t *)(o + cc * PITCH + d);
-#pragma unroll
-        for (int k = 1; k < 4; ++k) {
-            const f32x4_t x = *(PREFT_LDS f32x4_t *)(o + (k * 32 + cc) * PITCH + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += x[e];
-        }
-        if (u.slot < 0) {
-            const int32_t x = u.head0 + cc, q = (int32_t)((uint32_t)x * a.per_head >> 21), head = kv_head * a.s.group + (x - q * a.s.group);
-            const float inv = inverse(ll);
-            const int32_t row = max(0, min(u.row0 + q, a.s.T - 1));   // a group's units always have parts
-            store4<E>(as_global((char *)a.out + (int64_t)row * a.ldo + head * X::ROW + d * X::ELEM), v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-        } else {
-            const int64_t part = (int64_t)u.slot + kv_head * u.ncols + cc;
-            store4<float>(as_global((void *)(a.s.l.part_o + part * D + d)), v[0], v[1], v[2], v[3]);
-            if (d == 0) a.s.l.part_ml[part] = make_float2(mm, ll);
-        }
-    }
+    join_waves<E, D>(a, u, w, kv_head, lds, join);
 }
 
 // false: the call names another batch than the schedule's, and leaves a mark

@@ -22,7 +22,7 @@ decltype(&preft_direft_apply_layers) g_layers;
 decltype(&preft_kv_plan) g_plan;
 decltype(&preft_kv_store) g_store;
 decltype(&preft_prompt_attention) g_prompt;
-decltype(&preft_cached_attention) g_cached;
+decltype(&preft_cached_attention) g_cached, g_cached_mx;
 decltype(&preft_qk_rotate) g_rotate;
 decltype(&preft_kv_append) g_append, g_append4;
 decltype(&preft_kv_fetch_mx) g_fetch;
@@ -375,33 +375,6 @@ PyObject *prompt_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
     });
 }
 
-// (out, q, seg_start, seg_prefill_len or None, kv_len, k_cache, v_cache, block_table, group_start or None, group_prefix_len or None, n_heads, scale,
-//  mode, workspace, stream)
-PyObject *cached_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
-{
-    return answer([&](int &rc) {
-        Matrix out, q;
-        Cache c;
-        Pages b;
-        int32_t heads, *start, *prefill = nullptr, *kv_len, *groups = nullptr, *prefix = nullptr;
-        Last l;
-        if (n != 15 || !g_cached || !as_matrix(o[0], out) || !as_matrix(o[1], q)) return false;
-        const int64_t S = entries(o[4]);
-        if (S < 0 || !as_table(o[2], S + 1, start) || (o[3] != Py_None && !as_table(o[3], S, prefill)) || !as_table(o[4], S, kv_len) ||
-            !as_cache(o[5], o[6], c) || !as_block_table(o[7], (int32_t)S, b) || !as_int(o[10], heads) || !as_last(o + 11, l)) return false;
-        if ((o[8] == Py_None) != (o[9] == Py_None)) return false;
-        const int64_t n_groups = o[9] == Py_None ? 0 : entries(o[9]);
-        if (n_groups < 0 || (n_groups > 0 && (!as_table(o[8], n_groups + 1, groups) || !as_table(o[9], n_groups, prefix)))) return false;
-        if (heads < 1 || out.cols != (int64_t)heads * c.dim || q.cols != out.cols || q.rows != out.rows || q.type != out.type || c.type != out.type)
-            return false;
-        rc = without_gil([&] {
-            return g_cached(out.p, out.ld, q.p, q.ld, out.rows, heads, c.heads, c.dim, start, prefill, kv_len, (int32_t)S, c.k, c.v, c.n_pages, c.page,
-                            b.p, b.ld, b.max_pages, groups, prefix, (int32_t)n_groups, l.scale, dtype_of(out.type), l.mode, l.workspace, l.bytes, l.stream);
-        });
-        return true;
-    });
-}
-
 // contiguous byte tensors [n_pages, n_kv_heads, page_size, head_dim / 2 + head_dim / 32]
 bool as_mx4_cache(PyObject *ko, PyObject *vo, Cache &c)
 {
@@ -412,6 +385,35 @@ bool as_mx4_cache(PyObject *ko, PyObject *vo, Cache &c)
         if (k->size(i) > INT32_MAX / 32) return false;
     c = {k->data_ptr(), v->data_ptr(), (int32_t)k->size(0), (int32_t)k->size(1), (int32_t)k->size(2), (int32_t)(k->size(3) * 32 / 17), at::kByte};
     return true;
+}
+
+// (out, q, seg_start, seg_prefill_len or None, kv_len, k_cache, v_cache, block_table, group_start or None, group_prefix_len or None, n_heads, scale,
+//  mode, workspace, stream)
+template <bool MX>
+PyObject *cached_attention(PyObject *, PyObject *const *o, Py_ssize_t n)
+{
+    return answer([&](int &rc) {
+        Matrix out, q;
+        Cache c;
+        Pages b;
+        int32_t heads, *start, *prefill = nullptr, *kv_len, *groups = nullptr, *prefix = nullptr;
+        Last l;
+        const auto entry = MX ? g_cached_mx : g_cached;
+        if (n != 15 || !entry || !as_matrix(o[0], out) || !as_matrix(o[1], q)) return false;
+        const int64_t S = entries(o[4]);
+        if (S < 0 || !as_table(o[2], S + 1, start) || (o[3] != Py_None && !as_table(o[3], S, prefill)) || !as_table(o[4], S, kv_len) ||
+            !(MX ? as_mx4_cache(o[5], o[6], c) : as_cache(o[5], o[6], c)) || !as_block_table(o[7], (int32_t)S, b) || !as_int(o[10], heads) || !as_last(o + 11, l)) return false;
+        if ((o[8] == Py_None) != (o[9] == Py_None)) return false;
+        const int64_t n_groups = o[9] == Py_None ? 0 : entries(o[9]);
+        if (n_groups < 0 || (n_groups > 0 && (!as_table(o[8], n_groups + 1, groups) || !as_table(o[9], n_groups, prefix)))) return false;
+        if (heads < 1 || out.cols != (int64_t)heads * c.dim || q.cols != out.cols || q.rows != out.rows || q.type != out.type || (!MX && c.type != out.type))
+            return false;
+        rc = without_gil([&] {
+            return entry(out.p, out.ld, q.p, q.ld, out.rows, heads, c.heads, c.dim, start, prefill, kv_len, (int32_t)S, c.k, c.v, c.n_pages, c.page,
+                            b.p, b.ld, b.max_pages, groups, prefix, (int32_t)n_groups, l.scale, dtype_of(out.type), l.mode, l.workspace, l.bytes, l.stream);
+        });
+        return true;
+    });
 }
 
 // heads and what they become; None and None: none
@@ -520,12 +522,12 @@ PyObject *kv_fetch(PyObject *, PyObject *const *o, Py_ssize_t n)
     });
 }
 
-// the addresses of preft_qk_rotate, preft_kv_append, preft_kv_append_mx and preft_kv_fetch_mx
+// the addresses of preft_qk_rotate, preft_kv_append, preft_kv_append_mx, preft_kv_fetch_mx and preft_cached_attention_mx
 PyObject *bind_heads(PyObject *, PyObject *const *o, Py_ssize_t n)
 {
-    void *p[4];
-    if (n != 4) { PyErr_SetString(PyExc_TypeError, "four addresses"); return nullptr; }
-    for (int i = 0; i < 4; ++i) {
+    void *p[5];
+    if (n != 5) { PyErr_SetString(PyExc_TypeError, "five addresses"); return nullptr; }
+    for (int i = 0; i < 5; ++i) {
         p[i] = PyLong_AsVoidPtr(o[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -533,6 +535,7 @@ PyObject *bind_heads(PyObject *, PyObject *const *o, Py_ssize_t n)
     g_append = reinterpret_cast<decltype(g_append)>(p[1]);
     g_append4 = reinterpret_cast<decltype(g_append4)>(p[2]);
     g_fetch = reinterpret_cast<decltype(g_fetch)>(p[3]);
+    g_cached_mx = reinterpret_cast<decltype(g_cached_mx)>(p[4]);
     Py_RETURN_NONE;
 }
 
@@ -591,7 +594,8 @@ PyMethodDef methods[] = {
     {"kv_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_plan)), METH_FASTCALL, nullptr},
     {"kv_store", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_store)), METH_FASTCALL, nullptr},
     {"prompt_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(prompt_attention)), METH_FASTCALL, nullptr},
-    {"cached_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cached_attention)), METH_FASTCALL, nullptr},
+    {"cached_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cached_attention<false>)), METH_FASTCALL, nullptr},
+    {"cached_attention_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(cached_attention<true>)), METH_FASTCALL, nullptr},
     {"qk_rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(qk_rotate)), METH_FASTCALL, nullptr},
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_append)), METH_FASTCALL, nullptr},
     {"kv_fetch", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(kv_fetch)), METH_FASTCALL, nullptr},

@@ -76,6 +76,28 @@ def test_fetch_refusals(lib):
     assert fetch(lib, T=0) == 0 and fetch(lib, n_pages=0) == 0
 
 
+def cached(lib, out=A, ldo=1024, q=B, ldq=1024, T=100, H=8, Hkv=2, D=128, start=E, prefill=None, kv=E, S=4, kc=C, vc=D_, n_pages=50, page=16, table=E,
+           ld=20, max_pages=20, gs=None, gp=None, groups=0, scale=0.1, dtype=1, mode=0, ws=W, wsb=1 << 40):
+    return lib.preft_cached_attention_mx(out, ldo, q, ldq, T, H, Hkv, D, start, prefill, kv, S, kc, vc, n_pages, page, table, ld, max_pages, gs, gp, groups,
+                                         scale, dtype, mode, ws, wsb, None)
+
+
+def test_attention_refusals(lib):
+    size = 50 * 16 * 2 * 68
+    for bad in (dict(T=-1), dict(S=-1), dict(groups=-1), dict(H=9), dict(dtype=-1), dict(dtype=0x11), dict(mode=2), dict(scale=0.0), dict(n_pages=-1), dict(max_pages=-1),
+                dict(ld=19), dict(start=None), dict(kv=None), dict(groups=1), dict(groups=1, gs=E), dict(out=None), dict(q=None), dict(kc=None),
+                dict(vc=None), dict(table=None), dict(q=A), dict(out=C), dict(out=C + size - 16), dict(out=D_ + 64)):
+        assert cached(lib, **bad) == -1, bad
+    assert cached(lib, out=C + size, ws=None) == -4            # right behind the cache
+    for bad in (dict(D=80), dict(page=0), dict(page=100)):
+        assert cached(lib, **bad) == -2, bad
+    for bad in (dict(kc=C + 8), dict(q=B + 8), dict(ldo=1025)):
+        assert cached(lib, **bad) == -3, bad
+    assert cached(lib, ws=None) == -4 and cached(lib, wsb=100) == -4 and cached(lib, ws=W + 4) == -4
+    assert cached(lib, T=1 << 28) == -8
+    assert cached(lib, T=0) == 0 and cached(lib, S=0) == 0
+
+
 def test_binding_refuses_what_is_no_device_tensor():
     t, i = torch.zeros(4, 128), torch.zeros(4, dtype=torch.int32)
     cache, four = torch.zeros(2, 2, 16, 64), preft.new_mx_cache(2, 2, 16, 64, device="cpu")
@@ -93,6 +115,8 @@ def test_binding_refuses_what_is_no_device_tensor():
             preft.preft_kv_append_mx(c, c, None, None, None, t, t, i.long(), i, t, 2, stream=0)
         with pytest.raises(ValueError, match="k_cache: need a contiguous uint8 device tensor"):
             preft.preft_kv_fetch_mx(t, t, i.long(), c, c, stream=0)
+    with pytest.raises(ValueError, match="out: need a 2-D device tensor"):
+        preft.preft_cached_attention_mx(t, t, i, None, i[:2], four, four, i[None], None, None, 2, 0.1, 0, four, stream=0)
 
 
 def test_marshalling_declines_what_is_no_ordinary_call():
@@ -105,6 +129,7 @@ def test_marshalling_declines_what_is_no_ordinary_call():
     assert native.qk_rotate(None, None, None, None, i, t, 2, 2, None, None, 1e-6, 0, 0) is None
     for mx4, c in ((False, cache), (True, four), (True, cache), (False, None)):
         assert native.kv_append(mx4, c, c, None, None, None, t, t, i.long(), i, t, 2, None, None, 1e-6, 0, 0) is None
+    assert native.cached_attention_mx(t, t, i, None, i, four, four, i[None], None, None, 2, 0.1, 0, four, 0) is None and native.cached_attention_mx(t) is None
     assert native.kv_append() is None and native.kv_fetch(t, t, i.long(), four, four, 0) is None and native.kv_fetch(1) is None
     with pytest.raises(TypeError):
         native.bind_heads(1)
