@@ -19,11 +19,11 @@ HIPCC_FLAGS = [
 
 def sources():
     """preft_api.hip (the C ABI of the apply calls, the launch logic and the few kernels it instantiates itself), slots.hip,
-    kv_pages.hip, kv_append.hip and attention.hip (pages, head norms and rotation on the way to them, attention, each with its entry points), and the kernel instantiations of
+    kv_pages.hip, kv_append.hip, attention.hip and attention_mx.hip (pages, head norms and rotation on the way to them, attention, with their entry points), and the kernel instantiations of
     csrc/instances/ (written by csrc/gen_instances.py)."""
     inst = os.path.join(CSRC, "instances")
     groups = sorted(os.path.join(inst, n) for n in os.listdir(inst) if n.endswith(".hip")) if os.path.isdir(inst) else []
-    return [os.path.join(CSRC, n) for n in ("preft_api.hip", "slots.hip", "kv_pages.hip", "kv_append.hip", "attention.hip")] + groups
+    return [os.path.join(CSRC, n) for n in ("preft_api.hip", "slots.hip", "kv_pages.hip", "kv_append.hip", "attention.hip", "attention_mx.hip")] + groups
 
 
 def built_for() -> str:

@@ -3,7 +3,7 @@
 
 #include "attention_common.hpp"
 #include "attention_kernel.hpp"
-#include "attention_mx_kernel.hpp"
+#include "attention_mx.hpp"
 #include "attention_plan.hpp"
 
 #include <cmath>
@@ -18,7 +18,7 @@ template <typename E, int D, int KEYS, bool DIRECT>
 int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)(p.units * a.s.kv_heads));
-    if constexpr (KEYS == MX_PAGES) hipLaunchKernelGGL((attention_mx_kernel<E, D, DIRECT>), grid, dim3(256), 0, st, a);
+    if constexpr (KEYS == MX_PAGES) launch_mx_attention(a, (int)sizeof(E), D, DIRECT, grid, st);
     else hipLaunchKernelGGL((attention_kernel<E, D, KEYS == PAGES, DIRECT>), grid, dim3(256), 0, st, a);
     if (p.merge) {
         const unsigned tiles = (unsigned)(a.s.l.merge_cap < 1024 ? a.s.l.merge_cap : 1024);

@@ -157,6 +157,28 @@ template <typename E, int D, bool PAGED> struct AttnSource {
     }
 };
 
+struct AttnQuery { int32_t row, head, lim; bool valid; };
+// column `col` of a unit: its query, and the keys it sees
+__device__ __forceinline__ AttnQuery attn_query(const AttnArgs &a, const AttnUnit &u, int kv_head, int col)
+{
+    AttnQuery r;
+    const int G = a.s.group;
+    r.valid = col < u.ncols;
+    const int32_t x = u.head0 + min(col, u.ncols - 1), i = (int32_t)((uint32_t)x * a.per_head >> 21);
+    r.head = kv_head * G + (x - i * G);
+    if (u.row0 >= 0) {
+        r.row = u.row0 + i;
+        r.lim = u.lim0 + i;
+    } else {
+        const int2 e = a.s.l.group_rows[min(-1 - u.row0 + i, a.s.l.group_row_cap - 1)];
+        r.row = e.x;
+        r.lim = e.y;
+    }
+    r.row = max(0, min(r.row, a.s.T - 1));
+    r.lim = min(r.lim, u.key1);
+    return r;
+}
+
 // ---------------------------------------------------------------------------------------
 // 32 columns of a wavefront
 // ---------------------------------------------------------------------------------------
@@ -181,20 +203,8 @@ template <typename E, int D> struct AttnColumns {
     // everything but the queries
     __device__ __forceinline__ void place(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
     {
-        const int lane = threadIdx.x & 63, col = first + (lane & 31), G = a.s.group;
-        valid = col < u.ncols;
-        const int32_t x = u.head0 + min(col, u.ncols - 1), i = (int32_t)((uint32_t)x * a.per_head >> 21);
-        head = kv_head * G + (x - i * G);
-        if (u.row0 >= 0) {
-            row = u.row0 + i;
-            lim = u.lim0 + i;
-        } else {
-            const int2 r = a.s.l.group_rows[min(-1 - u.row0 + i, a.s.l.group_row_cap - 1)];
-            row = r.x;
-            lim = r.y;
-        }
-        row = max(0, min(row, a.s.T - 1));
-        lim = min(lim, u.key1);
+        const AttnQuery r = attn_query(a, u, kv_head, first + (threadIdx.x & 31));
+        row = r.row; head = r.head; lim = r.lim; valid = r.valid;
 #pragma unroll
         for (int b = 0; b < X::BLOCKS; ++b)
 #pragma unroll
@@ -208,6 +218,21 @@ template <typename E, int D> struct AttnColumns {
     {
 #pragma unroll
         for (int s = 0; s < X::STEPS; ++s) asm volatile("" : "+v"(q[s]));
+    }
+
+    static constexpr int COLS = 32;
+    __device__ __forceinline__ float total() const { return both_halves_sum(l); }
+    // this lane's share of its column's sums, times f
+    __device__ __forceinline__ void put(PREFT_LDS float *to, float f) const
+    {
+        const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int b = 0; b < X::BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const f32x4_t v = {o[b][4 * r] * f, o[b][4 * r + 1] * f, o[b][4 * r + 2] * f, o[b][4 * r + 3] * f};
+                *(PREFT_LDS f32x4_t *)(to + b * 32 + 8 * r + 4 * half) = v;
+            }
     }
 
     // S^T of 32 keys from row `row0` of the K tile on
@@ -442,41 +467,33 @@ __device__ __forceinline__ void write_columns(const AttnArgs &a, const AttnUnit 
     }
 }
 
-// The four wavefronts' sums of a unit's up to 32 columns together: results, or their part.  LDS is free once all are here.
+// The four wavefronts' sums of a unit's up to Columns::COLS columns together: results, or their part.  LDS is free once all are here.
 template <typename E, int D, typename Columns>
 __device__ __forceinline__ void join_waves(const AttnArgs &a, const AttnUnit &u, Columns &w, int kv_head, lds_t lds, float *join)
 {
     using X = AttnTile<E, D>;
-    constexpr int PITCH = D + 4;                                  // floats between columns when they are joined: spreads the banks
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, tid = threadIdx.x;
+    constexpr int PITCH = D + 4, COLS = Columns::COLS;            // floats between columns when they are joined: spreads the banks
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, tid = threadIdx.x;
     // every wavefront's sums at the largest m of all
-    const float l = both_halves_sum(w.l);
-    if (half == 0) { join[wave * 32 + lane] = w.m; join[128 + wave * 32 + lane] = l; }
+    const float l = w.total();
+    if (lane < COLS) { join[wave * COLS + lane] = w.m; join[(4 + wave) * COLS + lane] = l; }
     __syncthreads();                                              // and nobody reads K or V any more
-    const int col = lane & 31;
-    const float top = fmaxf(fmaxf(join[col], join[32 + col]), fmaxf(join[64 + col], join[96 + col]));
+    const int col = lane % COLS;
+    const float top = fmaxf(fmaxf(join[col], join[COLS + col]), fmaxf(join[2 * COLS + col], join[3 * COLS + col]));
     const float f = __builtin_amdgcn_exp2f(w.m - top);
     PREFT_LDS float *o = (PREFT_LDS float *)lds;
-    if (col < u.ncols) {
-#pragma unroll
-        for (int b = 0; b < X::BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4_t v = {w.o[b][4 * r] * f, w.o[b][4 * r + 1] * f, w.o[b][4 * r + 2] * f, w.o[b][4 * r + 3] * f};
-                *(PREFT_LDS f32x4_t *)(o + (wave * 32 + col) * PITCH + b * 32 + 8 * r + 4 * half) = v;
-            }
-    }
+    if (col < u.ncols) w.put(o + (wave * COLS + col) * PITCH, f);
     __syncthreads();
     for (int i = tid; i < u.ncols * (D / 4); i += 256) {
         const int cc = i / (D / 4), d = i % (D / 4) * 4;
-        const float m0 = join[cc], m1 = join[32 + cc], m2 = join[64 + cc], m3 = join[96 + cc];
+        const float m0 = join[cc], m1 = join[COLS + cc], m2 = join[2 * COLS + cc], m3 = join[3 * COLS + cc];
         const float mm = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-        const float ll = join[128 + cc] * __builtin_amdgcn_exp2f(m0 - mm) + join[160 + cc] * __builtin_amdgcn_exp2f(m1 - mm) +
-                         join[192 + cc] * __builtin_amdgcn_exp2f(m2 - mm) + join[224 + cc] * __builtin_amdgcn_exp2f(m3 - mm);
+        const float ll = join[4 * COLS + cc] * __builtin_amdgcn_exp2f(m0 - mm) + join[5 * COLS + cc] * __builtin_amdgcn_exp2f(m1 - mm) +
+                         join[6 * COLS + cc] * __builtin_amdgcn_exp2f(m2 - mm) + join[7 * COLS + cc] * __builtin_amdgcn_exp2f(m3 - mm);
         f32x4_t v = *(PREFT_LDS f32x4_t *)(o + cc * PITCH + d);
 #pragma unroll
         for (int k = 1; k < 4; ++k) {
-            const f32x4_t x = *(PREFT_LDS f32x4_t *)(o + (k * 32 + cc) * PITCH + d);
+            const f32x4_t x = *(PREFT_LDS f32x4_t *)(o + (k * COLS + cc) * PITCH + d);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }

@@ -40,6 +40,47 @@ __device__ __forceinline__ Thirds thirds(float v)
 // the upper halves of two numbers
 __device__ __forceinline__ uint32_t upper_halves(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
 
+// eight elements of a query, as they go to the matrix cores
+template <typename E, int PARTS, int STEPS> __device__ __forceinline__ void mx_query(gcptr_t from, u32x4_t (&q)[PARTS][STEPS], int t)
+{
+    if constexpr (sizeof(E) == 2) {
+        q[0][t] = ld16(from);
+    } else {
+        const u32x4_t lo = ld16(from), hi = ld16(from + 16);
+        auto cut = [](uint32_t bits) {
+            const float v = __uint_as_float(bits);
+            if (__builtin_isfinite(v)) return thirds(v);
+            return Thirds{{__uint_as_float(v != v ? 0x7fc00000u : bits), 0.0f, 0.0f}};
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32x4_t &two = i < 2 ? lo : hi;
+            const Thirds x = cut(two[2 * i & 3]), y = cut(two[(2 * i & 3) + 1]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) q[p][t][i] = upper_halves(x.part[p], y.part[p]);
+        }
+    }
+}
+// two weights likewise: put(part, both)
+template <int PARTS, typename Put> __device__ __forceinline__ void mx_weights(float x, float y, Put put)
+{
+    if constexpr (PARTS == 1) {
+        put(0, pack_bf16(x, y));
+    } else {
+        const Thirds xs = thirds(x), ys = thirds(y);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) put(k, upper_halves(xs.part[k], ys.part[k]));
+    }
+}
+// of 32 keys from `key` on, those that a column sees
+__device__ __forceinline__ uint32_t seen_keys(int32_t lim, int32_t key, int32_t key0)
+{
+    const int32_t from = max(key0 - key, 0), to = max(0, min(lim - key, 32));
+    return (to >= 32 ? ~0u : (1u << to) - 1) & (from >= 32 ? 0u : ~0u << from);
+}
+
+constexpr int MX_FEW_COLS = 16;        // up to here a unit's columns are one tile of 16
+
 template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
     using X = MxTile<D>;
     using Base = AttnColumns<E, D>;
@@ -52,26 +93,9 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
         Base::place(a, u, kv_head, first);
         const int half = (threadIdx.x & 63) >> 5;
         const gcptr_t from = as_global((const char *)a.q + (int64_t)this->row * a.ldq + (int64_t)this->head * D * sizeof(E) + half * (D / 2) * (int)sizeof(E));
-        if constexpr (PARTS == 1) {
 #pragma unroll
-            for (int t = 0; t < X::STEPS; ++t) qp[0][t] = ld16(from + t * 16);
-        } else {
-#pragma unroll
-            for (int t = 0; t < X::STEPS; ++t) {
-                const u32x4_t lo = ld16(from + t * 32), hi = ld16(from + t * 32 + 16);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const u32x4_t &two = i < 2 ? lo : hi;
-                    Thirds x = thirds(__uint_as_float(two[2 * i & 3])), y = thirds(__uint_as_float(two[(2 * i & 3) + 1]));
-                    if (!__builtin_isfinite(x.part[0])) x = whole(__uint_as_float(two[2 * i & 3]));
-                    if (!__builtin_isfinite(y.part[0])) y = whole(__uint_as_float(two[(2 * i & 3) + 1]));
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) qp[p][t][i] = upper_halves(x.part[p], y.part[p]);
-                }
-            }
-        }
+        for (int t = 0; t < X::STEPS; ++t) mx_query<E>(from + t * 8 * (int)sizeof(E), qp, t);
     }
-    static __device__ __forceinline__ Thirds whole(float v) { return Thirds{{__uint_as_float(v != v ? 0x7fc00000u : __float_as_uint(v)), 0.0f, 0.0f}}; }
 
     __device__ __forceinline__ void arrived()
     {
@@ -89,19 +113,24 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
     }
 
     // S^T of 32 keys, a lane's half of its key in registers
-    __device__ __forceinline__ f32x16_t scores(const u32x4_t (&k)[X::MINE], uint32_t powers) const
+    struct Scores { f32x16_t s[1]; };
+    __device__ __forceinline__ void scores(Scores &r, const uint32_t (&k)[4 * X::MINE], const uint32_t (&powers)[2]) const
     {
-        f32x16_t s;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+        for (int i = 0; i < 16; ++i) r.s[0][i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < X::MINE; ++j) {
-            const float scale = mx4_scale((powers >> (8 * j)) & 255u);
+            const float scale = mx4_scale((powers[0] >> (8 * j)) & 255u);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) score(s, mx4_bf16(k[j][e], scale), 4 * j + e);
+            for (int e = 0; e < 4; ++e) score(r.s[0], mx4_bf16(k[4 * j + e], scale), 4 * j + e);
         }
-        return s;
     }
+    __device__ __forceinline__ void hide_all(Scores &r, int32_t key, int32_t key0) const { this->hide(r.s[0], key, key0); }
+    using Base::exponentials;
+    __device__ __forceinline__ void exponentials(Scores &r, float c) { Base::template exponentials<1>(r.s, c); }
+    __device__ __forceinline__ void add_all(lds_t tile, const Scores &r) { add(tile, 0, r.s[0]); }
+    __device__ __forceinline__ void write(const AttnArgs &a, const AttnUnit &u, int kv_head) { write_columns<E, D>(a, u, *this, kv_head, 0); }
+    static __device__ __forceinline__ int v_turn(int row) { return X::v_turn(row); }
 
     // S^T of 32 keys from row `row0` of a K tile on
     __device__ __forceinline__ f32x16_t scores(lds_t tile, int row0) const
@@ -128,16 +157,7 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
         for (int h = 0; h < 2; ++h) {
             union { uint32_t w[4]; bf16x8_t v; } pb[PARTS];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float x = p[8 * h + 2 * w], y = p[8 * h + 2 * w + 1];
-                if constexpr (PARTS == 1) {
-                    pb[0].w[w] = pack_bf16(x, y);
-                } else {
-                    const Thirds xs = thirds(x), ys = thirds(y);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) pb[k].w[w] = upper_halves(xs.part[k], ys.part[k]);
-                }
-            }
+            for (int w = 0; w < 4; ++w) mx_weights<PARTS>(p[8 * h + 2 * w], p[8 * h + 2 * w + 1], [&](int k, uint32_t two) { pb[k].w[w] = two; });
 #pragma unroll
             for (int b = 0; b < X::BLOCKS; ++b) {
                 const lds_t from = at + 16 * h * X::ROW;
@@ -153,9 +173,7 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
     // Of 32 keys from `key` on, those of `bad` are NaN in 32 elements of V: so is a column that sees one, in these.
     __device__ __forceinline__ void spoil(int b, uint32_t bad, int32_t key, int32_t key0)
     {
-        const int32_t from = max(key0 - key, 0), to = max(0, min(this->lim - key, 32));
-        const uint32_t seen = (to >= 32 ? ~0u : (1u << to) - 1) & (from >= 32 ? 0u : ~0u << from);
-        if (bad & seen) {
+        if (bad & seen_keys(this->lim, key, key0)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[b][i] = __uint_as_float(0x7fc00000u);
         }
@@ -186,6 +204,132 @@ template <int D> struct MxSource {
     // where a lane's key begins in its page, and that page (keys past the last: the last)
     __device__ __forceinline__ int64_t page_at(uint32_t page) const { return (int64_t)min(page, (uint32_t)(n_pages - 1)) * page_bytes; }
     __device__ __forceinline__ int32_t in_page(int32_t key) const { return min(key, last) & ((1 << page_shift) - 1); }
+};
+
+// Blocks of 32 keys on their way to a wavefront's registers.  What a lane has of K: FEW, quarter lane / 16 of keys lane % 16 and 16 + lane % 16; else half lane / 32 of key lane % 32, as
+// always of V.
+//
+// ONE: the 32 keys are in one page (32 tokens and more).  The page is looked up when the block is asked for, among 64 entries of the table that the lanes hold, and the loads are
+// buffer loads: a page's address and a block's place in it are scalar, the lanes' offsets constant, and what is asked for past the last block is a load of no bytes: no
+// branch stands between the loads, so that the compiler waits for those of one block and not for all.  Else each lane looks its keys' pages up, a block earlier, and
+// past the last block asks for that again.
+template <int D, bool FEW, bool ONE> struct MxStream {
+    using P = Mx4Page<D>;
+    static constexpr int MINE = D / 64, WORDS = D / 16;           // 16-byte pieces of V, and words of K
+    struct Block { uint32_t k[WORDS], kp[2], vp, page[2]; u32x4_t v[MINE]; };
+    MxSource<D> src;
+    int32_t n, base, first, step, skip;
+    int32_t ids, ids_first;            // ONE: 64 page numbers from table[ids_first] on, one a lane
+    int32_t k_at, kp_at, v_at, vp_at;  // ONE: bytes of the lane's share in a block's numbers and powers
+
+    __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first_, int step_)
+    {
+        src.init(a, u, kv_head);
+        first = first_;
+        step = step_;
+        // Blocks first, first + step, ... of 32 keys; the first one last if it begins before key0.
+        base = u.key0 / 32 * 32;
+        const int32_t blocks = u.key1 > u.key0 ? (u.key1 - 1 - base) / 32 + 1 : 0;
+        n = (blocks - first + step - 1) / step;
+        skip = first == 0 && u.key0 > base ? 1 : 0;
+        const int lane = threadIdx.x & 63, g = lane >> 4, half = lane >> 5, r = lane & 31;
+        v_at = r * P::NUMBERS + half * (16 * MINE);
+        vp_at = r * P::POWERS + half * MINE;
+        k_at = FEW ? (lane & 15) * P::NUMBERS + g * (D / 8) : v_at;
+        kp_at = FEW ? (lane & 15) * P::POWERS + g * P::POWERS / 4 : vp_at;
+        if constexpr (ONE) {
+            ids_first = 0;
+            if (n > 0) reload(key_of(0) >> src.page_shift);
+        }
+    }
+    __device__ __forceinline__ int32_t key_of(int32_t i) const { return base + (first + step * (i + skip < n ? i + skip : i + skip - n)) * 32; }
+    // blocks that come before any that some column does not see whole; low: keys that every column sees
+    __device__ __forceinline__ int32_t whole(int32_t low) const { return min(n, max(0, ((low - base) / 32 - first + step - 1) / step - skip)); }
+
+    __device__ __forceinline__ void reload(int32_t i)
+    {
+        ids_first = i;
+        ids = src.table[min(i + (int32_t)(threadIdx.x & 63), src.last >> src.page_shift)];
+        asm volatile("" : "+v"(ids));                             // waited for here, and not wherever it is read
+    }
+    __device__ __forceinline__ void look(Block &b, int32_t i) const
+    {
+        if constexpr (!ONE) {
+            const int lane = threadIdx.x & 63;
+            const int32_t key = key_of(min(i, n - 1));
+            b.page[0] = src.page_of(key + (FEW ? lane & 15 : lane & 31));
+            if constexpr (FEW) b.page[1] = src.page_of(key + 16 + (lane & 15));
+        }
+    }
+    __device__ __forceinline__ void fetch(Block &b, int32_t i)
+    {
+        const int lane = threadIdx.x & 63;
+        if constexpr (ONE) {
+            const bool there = i < n;
+            const int32_t key = key_of(there ? i : 0), at = key >> src.page_shift, in = key & ((1 << src.page_shift) - 1);
+            if (there && (at - ids_first >= 64 || at < ids_first)) reload(at);
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(ids, there ? at - ids_first : 0);
+            const int64_t from = src.page_at(page);
+            const int bytes = there ? (int)P::head_bytes(src.page_shift) : 0;
+            const auto k = __builtin_amdgcn_make_buffer_rsrc((void *)(src.k + from), 0, bytes, 0x00027000);
+            const auto v = __builtin_amdgcn_make_buffer_rsrc((void *)(src.v + from), 0, bytes, 0x00027000);
+            const int numbers = in * P::NUMBERS, powers = (P::NUMBERS << src.page_shift) + in * P::POWERS;
+            if constexpr (!FEW) {
+#pragma unroll
+                for (int j = 0; j < MINE; ++j) words(b, 4 * j, __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, k_at + 16 * j, numbers, 0)));
+                b.kp[0] = MINE == 2 ? __builtin_amdgcn_raw_buffer_load_b16(k, kp_at, powers, 0) : __builtin_amdgcn_raw_buffer_load_b8(k, kp_at, powers, 0);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (D == 128) words(b, 4 * h, __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, k_at + 16 * h * P::NUMBERS, numbers, 0)));
+                    else two_words(b, 2 * h, __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(k, k_at + 16 * h * P::NUMBERS, numbers, 0)));
+                    b.kp[h] = __builtin_amdgcn_raw_buffer_load_b8(k, kp_at + 16 * h * P::POWERS, powers, 0);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) b.v[j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(v, v_at + 16 * j, numbers, 0));
+            b.vp = MINE == 2 ? __builtin_amdgcn_raw_buffer_load_b16(v, vp_at, powers, 0) : __builtin_amdgcn_raw_buffer_load_b8(v, vp_at, powers, 0);
+        } else {
+            const int g = lane >> 4, half = lane >> 5;
+            const int32_t key = key_of(min(i, n - 1));
+            const gcptr_t k = as_global((const void *)src.k), v = as_global((const void *)src.v);
+            const int64_t powers = (int64_t)P::NUMBERS << src.page_shift;
+            int64_t from[2];
+            int32_t in[2];
+#pragma unroll
+            for (int h = 0; h < (FEW ? 2 : 1); ++h) {
+                from[h] = src.page_at(b.page[h]);
+                in[h] = src.in_page(key + 16 * h + (FEW ? lane & 15 : lane & 31));
+                const gcptr_t row = k + from[h] + in[h] * P::NUMBERS, power = k + from[h] + powers + in[h] * P::POWERS;
+                if constexpr (FEW) {
+                    if constexpr (D == 128) words(b, 4 * h, ld16(row + g * 16));
+                    else two_words(b, 2 * h, ld8(row + g * 8));
+                    b.kp[h] = *(const PREFT_GLOBAL uint8_t *)(power + g * P::POWERS / 4);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j) words(b, 4 * j, ld16(row + half * (16 * MINE) + 16 * j));
+                    b.kp[0] = few_bytes(power + half * MINE);
+                }
+            }
+            const bool second = FEW && (lane & 16);
+            const int64_t page = second ? from[1] : from[0];
+            const int32_t at = second ? in[1] : in[0];
+#pragma unroll
+            for (int j = 0; j < MINE; ++j) b.v[j] = ld16(v + page + at * P::NUMBERS + half * (16 * MINE) + 16 * j);
+            b.vp = few_bytes(v + page + powers + at * P::POWERS + half * MINE);
+        }
+    }
+    static __device__ __forceinline__ uint32_t few_bytes(gcptr_t p)
+    {
+        if constexpr (MINE == 2) return *(const PREFT_GLOBAL uint16_t *)p;
+        else return *(const PREFT_GLOBAL uint8_t *)p;
+    }
+    static __device__ __forceinline__ void words(Block &b, int at, u32x4_t x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b.k[at + i] = x[i];
+    }
+    static __device__ __forceinline__ void two_words(Block &b, int at, u32x2_t x) { b.k[at] = x[0]; b.k[at + 1] = x[1]; }
 };
 
 // What is NaN, or lies in a row that no column sees, becomes zeros; says whether it is NaN in a row that some column sees.
@@ -220,7 +364,7 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
     const int32_t skip = u.key0 > base ? 1 : 0;                  // a first tile that begins before key0 comes last
     auto key_of = [&](int32_t i) { return base + (i + skip < n ? i + skip : i + skip - n) * ATTN_KEYS; };
     // this thread's row of the tile, and 32 elements of it; heads of 64: two wavefronts have K and two V
-    const int r = (lane & 31) + 32 * (wave & 1), block = D == 128 ? (lane >> 5) + 2 * (wave >> 1) : lane >> 5;
+    const int r = (lane & 31) + 32 * (wave & 1), block = D == 128 ? 2 * (lane >> 5) + (wave >> 1) : lane >> 5;
     const bool has_k = D == 128 || wave < 2, has_v = D == 128 || wave >= 2;
     u32x4_t kn = {}, vn = {};
     uint32_t kp = 127, vp = 127, page = 0;
@@ -294,74 +438,214 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
 }
 
 // ---------------------------------------------------------------------------------------
-// A unit of up to 32 columns: bound by the bytes of its keys.  The four wavefronts take blocks of 32 keys in turn, the next one's on their way in registers, and join their sums at
-// the end.  SOLO: the unit is one wavefront's.
+// 16 columns of a wavefront: decode rows of up to 16 query heads to a key/value head.  Products of 16x16x32: a lane has a quarter of one key's numbers, and 4 keys of 16 of one column
+// of S^T.  As the right operand of the second product its keys of 32 are 4 g .. 4 g + 3 and 16 + 4 g .. (g = lane / 16), and V^T is read so.
 // ---------------------------------------------------------------------------------------
-template <typename E, int D, bool SOLO>
+template <typename E, int D> struct MxFewColumns {
+    static constexpr int COLS = 16, PARTS = sizeof(E) == 2 ? 1 : 3;
+    static constexpr int ROW = 2 * D, STEPS = D / 32, BLOCKS = D / 16, EACH = D / 4;      // EACH: elements of a key that a lane has
+    u32x4_t qp[PARTS][STEPS];
+    f32x4_t o[BLOCKS];
+    float   m, l;
+    int32_t lim, row, head;
+    bool    valid;
+    // rows of V in LDS: as in MxTile, for 16 lanes that read 16 elements of 4 rows, two such at a time
+    static __device__ __forceinline__ int v_turn(int r) { return (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3)) + ((r >> 3) & 1); }
+
+    __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
+    {
+        const int lane = threadIdx.x & 63, g = lane >> 4;
+        const AttnQuery r = attn_query(a, u, kv_head, first + (lane & 15));
+        row = r.row; head = r.head; lim = r.lim; valid = r.valid;
+        const gcptr_t from = as_global((const char *)a.q + (int64_t)row * a.ldq + ((int64_t)head * D + g * EACH) * (int)sizeof(E));
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) mx_query<E>(from + t * 8 * (int)sizeof(E), qp, t);
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) o[b] = f32x4_t{0, 0, 0, 0};
+        m = ATTN_LOWEST;
+        l = 0.0f;
+    }
+    __device__ __forceinline__ void arrived()
+    {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) asm volatile("" : "+v"(qp[p][t]));
+    }
+    // the largest, and the sum, of a column's four lanes
+    static __device__ __forceinline__ float most(float v)
+    {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return other_half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    }
+    __device__ __forceinline__ float total() const
+    {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        return both_halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+    }
+
+    // S^T of 16 keys twice: a lane's quarter of its two keys
+    struct Scores { f32x4_t s[2]; };
+    __device__ __forceinline__ void scores(Scores &r, const uint32_t (&k)[2 * STEPS], const uint32_t (&power)[2]) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float scale = mx4_scale(power[h]);
+            r.s[h] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                const bf16x8_t kt = __builtin_bit_cast(bf16x8_t, mx4_bf16(k[STEPS * h + t], scale));
+#pragma unroll
+                for (int p = PARTS - 1; p >= 0; --p) r.s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kt, __builtin_bit_cast(bf16x8_t, qp[p][t]), r.s[h], 0, 0, 0);
+            }
+        }
+    }
+    __device__ __forceinline__ void hide_all(Scores &r, int32_t key, int32_t key0) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t at = key + 16 * h + 4 * ((threadIdx.x & 63) >> 4) + i;
+                r.s[h][i] = at < lim && at >= key0 ? r.s[h][i] : -INFINITY;
+            }
+    }
+    __device__ __forceinline__ void exponentials(Scores &r, float c)
+    {
+        f32x4_t (&s)[2] = r.s;
+        float top = s[0][0];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, s[h][i]);
+        top = most(top) * c;
+        if (__any(top > m + 8.0f)) {
+            const float to = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[b][i] *= f;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], c, -m));
+                l += s[h][i];
+            }
+    }
+    // O^T += V^T P^T over the 32 keys of the V tile
+    __device__ __forceinline__ void add_all(lds_t tile, const Scores &r)
+    {
+        const f32x4_t (&p)[2] = r.s;
+        const int lane = threadIdx.x & 63, i = lane & 15, key = 4 * (lane >> 4) + (i >> 2), turn = v_turn(key);     // 16 rows further on it is the same
+        const lds_t at = tile + key * ROW + (i & 1) * 8;
+        const int piece = (i & 3) >> 1;
+        union { uint32_t w[4]; bf16x8_t v; } pb[PARTS];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mx_weights<PARTS>(p[w >> 1][2 * w & 3], p[w >> 1][(2 * w & 3) + 1], [&](int k, uint32_t two) { pb[k].w[w] = two; });
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            const lds_t from = at + (((2 * b + piece) ^ turn) << 4);
+            const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)from);
+            const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)(from + 16 * ROW));
+            const bf16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int k = PARTS - 1; k >= 0; --k) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pb[k].v, o[b], 0, 0, 0);
+        }
+    }
+    // as in MxColumns; b: 32 elements
+    __device__ __forceinline__ void spoil(int b, uint32_t bad, int32_t key, int32_t key0)
+    {
+        if (bad & seen_keys(lim, key, key0)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[2 * b][i] = o[2 * b + 1][i] = __uint_as_float(0x7fc00000u);
+        }
+    }
+    // this lane's share of its column's sums, times f
+    __device__ __forceinline__ void put(PREFT_LDS float *to, float f) const
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) *(PREFT_LDS f32x4_t *)(to + b * 16 + 4 * g) = f32x4_t{o[b][0] * f, o[b][1] * f, o[b][2] * f, o[b][3] * f};
+    }
+    // the columns' results, or their part
+    __device__ __forceinline__ void write(const AttnArgs &a, const AttnUnit &u, int kv_head) const
+    {
+        const int lane = threadIdx.x & 63, g = lane >> 4;
+        const float sum = total();
+        if (!valid) return;
+        if (u.slot < 0) {
+            const float f = inverse(sum);
+            const gptr_t to = as_global((char *)a.out + (int64_t)row * a.ldo + ((int64_t)head * D + 4 * g) * (int)sizeof(E));
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) store4<E>(to + b * 16 * (int)sizeof(E), o[b][0] * f, o[b][1] * f, o[b][2] * f, o[b][3] * f);
+        } else {
+            const int64_t part = (int64_t)u.slot + kv_head * u.ncols + (lane & 15);
+            const gptr_t to = as_global((void *)(a.s.l.part_o + part * D + 4 * g));
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) store4<float>(to + b * 64, o[b][0], o[b][1], o[b][2], o[b][3]);
+            if (g == 0) a.s.l.part_ml[part] = make_float2(m, sum);
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------------
+// A unit of up to 32 columns (C: MxColumns), or up to 16 (MxFewColumns): bound by the bytes of its keys.  The four wavefronts take blocks of 32 keys in turn, AHEAD of them on their way in
+// registers, V through LDS of their own without a barrier, and join their sums at the end.  SOLO: the unit is one wavefront's.
+// ---------------------------------------------------------------------------------------
+template <typename E, int D, typename C, int AHEAD, bool SOLO, bool ONE>
 __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)
 {
     using X = MxTile<D>;
-    using P = Mx4Page<D>;
+    using Stream = MxStream<D, C::COLS == 16, ONE>;
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
-    MxSource<D> src;
-    src.init(a, u, kv_head);
     const lds_t vt = lds + wave * (X::TILE / 2);
-    // Blocks first, first + STEP, ... of 32 keys; the first one last if it begins before key0.
-    constexpr int STEP = SOLO ? 1 : 4;
-    const int first = SOLO ? 0 : wave;
-    const int32_t base = u.key0 / 32 * 32, blocks = u.key1 > u.key0 ? (u.key1 - 1 - base) / 32 + 1 : 0, n = (blocks - first + STEP - 1) / STEP;
-    const int32_t skip = first == 0 && u.key0 > base ? 1 : 0;
-    auto key_of = [&](int32_t i) { return base + (first + STEP * (i + skip < n ? i + skip : i + skip - n)) * 32; };
-    u32x4_t kn[X::MINE], vn[X::MINE];
-    uint32_t kp = 0, vp = 0, page = 0;
-    auto look = [&](int32_t i) { page = src.page_of(key_of(i) + r); };
-    auto fetch = [&](int32_t i) {
-        const int64_t at = src.page_at(page);
-        const int32_t in = src.in_page(key_of(i) + r);
-        const int64_t numbers = at + in * P::NUMBERS + half * (16 * X::MINE), powers = at + ((int64_t)P::NUMBERS << src.page_shift) + in * P::POWERS + half * X::MINE;
-        const gcptr_t k = as_global((const void *)src.k), v = as_global((const void *)src.v);
-#pragma unroll
-        for (int j = 0; j < X::MINE; ++j) { kn[j] = ld16(k + numbers + j * 16); vn[j] = ld16(v + numbers + j * 16); }
-        if constexpr (X::MINE == 2) {
-            kp = *(const PREFT_GLOBAL uint16_t *)(k + powers);
-            vp = *(const PREFT_GLOBAL uint16_t *)(v + powers);
-        } else {
-            kp = *(const PREFT_GLOBAL uint8_t *)(k + powers);
-            vp = *(const PREFT_GLOBAL uint8_t *)(v + powers);
-        }
-    };
-    MxColumns<E, D> w;
-    if (n > 0) look(0);
-    w.init(a, u, kv_head, 0);                                     // the queries are on their way while the first page is looked up
-    if (n > 0) fetch(0);
-    if (n > 1) look(1);
+    Stream st;
+    st.init(a, u, kv_head, SOLO ? 0 : wave, SOLO ? 1 : 4);
+    const int32_t n = st.n;
+    typename Stream::Block on_way[AHEAD];
+    C w;
+    w.init(a, u, kv_head, 0);
     const float c = a.scale_log2;
-    w.arrived();
-    const int32_t low = min(u.lim0, u.key1), before = (low - base) / 32 - first;           // blocks from this wavefront's first on that all columns see whole
-    const int32_t full = min(n, max(0, (before + STEP - 1) / STEP - skip));
-    for (int32_t i = 0; i < n; ++i) {
-        const int32_t key = key_of(i);
-        u32x4_t k[X::MINE], v[X::MINE];
-        uint32_t powers = kp, vpowers[X::MINE];
+    const int32_t full = st.whole(min(u.lim0, u.key1));
+    if (n > 0) {
 #pragma unroll
-        for (int j = 0; j < X::MINE; ++j) { k[j] = kn[j]; v[j] = vn[j]; vpowers[j] = (vp >> (8 * j)) & 255u; }
-        if (i + 1 < n) fetch(i + 1);
-        if (i + 2 < n) look(i + 2);
+        for (int j = 0; j < AHEAD; ++j) st.look(on_way[j], j);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            st.fetch(on_way[j], j);
+            st.look(on_way[j], j + AHEAD);
+        }
+    }
+    w.arrived();
+    auto block = [&](auto &b, int32_t i, bool more) {
+        const int32_t key = st.key_of(i);
+        typename C::Scores s;
+        w.scores(s, b.k, b.kp);
+        u32x4_t v[X::MINE];
+        uint32_t vp[X::MINE];
+#pragma unroll
+        for (int j = 0; j < X::MINE; ++j) { v[j] = b.v[j]; vp[j] = (b.vp >> (8 * j)) & 255u; }
         uint64_t bad[X::MINE] = {};
         if (i >= full) {
             const int32_t mine = key + r;
 #pragma unroll
-            for (int j = 0; j < X::MINE; ++j) bad[j] = __ballot(mx4_clean(v[j], vpowers[j], mine >= u.key0 && mine < u.key1));
+            for (int j = 0; j < X::MINE; ++j) bad[j] = __ballot(mx4_clean(v[j], vp[j], mine >= u.key0 && mine < u.key1));
         }
-        f32x16_t s[1];
-        s[0] = w.scores(k, powers);
         wait_lds_reads();                                         // of the block before
 #pragma unroll
-        for (int j = 0; j < X::MINE; ++j) mx4_put(vt + r * X::ROW, 4 * (X::MINE * half + j), X::v_turn(r), v[j], vpowers[j]);
-        if (i >= full) w.hide(s[0], key, u.key0);
-        w.template exponentials<1>(s, c);
+        for (int j = 0; j < X::MINE; ++j) mx4_put(vt + r * X::ROW, 4 * (X::MINE * half + j), C::v_turn(r), v[j], vp[j]);
+        if (more) {
+            st.fetch(b, i + AHEAD);
+            st.look(b, i + 2 * AHEAD);
+        }
+        if (i >= full) w.hide_all(s, key, u.key0);
+        w.exponentials(s, c);
         wait_lds_reads();                                         // written: nobody else's, so without a barrier
-        w.add(vt, 0, s[0]);
+        w.add_all(vt, s);
         if (i >= full) {
 #pragma unroll
             for (int j = 0; j < X::MINE; ++j) {
@@ -369,9 +653,31 @@ __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit
                 w.spoil(X::MINE + j, (uint32_t)(bad[j] >> 32), key, u.key0);
             }
         }
+    };
+    int32_t i = 0;
+    for (; i + AHEAD <= n; i += AHEAD) {
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) block(on_way[q], i + q, true);
     }
-    if constexpr (SOLO) write_columns<E, D>(a, u, w, kv_head, 0);
+#pragma unroll
+    for (int q = 0; q < AHEAD - 1; ++q)                           // a loop with a way out in its middle would be one that waits for all
+        if (i + q < n) block(on_way[q], i + q, false);
+    if constexpr (SOLO) w.write(a, u, kv_head);
     else join_waves<E, D>(a, u, w, kv_head, lds, join);
+}
+
+template <typename E, int D, bool SOLO>
+__device__ __forceinline__ void mx_attend_narrow(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)
+{
+    constexpr int AHEAD = 3, AHEAD_WIDE = sizeof(E) == 2 ? 2 : 1;             // as many as registers allow
+    const bool one = a.page_shift >= 5;
+    if (u.ncols <= MX_FEW_COLS) {
+        if (one) mx_attend_keys<E, D, MxFewColumns<E, D>, AHEAD, SOLO, true>(a, u, kv_head, lds, join);
+        else mx_attend_keys<E, D, MxFewColumns<E, D>, AHEAD, SOLO, false>(a, u, kv_head, lds, join);
+    } else {
+        if (one) mx_attend_keys<E, D, MxColumns<E, D>, AHEAD_WIDE, SOLO, true>(a, u, kv_head, lds, join);
+        else mx_attend_keys<E, D, MxColumns<E, D>, AHEAD_WIDE, SOLO, false>(a, u, kv_head, lds, join);
+    }
 }
 
 template <typename E, int D, bool DIRECT>
@@ -386,6 +692,7 @@ __global__ __launch_bounds__(256, 2) void attention_mx_kernel(AttnArgs a)
     if constexpr (DIRECT) {
         if (a.ready && !attn_schedule_is(a, KIND)) return;
         if (!attn_direct_unit(a.s, unit, kv_head, a.ready != 0, u)) return;
+        u.table = uniform(u.table); u.key0 = uniform(u.key0); u.key1 = uniform(u.key1); u.lim0 = uniform(u.lim0); u.ncols = uniform(u.ncols);
     } else {
         if (!attn_schedule_is(a, KIND)) return;
         // short units: one a wavefront, four a workgroup
@@ -395,13 +702,13 @@ __global__ __launch_bounds__(256, 2) void attention_mx_kernel(AttnArgs a)
         const PREFT_CONST AttnUnit *p = as_const(a.s.l.units) + i;
         u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
         if (unit >= alone) {
-            if (u.ncols > 0) mx_attend_keys<E, D, true>(a, u, kv_head, (lds_t)lds, join);
+            if (u.ncols > 0) mx_attend_narrow<E, D, true>(a, u, kv_head, (lds_t)lds, join);
             return;
         }
     }
     if (u.ncols <= 0) return;
     if (u.ncols > ATTN_FEW_COLS) mx_attend_columns<E, D>(a, u, kv_head, (lds_t)lds, (uint32_t *)join);
-    else mx_attend_keys<E, D, false>(a, u, kv_head, (lds_t)lds, join);
+    else mx_attend_narrow<E, D, false>(a, u, kv_head, (lds_t)lds, join);
 }
 
 }  // namespace preft

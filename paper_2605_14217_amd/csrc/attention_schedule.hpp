@@ -154,7 +154,7 @@ __device__ __forceinline__ int32_t last_at_or_before(P first, int32_t n, int32_t
 // Units stand in the order of falling time (counting sort over 256 classes): the longest of a causal prompt begin first and the short ones fill the ends.
 // (Wide units, bound by the matrix cores, and narrow ones, bound by memory, in turns, so that a compute unit has one of each: 229 us against 187 on 256 rows of
 // 64 heads with prefixes of 8192 -- the wide ones then end late.)  Their order does not change a result: every unit has an output or part of its own.
-__global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnScheduleArgs a)
+static __global__ __launch_bounds__(SCHED_THREADS) void attn_schedule_kernel(AttnScheduleArgs a)
 {
     __shared__ int32_t lds[32];
     __shared__ int32_t first_tile[ATTN_SCAN + 1];
