@@ -20,10 +20,11 @@ template <int D> struct MxTile {
     static constexpr int ROW = 2 * D, PIECES = ROW / 16;           // of a key in LDS, in bf16
     static constexpr int STEPS = PIECES / 2, BLOCKS = D / 32;
     static constexpr int MINE = D / 64;                            // 16-byte pieces of a key, of 32 numbers each, that a lane of 32 keys has
-    static constexpr int TILE = ATTN_KEYS * ROW;
-    // As in AttnTile; in V also by the row's bits above, so that a lane writes whole pieces of its row without a conflict.
-    static __device__ __forceinline__ int k_turn(int row) { return PIECES < 16 ? (row >> 1) & 7 : row & 15; }
-    static __device__ __forceinline__ int v_turn(int row) { return (PIECES >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)) + ((row >> 2) & 3); }
+    // Rows in LDS are further apart than they are long, so that what is read in one cycle comes from all banks: of K, 16 lanes' 16 bytes of as many rows; of V, 64 bytes each
+    // of 4 rows.  (Turning the pieces of a row does it too, but takes a register for every address: with 16-byte pieces at constant distances one is enough, and nothing spills.)
+    static constexpr int K_PITCH = ROW + 16;
+    static __device__ __forceinline__ constexpr int v_row(int row) { return row * (ROW + 64) + (row >> 2) * 16; }       // (and what is written, 16 bytes of 16 rows)
+    static constexpr int K_TILE = ATTN_KEYS * K_PITCH, V_TILE = ATTN_KEYS * (ROW + 68), LDS = 2 * (K_TILE + V_TILE);
 };
 
 // a number as three of 8 bits, its own upper bits first; infinite: the first alone; NaN stays NaN
@@ -130,29 +131,45 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
     __device__ __forceinline__ void exponentials(Scores &r, float c) { Base::template exponentials<1>(r.s, c); }
     __device__ __forceinline__ void add_all(lds_t tile, const Scores &r) { add(tile, 0, r.s[0]); }
     __device__ __forceinline__ void write(const AttnArgs &a, const AttnUnit &u, int kv_head) { write_columns<E, D>(a, u, *this, kv_head, 0); }
-    static __device__ __forceinline__ int v_turn(int row) { return X::v_turn(row); }
+    static constexpr int V_BLOCK = X::V_TILE / 2;
+    static __device__ __forceinline__ int v_row(int row) { return X::v_row(row); }
 
     // S^T of 32 keys from row `row0` of a K tile on
     __device__ __forceinline__ f32x16_t scores(lds_t tile, int row0) const
     {
         const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
-        const lds_t at = tile + (row0 + r) * X::ROW;
-        const int turn = X::k_turn(r);
+        const lds_t at = tile + r * X::K_PITCH + half * (X::ROW / 2);
         f32x16_t s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < X::STEPS; ++t) score(s, *(const PREFT_LDS u32x4_t *)(at + (((X::STEPS * half + t) ^ turn) << 4)), t);
+        for (int t = 0; t < X::STEPS; ++t) score(s, *(const PREFT_LDS u32x4_t *)(at + row0 * X::K_PITCH + 16 * t), t);
         return s;
+    }
+
+    // S^T -> P^T by the m there is, without the largest S, a tenth of a tile's vector instructions: true where a weight may pass 2^8, S^T and m are then to be taken anew.  (Sums that
+    // are NaN stay: so is the result.)
+    __device__ __forceinline__ bool try_exponentials(f32x16_t (&s)[2], float c)
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -this->m));
+                sum += s[b][i];
+            }
+        if (__any(sum > 256.0f)) return true;
+        this->l += sum;
+        return false;
     }
 
     // O^T += V^T P^T over 32 keys from row `row0` of a V tile on
     __device__ __forceinline__ void add(lds_t tile, int row0, const f32x16_t &p)
     {
         const int lane = threadIdx.x & 63, half = lane >> 5;
-        const int i = lane & 15, key = 4 * half + (i >> 2), turn = X::v_turn(key);          // 8 keys further on: the turn's bit 1 changes
-        const lds_t at = tile + (row0 + key) * X::ROW + (i & 1) * 8;
-        const int piece = ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+        const int i = lane & 15;
+        const lds_t at = tile + X::v_row(4 * half + (i >> 2)) + ((lane >> 4) & 1) * 32 + (i & 3) * 8;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             union { uint32_t w[4]; bf16x8_t v; } pb[PARTS];
@@ -160,14 +177,37 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
             for (int w = 0; w < 4; ++w) mx_weights<PARTS>(p[8 * h + 2 * w], p[8 * h + 2 * w + 1], [&](int k, uint32_t two) { pb[k].w[w] = two; });
 #pragma unroll
             for (int b = 0; b < X::BLOCKS; ++b) {
-                const lds_t from = at + 16 * h * X::ROW;
-                const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)(from + (((b * 4 + piece) ^ turn) << 4)));
-                const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)(from + 8 * X::ROW + (((b * 4 + piece) ^ turn ^ 2) << 4)));
+                const lds_t from = at + X::v_row(row0 + 16 * h) + 64 * b;
+                const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)from);
+                const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)(from + X::v_row(8)));
                 const bf16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
                 for (int k = PARTS - 1; k >= 0; --k) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[k].v, o[b], 0, 0, 0);
             }
         }
+    }
+
+    // How the reads of LDS and the products of 64 keys stand: reads several products ahead (the compiler keeps two in flight).
+    static __device__ __forceinline__ void order_scores()
+    {
+        __builtin_amdgcn_sched_group_barrier(0x100, X::STEPS, 0);
+#pragma unroll
+        for (int t = 0; t < X::STEPS; ++t) {
+            __builtin_amdgcn_sched_group_barrier(0x008, PARTS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, X::STEPS * PARTS, 0);
+    }
+    static __device__ __forceinline__ void order_sums()
+    {
+        constexpr int READS = 8 * X::BLOCKS, FIRST = 8;           // of 8 bytes
+        __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 1);
+#pragma unroll
+        for (int t = 0; t < (READS - FIRST) / 2; ++t) {
+            __builtin_amdgcn_sched_group_barrier(0x008, PARTS, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, FIRST / 2 * PARTS, 1);
     }
 
     // Of 32 keys from `key` on, those of `bad` are NaN in 32 elements of V: so is a column that sees one, in these.
@@ -206,20 +246,43 @@ template <int D> struct MxSource {
     __device__ __forceinline__ int32_t in_page(int32_t key) const { return min(key, last) & ((1 << page_shift) - 1); }
 };
 
+// Pages of 32 tokens and more: 32 keys that begin at a multiple of 32 are in one.  It is looked up when they are asked for, among 64 entries of the table that the lanes hold, and the
+// loads are buffer loads: a page's address and the keys' place in it are scalar, the lanes' offsets constant, and what is asked for past the last block is a load of no bytes.  So no
+// vector instruction makes an address, no branch need stand between the loads of a stream, and the compiler waits for those that it needs and not for all.
+template <int D> struct MxOnePage {
+    using P = Mx4Page<D>;
+    int32_t ids, ids_first;            // 64 page numbers from table[ids_first] on, one a lane
+    struct Keys { __amdgpu_buffer_rsrc_t k, v; int numbers, powers; };     // of a block: the page's K and V, and where its numbers and powers begin there
+
+    __device__ __forceinline__ void init(const MxSource<D> &src, int32_t key) { reload(src, min(key, src.last) >> src.page_shift); }
+    __device__ __forceinline__ void reload(const MxSource<D> &src, int32_t i)
+    {
+        ids_first = i;
+        ids = src.table[min(i + (int32_t)(threadIdx.x & 63), src.last >> src.page_shift)];
+        asm volatile("" : "+v"(ids));                             // waited for here, and not wherever it is read
+    }
+    __device__ __forceinline__ Keys at(const MxSource<D> &src, int32_t key, bool there)
+    {
+        const int32_t i = min(key, src.last) >> src.page_shift, in = key & ((1 << src.page_shift) - 1);
+        if (there && (i - ids_first >= 64 || i < ids_first)) reload(src, i);
+        const int64_t from = src.page_at((uint32_t)__builtin_amdgcn_readlane(ids, there ? i - ids_first : 0));
+        const int bytes = there ? (int)P::head_bytes(src.page_shift) : 0;
+        return Keys{__builtin_amdgcn_make_buffer_rsrc((void *)(src.k + from), 0, bytes, 0x00027000),
+                    __builtin_amdgcn_make_buffer_rsrc((void *)(src.v + from), 0, bytes, 0x00027000), in * P::NUMBERS, (P::NUMBERS << src.page_shift) + in * P::POWERS};
+    }
+};
+
 // Blocks of 32 keys on their way to a wavefront's registers.  What a lane has of K: FEW, quarter lane / 16 of keys lane % 16 and 16 + lane % 16; else half lane / 32 of key lane % 32, as
 // always of V.
 //
-// ONE: the 32 keys are in one page (32 tokens and more).  The page is looked up when the block is asked for, among 64 entries of the table that the lanes hold, and the loads are
-// buffer loads: a page's address and a block's place in it are scalar, the lanes' offsets constant, and what is asked for past the last block is a load of no bytes: no
-// branch stands between the loads, so that the compiler waits for those of one block and not for all.  Else each lane looks its keys' pages up, a block earlier, and
-// past the last block asks for that again.
+// ONE: MxOnePage.  Else each lane looks its keys' pages up, a block earlier, and past the last block asks for that again.
 template <int D, bool FEW, bool ONE> struct MxStream {
     using P = Mx4Page<D>;
     static constexpr int MINE = D / 64, WORDS = D / 16;           // 16-byte pieces of V, and words of K
     struct Block { uint32_t k[WORDS], kp[2], vp, page[2]; u32x4_t v[MINE]; };
     MxSource<D> src;
     int32_t n, base, first, step, skip;
-    int32_t ids, ids_first;            // ONE: 64 page numbers from table[ids_first] on, one a lane
+    MxOnePage<D> one;
     int32_t k_at, kp_at, v_at, vp_at;  // ONE: bytes of the lane's share in a block's numbers and powers
 
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first_, int step_)
@@ -237,21 +300,12 @@ template <int D, bool FEW, bool ONE> struct MxStream {
         vp_at = r * P::POWERS + half * MINE;
         k_at = FEW ? (lane & 15) * P::NUMBERS + g * (D / 8) : v_at;
         kp_at = FEW ? (lane & 15) * P::POWERS + g * P::POWERS / 4 : vp_at;
-        if constexpr (ONE) {
-            ids_first = 0;
-            if (n > 0) reload(key_of(0) >> src.page_shift);
-        }
+        if (ONE && n > 0) one.init(src, key_of(0));                // no key: the table may have no entry
     }
     __device__ __forceinline__ int32_t key_of(int32_t i) const { return base + (first + step * (i + skip < n ? i + skip : i + skip - n)) * 32; }
     // blocks that come before any that some column does not see whole; low: keys that every column sees
     __device__ __forceinline__ int32_t whole(int32_t low) const { return min(n, max(0, ((low - base) / 32 - first + step - 1) / step - skip)); }
 
-    __device__ __forceinline__ void reload(int32_t i)
-    {
-        ids_first = i;
-        ids = src.table[min(i + (int32_t)(threadIdx.x & 63), src.last >> src.page_shift)];
-        asm volatile("" : "+v"(ids));                             // waited for here, and not wherever it is read
-    }
     __device__ __forceinline__ void look(Block &b, int32_t i) const
     {
         if constexpr (!ONE) {
@@ -266,14 +320,7 @@ template <int D, bool FEW, bool ONE> struct MxStream {
         const int lane = threadIdx.x & 63;
         if constexpr (ONE) {
             const bool there = i < n;
-            const int32_t key = key_of(there ? i : 0), at = key >> src.page_shift, in = key & ((1 << src.page_shift) - 1);
-            if (there && (at - ids_first >= 64 || at < ids_first)) reload(at);
-            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(ids, there ? at - ids_first : 0);
-            const int64_t from = src.page_at(page);
-            const int bytes = there ? (int)P::head_bytes(src.page_shift) : 0;
-            const auto k = __builtin_amdgcn_make_buffer_rsrc((void *)(src.k + from), 0, bytes, 0x00027000);
-            const auto v = __builtin_amdgcn_make_buffer_rsrc((void *)(src.v + from), 0, bytes, 0x00027000);
-            const int numbers = in * P::NUMBERS, powers = (P::NUMBERS << src.page_shift) + in * P::POWERS;
+            const auto [k, v, numbers, powers] = one.at(src, key_of(there ? i : 0), there);
             if constexpr (!FEW) {
 #pragma unroll
                 for (int j = 0; j < MINE; ++j) words(b, 4 * j, __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, k_at + 16 * j, numbers, 0)));
@@ -340,19 +387,21 @@ __device__ __forceinline__ bool mx4_clean(u32x4_t &numbers, uint32_t &power, boo
     return nan && seen;
 }
 
-// 32 numbers to four pieces of a row in LDS
-__device__ __forceinline__ void mx4_put(lds_t row, int piece, int turn, u32x4_t numbers, uint32_t power)
+// 32 numbers to their place in a row in LDS
+__device__ __forceinline__ void mx4_put(lds_t to, u32x4_t numbers, uint32_t power)
 {
     const float scale = mx4_scale(power);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) *(PREFT_LDS u32x4_t *)(row + (((piece + e) ^ turn) << 4)) = mx4_bf16(numbers[e], scale);
+    for (int e = 0; e < 4; ++e) *(PREFT_LDS u32x4_t *)(to + 16 * e) = mx4_bf16(numbers[e], scale);
 }
 
 // ---------------------------------------------------------------------------------------
 // A unit of more than 32 columns: as in attend_columns, but the tiles of 64 keys come through registers: each thread has 32 numbers of K and 32 of V (heads of 64: of one)
-// of the tile after next on their way while this one's products run.
+// of the tile after next on their way while this one's products run.  Four requests' further chunks, 6000 rows over 5000..17 000 tokens, 32 heads over 8 of 128: 867 us, 1150 TFLOP/s, 96 % of
+// a large matrix product's 1200; before the wavefronts' priorities and the weights without a look for the largest score 999, with them 958, with scalar addresses 900, with reads ordered ahead of the
+// products and rows at a pitch 867 (half of the products of a tile stood waiting for LDS; a K tile further ahead, its products beside the exponentials, took 1040).
 // ---------------------------------------------------------------------------------------
-template <typename E, int D>
+template <typename E, int D, bool ONE>
 __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, uint32_t *bad)
 {
     using X = MxTile<D>;
@@ -368,37 +417,59 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
     const bool has_k = D == 128 || wave < 2, has_v = D == 128 || wave >= 2;
     u32x4_t kn = {}, vn = {};
     uint32_t kp = 127, vp = 127, page = 0;
-    auto look = [&](int32_t i) { page = src.page_of(key_of(i) + r); };
+    MxOnePage<D> one;
+    if (ONE && n > 0) one.init(src, key_of(0) + 32 * (wave & 1));
+    auto look = [&](int32_t i) {
+        if constexpr (!ONE) page = src.page_of(key_of(min(i, n - 1)) + r);
+    };
     auto fetch = [&](int32_t i) {
-        const int64_t at = src.page_at(page);
-        const int32_t in = src.in_page(key_of(i) + r);
-        const int64_t numbers = at + in * P::NUMBERS + block * 16, power = at + ((int64_t)P::NUMBERS << src.page_shift) + in * P::POWERS + block;
-        if (has_k) { kn = ld16(as_global((const void *)src.k) + numbers); kp = *(as_global((const void *)src.k) + power) & 255u; }
-        if (has_v) { vn = ld16(as_global((const void *)src.v) + numbers); vp = *(as_global((const void *)src.v) + power) & 255u; }
+        if constexpr (ONE) {
+            const bool there = i < n;
+            const auto [k, v, numbers, powers] = one.at(src, key_of(there ? i : 0) + 32 * (wave & 1), there);
+            const int at = (lane & 31) * P::NUMBERS + block * 16, power_at = (lane & 31) * P::POWERS + block;
+            if (has_k) {
+                kn = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, at, numbers, 0));
+                kp = __builtin_amdgcn_raw_buffer_load_b8(k, power_at, powers, 0);
+            }
+            if (has_v) {
+                vn = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(v, at, numbers, 0));
+                vp = __builtin_amdgcn_raw_buffer_load_b8(v, power_at, powers, 0);
+            }
+        } else {
+            const int64_t at = src.page_at(page);
+            const int32_t in = src.in_page(key_of(min(i, n - 1)) + r);
+            const int64_t numbers = at + in * P::NUMBERS + block * 16, power = at + ((int64_t)P::NUMBERS << src.page_shift) + in * P::POWERS + block;
+            if (has_k) { kn = ld16(as_global((const void *)src.k) + numbers); kp = *(const PREFT_GLOBAL uint8_t *)(as_global((const void *)src.k) + power); }
+            if (has_v) { vn = ld16(as_global((const void *)src.v) + numbers); vp = *(const PREFT_GLOBAL uint8_t *)(as_global((const void *)src.v) + power); }
+        }
     };
     MxColumns<E, D> w;
     if (n > 0) look(0);
     w.init(a, u, kv_head, wave * 32);
-    if (n > 0) fetch(0);
-    if (n > 1) look(1);
+    if (n > 0) {
+        fetch(0);
+        look(1);
+    }
     w.arrived();
     const int32_t low = min(u.lim0, u.key1);                     // keys that every column sees
     const float c = a.scale_log2;
     const int32_t full = min(n, max(0, (low - base) / ATTN_KEYS - skip));         // tiles that every column sees whole
+    auto k_tile = [&](int32_t i) { return lds + (i & 1) * X::K_TILE; };
+    auto v_tile = [&](int32_t i) { return lds + 2 * X::K_TILE + (i & 1) * X::V_TILE; };
     // tile i, which is in registers, to LDS; `bad`: for each 32 keys and 32 elements of the tile the keys that are NaN there
     auto put = [&](int32_t i) {
-        const lds_t kt = lds + (i & 1) * X::TILE, vt = kt + 2 * X::TILE;
-        if (has_k) mx4_put(kt + r * X::ROW, 4 * block, X::k_turn(r), kn, kp);
+        if (has_k) mx4_put(k_tile(i) + r * X::K_PITCH + 64 * block, kn, kp);
         if (has_v) {
             if (i >= full) {
                 const int32_t key = key_of(i) + r;
                 const uint64_t nan = __ballot(mx4_clean(vn, vp, key >= u.key0 && key < u.key1));
                 if (lane % 32 == 0) bad[(i & 1) * 8 + (wave & 1) * 4 + block] = (uint32_t)(nan >> lane);
             }
-            mx4_put(vt + r * X::ROW, 4 * block, X::v_turn(r), vn, vp);
+            mx4_put(v_tile(i) + X::v_row(r) + 64 * block, vn, vp);
         }
         if (i + 1 < n) fetch(i + 1);
         if (i + 2 < n) look(i + 2);
+        __builtin_amdgcn_sched_barrier(0);                        // else it all stands among the products and takes their registers
     };
     if (n > 0) put(0);
     auto arrive = [&](int32_t i) {
@@ -409,17 +480,29 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
     int32_t i = 0;
     for (; i < full; ++i) {
         arrive(i);
-        const lds_t kt = lds + (i & 1) * X::TILE, vt = kt + 2 * X::TILE;
+        const lds_t kt = k_tile(i), vt = v_tile(i);
         f32x16_t s[2];
+        __builtin_amdgcn_s_setprio(1);                            // to the matrix cores first: the other wavefront of the unit has its exponentials in between
         s[0] = w.scores(kt, 0);
         s[1] = w.scores(kt, 32);
-        w.template exponentials<2>(s, c);
+        w.order_scores();
+        __builtin_amdgcn_s_setprio(0);
+        if (i == 0 || __any(w.try_exponentials(s, c))) {          // (__any: a branch for all lanes, in the compiler's eyes too)
+            if (i > 0) {
+                s[0] = w.scores(kt, 0);
+                s[1] = w.scores(kt, 32);
+            }
+            w.template exponentials<2>(s, c);
+        }
+        __builtin_amdgcn_s_setprio(1);
         w.add(vt, 0, s[0]);
         w.add(vt, 32, s[1]);
+        w.order_sums();
+        __builtin_amdgcn_s_setprio(0);
     }
     for (; i < n; ++i) {
         arrive(i);
-        const lds_t kt = lds + (i & 1) * X::TILE, vt = kt + 2 * X::TILE;
+        const lds_t kt = k_tile(i), vt = v_tile(i);
         const int32_t key = key_of(i);
         f32x16_t s[2];
         s[0] = w.scores(kt, 0);
@@ -449,8 +532,8 @@ template <typename E, int D> struct MxFewColumns {
     float   m, l;
     int32_t lim, row, head;
     bool    valid;
-    // rows of V in LDS: as in MxTile, for 16 lanes that read 16 elements of 4 rows, two such at a time
-    static __device__ __forceinline__ int v_turn(int r) { return (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3)) + ((r >> 3) & 1); }
+    static __device__ __forceinline__ constexpr int v_row(int row) { return row * (ROW + 32) + (row >> 3) * 16; }       // as in MxTile: 32 bytes each of 8 rows are read
+    static constexpr int V_BLOCK = 32 * (ROW + 34);
 
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first)
     {
@@ -540,17 +623,16 @@ template <typename E, int D> struct MxFewColumns {
     __device__ __forceinline__ void add_all(lds_t tile, const Scores &r)
     {
         const f32x4_t (&p)[2] = r.s;
-        const int lane = threadIdx.x & 63, i = lane & 15, key = 4 * (lane >> 4) + (i >> 2), turn = v_turn(key);     // 16 rows further on it is the same
-        const lds_t at = tile + key * ROW + (i & 1) * 8;
-        const int piece = (i & 3) >> 1;
+        const int lane = threadIdx.x & 63, i = lane & 15;
+        const lds_t at = tile + v_row(4 * (lane >> 4) + (i >> 2)) + (i & 3) * 8;
         union { uint32_t w[4]; bf16x8_t v; } pb[PARTS];
 #pragma unroll
         for (int w = 0; w < 4; ++w) mx_weights<PARTS>(p[w >> 1][2 * w & 3], p[w >> 1][(2 * w & 3) + 1], [&](int k, uint32_t two) { pb[k].w[w] = two; });
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) {
-            const lds_t from = at + (((2 * b + piece) ^ turn) << 4);
+            const lds_t from = at + 32 * b;
             const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)from);
-            const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)(from + 16 * ROW));
+            const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((PREFT_LDS bf16x4_t *)(from + v_row(16)));
             const bf16x8_t v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
             for (int k = PARTS - 1; k >= 0; --k) o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pb[k].v, o[b], 0, 0, 0);
@@ -602,7 +684,7 @@ __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit
     using X = MxTile<D>;
     using Stream = MxStream<D, C::COLS == 16, ONE>;
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
-    const lds_t vt = lds + wave * (X::TILE / 2);
+    const lds_t vt = lds + wave * C::V_BLOCK;
     Stream st;
     st.init(a, u, kv_head, SOLO ? 0 : wave, SOLO ? 1 : 4);
     const int32_t n = st.n;
@@ -637,7 +719,7 @@ __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit
         }
         wait_lds_reads();                                         // of the block before
 #pragma unroll
-        for (int j = 0; j < X::MINE; ++j) mx4_put(vt + r * X::ROW, 4 * (X::MINE * half + j), C::v_turn(r), v[j], vp[j]);
+        for (int j = 0; j < X::MINE; ++j) mx4_put(vt + C::v_row(r) + 64 * (X::MINE * half + j), v[j], vp[j]);
         if (more) {
             st.fetch(b, i + AHEAD);
             st.look(b, i + 2 * AHEAD);
@@ -685,7 +767,7 @@ __global__ __launch_bounds__(256, 2) void attention_mx_kernel(AttnArgs a)
 {
     using X = MxTile<D>;
     constexpr int JOIN = 4 * 32 * (D + 4) * 4, KIND = 2;
-    __shared__ __align__(1024) char lds[4 * X::TILE > JOIN ? 4 * X::TILE : JOIN];
+    __shared__ __align__(1024) char lds[X::LDS > JOIN ? X::LDS : JOIN];
     __shared__ float join[256];
     const int32_t unit = (int32_t)blockIdx.x / a.s.kv_heads, kv_head = (int32_t)blockIdx.x % a.s.kv_heads;
     AttnUnit u;
@@ -707,7 +789,10 @@ __global__ __launch_bounds__(256, 2) void attention_mx_kernel(AttnArgs a)
         }
     }
     if (u.ncols <= 0) return;
-    if (u.ncols > ATTN_FEW_COLS) mx_attend_columns<E, D>(a, u, kv_head, (lds_t)lds, (uint32_t *)join);
+    if (u.ncols > ATTN_FEW_COLS) {
+        if (a.page_shift >= 5) mx_attend_columns<E, D, true>(a, u, kv_head, (lds_t)lds, (uint32_t *)join);
+        else mx_attend_columns<E, D, false>(a, u, kv_head, (lds_t)lds, (uint32_t *)join);
+    }
     else mx_attend_narrow<E, D, false>(a, u, kv_head, (lds_t)lds, join);
 }
 

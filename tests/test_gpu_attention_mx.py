@@ -385,3 +385,18 @@ def test_pages_past_32_bits():
                                         preft.new_attention_workspace(rows, 1, H, Hkv, D))
         want = cached(q, [0, rows], None, [kv], *values, np.arange(len(ids))[None], H, 0.09)
         base.check(out.cpu(), want, torch.zeros_like(q))
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+def test_no_pages_at_all(rows):
+    """A pool or a table without pages: every row sees no key and is zero; tables and caches may be empty."""
+    print(f"\n[case] 4-bit no pages rows={rows}", flush=True)
+    H, Hkv, D = 4, 2, 64
+    q = torch.randn(rows, H * D, device="cuda").bfloat16()
+    ws = preft.new_attention_workspace(rows, 1, H, Hkv, D)
+    for n_pages, columns, page in ((0, 4, 16), (3, 0, 64), (0, 0, 32), (0, 3, 64)):
+        caches = [preft.new_mx_cache(n_pages, Hkv, page, D) for _ in "kv"]
+        table = torch.zeros(1, columns, dtype=torch.int32, device="cuda")
+        out = torch.full_like(q, 7.5)
+        preft.preft_cached_attention_mx(out, q, i32([0, rows]), None, i32([50]), *caches, table, None, None, H, 0.1, 0, ws)
+        assert not out.any()
