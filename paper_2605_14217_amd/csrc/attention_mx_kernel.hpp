@@ -73,6 +73,8 @@ template <int PARTS, typename Put> __device__ __forceinline__ void mx_weights(fl
         for (int k = 0; k < 3; ++k) put(k, upper_halves(xs.part[k], ys.part[k]));
     }
 }
+// the power that begins at bit `bits` of four
+__device__ __forceinline__ uint32_t mx4_power_of(uint32_t four, int bits) { return (four >> bits) & 255u; }
 // of 32 keys from `key` on, those that a column sees
 __device__ __forceinline__ uint32_t seen_keys(int32_t lim, int32_t key, int32_t key0)
 {
@@ -115,13 +117,13 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
 
     // S^T of 32 keys, a lane's half of its key in registers
     struct Scores { f32x16_t s[1]; };
-    __device__ __forceinline__ void scores(Scores &r, const uint32_t (&k)[4 * X::MINE], const uint32_t (&powers)[2]) const
+    __device__ __forceinline__ void scores(Scores &r, const uint32_t (&k)[4 * X::MINE], const uint32_t (&powers)[2], int bits) const
     {
 #pragma unroll
         for (int i = 0; i < 16; ++i) r.s[0][i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < X::MINE; ++j) {
-            const float scale = mx4_scale((powers[0] >> (8 * j)) & 255u);
+            const float scale = mx4_scale(mx4_power_of(powers[0], bits + 8 * j));
 #pragma unroll
             for (int e = 0; e < 4; ++e) score(r.s[0], mx4_bf16(k[4 * j + e], scale), 4 * j + e);
         }
@@ -244,6 +246,10 @@ template <int D> struct MxSource {
     // where a lane's key begins in its page, and that page (keys past the last: the last)
     __device__ __forceinline__ int64_t page_at(uint32_t page) const { return (int64_t)min(page, (uint32_t)(n_pages - 1)) * page_bytes; }
     __device__ __forceinline__ int32_t in_page(int32_t key) const { return min(key, last) & ((1 << page_shift) - 1); }
+    // Powers are loaded four at a time, a key's (heads of 64: those of two): bytes of the four from the first, of key `in` of a page; and the bits before its first.  (Loaded as bytes they are
+    // 8-bit values to the compiler, which copies such registers at the end of a loop, and waits there for all that is on its way.)
+    static __device__ __forceinline__ int32_t powers_at(int32_t in) { return D == 128 ? in * 4 : (in & ~1) * 2; }
+    static __device__ __forceinline__ int32_t power_bits(int32_t in) { return D == 128 ? 0 : (in & 1) * 16; }
 };
 
 // Pages of 32 tokens and more: 32 keys that begin at a multiple of 32 are in one.  It is looked up when they are asked for, among 64 entries of the table that the lanes hold, and the
@@ -283,7 +289,8 @@ template <int D, bool FEW, bool ONE> struct MxStream {
     MxSource<D> src;
     int32_t n, base, first, step, skip;
     MxOnePage<D> one;
-    int32_t k_at, kp_at, v_at, vp_at;  // ONE: bytes of the lane's share in a block's numbers and powers
+    int32_t k_at, kp_at, v_at, vp_at;  // ONE: bytes of the lane's share in a block's numbers, and of the powers of its keys
+    int32_t k_bits, v_bits;            // where the powers of its share are among four.  (Keys past the last are the last's in other places: nobody sees them.)
 
     __device__ __forceinline__ void init(const AttnArgs &a, const AttnUnit &u, int kv_head, int first_, int step_)
     {
@@ -297,9 +304,11 @@ template <int D, bool FEW, bool ONE> struct MxStream {
         skip = first == 0 && u.key0 > base ? 1 : 0;
         const int lane = threadIdx.x & 63, g = lane >> 4, half = lane >> 5, r = lane & 31;
         v_at = r * P::NUMBERS + half * (16 * MINE);
-        vp_at = r * P::POWERS + half * MINE;
+        vp_at = src.powers_at(r);
+        v_bits = src.power_bits(r) + 8 * half * MINE;
         k_at = FEW ? (lane & 15) * P::NUMBERS + g * (D / 8) : v_at;
-        kp_at = FEW ? (lane & 15) * P::POWERS + g * P::POWERS / 4 : vp_at;
+        kp_at = FEW ? src.powers_at(lane & 15) : vp_at;
+        k_bits = FEW ? src.power_bits(lane & 15) + 8 * (g * P::POWERS / 4) : v_bits;
         if (ONE && n > 0) one.init(src, key_of(0));                // no key: the table may have no entry
     }
     __device__ __forceinline__ int32_t key_of(int32_t i) const { return base + (first + step * (i + skip < n ? i + skip : i + skip - n)) * 32; }
@@ -324,18 +333,18 @@ template <int D, bool FEW, bool ONE> struct MxStream {
             if constexpr (!FEW) {
 #pragma unroll
                 for (int j = 0; j < MINE; ++j) words(b, 4 * j, __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, k_at + 16 * j, numbers, 0)));
-                b.kp[0] = MINE == 2 ? __builtin_amdgcn_raw_buffer_load_b16(k, kp_at, powers, 0) : __builtin_amdgcn_raw_buffer_load_b8(k, kp_at, powers, 0);
+                b.kp[0] = __builtin_amdgcn_raw_buffer_load_b32(k, kp_at, powers, 0);
             } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if constexpr (D == 128) words(b, 4 * h, __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, k_at + 16 * h * P::NUMBERS, numbers, 0)));
                     else two_words(b, 2 * h, __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(k, k_at + 16 * h * P::NUMBERS, numbers, 0)));
-                    b.kp[h] = __builtin_amdgcn_raw_buffer_load_b8(k, kp_at + 16 * h * P::POWERS, powers, 0);
+                    b.kp[h] = __builtin_amdgcn_raw_buffer_load_b32(k, kp_at + 16 * h * P::POWERS, powers, 0);
                 }
             }
 #pragma unroll
             for (int j = 0; j < MINE; ++j) b.v[j] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(v, v_at + 16 * j, numbers, 0));
-            b.vp = MINE == 2 ? __builtin_amdgcn_raw_buffer_load_b16(v, vp_at, powers, 0) : __builtin_amdgcn_raw_buffer_load_b8(v, vp_at, powers, 0);
+            b.vp = __builtin_amdgcn_raw_buffer_load_b32(v, vp_at, powers, 0);
         } else {
             const int g = lane >> 4, half = lane >> 5;
             const int32_t key = key_of(min(i, n - 1));
@@ -347,15 +356,15 @@ template <int D, bool FEW, bool ONE> struct MxStream {
             for (int h = 0; h < (FEW ? 2 : 1); ++h) {
                 from[h] = src.page_at(b.page[h]);
                 in[h] = src.in_page(key + 16 * h + (FEW ? lane & 15 : lane & 31));
-                const gcptr_t row = k + from[h] + in[h] * P::NUMBERS, power = k + from[h] + powers + in[h] * P::POWERS;
+                const gcptr_t row = k + from[h] + in[h] * P::NUMBERS, power = k + from[h] + powers + src.powers_at(in[h]);
                 if constexpr (FEW) {
                     if constexpr (D == 128) words(b, 4 * h, ld16(row + g * 16));
                     else two_words(b, 2 * h, ld8(row + g * 8));
-                    b.kp[h] = *(const PREFT_GLOBAL uint8_t *)(power + g * P::POWERS / 4);
+                    b.kp[h] = ld4(power);
                 } else {
 #pragma unroll
                     for (int j = 0; j < MINE; ++j) words(b, 4 * j, ld16(row + half * (16 * MINE) + 16 * j));
-                    b.kp[0] = few_bytes(power + half * MINE);
+                    b.kp[0] = ld4(power);
                 }
             }
             const bool second = FEW && (lane & 16);
@@ -363,13 +372,8 @@ template <int D, bool FEW, bool ONE> struct MxStream {
             const int32_t at = second ? in[1] : in[0];
 #pragma unroll
             for (int j = 0; j < MINE; ++j) b.v[j] = ld16(v + page + at * P::NUMBERS + half * (16 * MINE) + 16 * j);
-            b.vp = few_bytes(v + page + powers + at * P::POWERS + half * MINE);
+            b.vp = ld4(v + page + powers + src.powers_at(at));
         }
-    }
-    static __device__ __forceinline__ uint32_t few_bytes(gcptr_t p)
-    {
-        if constexpr (MINE == 2) return *(const PREFT_GLOBAL uint16_t *)p;
-        else return *(const PREFT_GLOBAL uint8_t *)p;
     }
     static __device__ __forceinline__ void words(Block &b, int at, u32x4_t x)
     {
@@ -415,8 +419,9 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
     // this thread's row of the tile, and 32 elements of it; heads of 64: two wavefronts have K and two V
     const int r = (lane & 31) + 32 * (wave & 1), block = D == 128 ? 2 * (lane >> 5) + (wave >> 1) : lane >> 5;
     const bool has_k = D == 128 || wave < 2, has_v = D == 128 || wave >= 2;
+    const int bits = src.power_bits(r) + 8 * block;              // of its power among four
     u32x4_t kn = {}, vn = {};
-    uint32_t kp = 127, vp = 127, page = 0;
+    uint32_t kp = 0, vp = 0, page = 0;
     MxOnePage<D> one;
     if (ONE && n > 0) one.init(src, key_of(0) + 32 * (wave & 1));
     auto look = [&](int32_t i) {
@@ -426,21 +431,21 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
         if constexpr (ONE) {
             const bool there = i < n;
             const auto [k, v, numbers, powers] = one.at(src, key_of(there ? i : 0) + 32 * (wave & 1), there);
-            const int at = (lane & 31) * P::NUMBERS + block * 16, power_at = (lane & 31) * P::POWERS + block;
+            const int at = (lane & 31) * P::NUMBERS + block * 16, power_at = src.powers_at(lane & 31);
             if (has_k) {
                 kn = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(k, at, numbers, 0));
-                kp = __builtin_amdgcn_raw_buffer_load_b8(k, power_at, powers, 0);
+                kp = __builtin_amdgcn_raw_buffer_load_b32(k, power_at, powers, 0);
             }
             if (has_v) {
                 vn = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(v, at, numbers, 0));
-                vp = __builtin_amdgcn_raw_buffer_load_b8(v, power_at, powers, 0);
+                vp = __builtin_amdgcn_raw_buffer_load_b32(v, power_at, powers, 0);
             }
         } else {
             const int64_t at = src.page_at(page);
             const int32_t in = src.in_page(key_of(min(i, n - 1)) + r);
-            const int64_t numbers = at + in * P::NUMBERS + block * 16, power = at + ((int64_t)P::NUMBERS << src.page_shift) + in * P::POWERS + block;
-            if (has_k) { kn = ld16(as_global((const void *)src.k) + numbers); kp = *(const PREFT_GLOBAL uint8_t *)(as_global((const void *)src.k) + power); }
-            if (has_v) { vn = ld16(as_global((const void *)src.v) + numbers); vp = *(const PREFT_GLOBAL uint8_t *)(as_global((const void *)src.v) + power); }
+            const int64_t numbers = at + in * P::NUMBERS + block * 16, power = at + ((int64_t)P::NUMBERS << src.page_shift) + src.powers_at(in);
+            if (has_k) { kn = ld16(as_global((const void *)src.k) + numbers); kp = ld4(as_global((const void *)src.k) + power); }
+            if (has_v) { vn = ld16(as_global((const void *)src.v) + numbers); vp = ld4(as_global((const void *)src.v) + power); }
         }
     };
     MxColumns<E, D> w;
@@ -458,14 +463,15 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
     auto v_tile = [&](int32_t i) { return lds + 2 * X::K_TILE + (i & 1) * X::V_TILE; };
     // tile i, which is in registers, to LDS; `bad`: for each 32 keys and 32 elements of the tile the keys that are NaN there
     auto put = [&](int32_t i) {
-        if (has_k) mx4_put(k_tile(i) + r * X::K_PITCH + 64 * block, kn, kp);
+        if (has_k) mx4_put(k_tile(i) + r * X::K_PITCH + 64 * block, kn, mx4_power_of(kp, bits));
         if (has_v) {
+            uint32_t power = mx4_power_of(vp, bits);
             if (i >= full) {
                 const int32_t key = key_of(i) + r;
-                const uint64_t nan = __ballot(mx4_clean(vn, vp, key >= u.key0 && key < u.key1));
+                const uint64_t nan = __ballot(mx4_clean(vn, power, key >= u.key0 && key < u.key1));
                 if (lane % 32 == 0) bad[(i & 1) * 8 + (wave & 1) * 4 + block] = (uint32_t)(nan >> lane);
             }
-            mx4_put(v_tile(i) + X::v_row(r) + 64 * block, vn, vp);
+            mx4_put(v_tile(i) + X::v_row(r) + 64 * block, vn, power);
         }
         if (i + 1 < n) fetch(i + 1);
         if (i + 2 < n) look(i + 2);
@@ -569,11 +575,11 @@ template <typename E, int D> struct MxFewColumns {
 
     // S^T of 16 keys twice: a lane's quarter of its two keys
     struct Scores { f32x4_t s[2]; };
-    __device__ __forceinline__ void scores(Scores &r, const uint32_t (&k)[2 * STEPS], const uint32_t (&power)[2]) const
+    __device__ __forceinline__ void scores(Scores &r, const uint32_t (&k)[2 * STEPS], const uint32_t (&powers)[2], int bits) const
     {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float scale = mx4_scale(power[h]);
+            const float scale = mx4_scale(mx4_power_of(powers[h], bits));
             r.s[h] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
@@ -706,11 +712,11 @@ __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit
     auto block = [&](auto &b, int32_t i, bool more) {
         const int32_t key = st.key_of(i);
         typename C::Scores s;
-        w.scores(s, b.k, b.kp);
+        w.scores(s, b.k, b.kp, st.k_bits);
         u32x4_t v[X::MINE];
         uint32_t vp[X::MINE];
 #pragma unroll
-        for (int j = 0; j < X::MINE; ++j) { v[j] = b.v[j]; vp[j] = (b.vp >> (8 * j)) & 255u; }
+        for (int j = 0; j < X::MINE; ++j) { v[j] = b.v[j]; vp[j] = mx4_power_of(b.vp, st.v_bits + 8 * j); }
         uint64_t bad[X::MINE] = {};
         if (i >= full) {
             const int32_t mine = key + r;
@@ -751,7 +757,7 @@ __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit
 template <typename E, int D, bool SOLO>
 __device__ __forceinline__ void mx_attend_narrow(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)
 {
-    constexpr int AHEAD = 3, AHEAD_WIDE = sizeof(E) == 2 ? 2 : 1;             // as many as registers allow
+    constexpr int AHEAD = 2, AHEAD_WIDE = sizeof(E) == 2 ? 2 : 1;             // as many as registers allow
     const bool one = a.page_shift >= 5;
     if (u.ncols <= MX_FEW_COLS) {
         if (one) mx_attend_keys<E, D, MxFewColumns<E, D>, AHEAD, SOLO, true>(a, u, kv_head, lds, join);
