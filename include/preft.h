@@ -455,7 +455,7 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
  *   n[i], n[j] <- n[i] c - n[j] s, n[j] c + n[i] s      for the rotary_dim / 2 pairs i, j of its first rotary_dim elements; pairs says which they are:
  *                                          PREFT_PAIRS_HALVES  p and p + rotary_dim / 2;  PREFT_PAIRS_ADJACENT  2 p and 2 p + 1;
  * with the cosine c = rotation[position][p] and the sine s = rotation[position][rotary_dim / 2 + p], a table [n_positions, rotary_dim] in fp32, 16-byte aligned, that the caller makes
- * once (any base, any stretching of positions).  rotary_dim: a multiple of 16, up to head_dim; 0 turns nothing (positions and rotation may then be NULL).  positions [T]: as
+ * once (any base, any stretching of positions).  rotary_dim: a multiple of 16, up to head_dim; 0 turns nothing (rotation is not looked at).  positions [T] (NULL where nothing is turned and no row is padding): as
  * preft_kv_plan writes them; those past the table count as its last.  A row whose position is negative is padding: nothing of it is written, in rows or pages.
  * Computed in 64 bits from the inputs and the table, and rounded once to the rows' type (through fp32), so that a number on the border of two 4-bit numbers falls where the
  * formula puts it.  Infinities and NaN stay within their head.

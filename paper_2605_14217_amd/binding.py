@@ -753,13 +753,14 @@ def _turned(T: int, dim: int, dtype, positions, rotation, q_weight, k_weight):
         if w is not None and (w.dtype is not dtype or w.numel() != dim or not w.is_cuda or not w.is_contiguous()):
             raise ValueError(f"{name}: need a contiguous device tensor of {dim} entries and the dtype of the rows")
         weights.append(None if w is None else w.data_ptr())
+    at = None if positions is None else _table(positions, "positions", T)
     if rotation is None:
-        return weights, (None, None, 0, 0)
+        return weights, (at, None, 0, 0)
     if rotation.dim() != 2 or rotation.dtype is not _FP32 or not rotation.is_cuda or not rotation.is_contiguous():
         raise ValueError("rotation: need a contiguous float32 device tensor [n_positions, rotary_dim]")
     if positions is None:
         raise ValueError("positions: needed with a rotation")
-    return weights, (_table(positions, "positions", T), rotation.data_ptr(), rotation.shape[0], rotation.shape[1])
+    return weights, (at, rotation.data_ptr(), rotation.shape[0], rotation.shape[1])
 
 
 def _head_rows(out, x, name: str, n_heads: int, dim: int, T: Optional[int], dtype, optional: bool = False):

@@ -154,11 +154,11 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
     constexpr int PE = H::PE;
     __shared__ __align__(16) char lds[PAGES == MX4_PAGES ? 4 * 2048 : 16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane / H::LANES, j = lane % H::LANES;
-    const int64_t task = (int64_t)blockIdx.x * 4 + wave;
-    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(task / a.splits)), part = __builtin_amdgcn_readfirstlane((int32_t)(task % a.splits));
-    if (row >= a.T) return;
+    const uint32_t task = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + wave)), at = task / (uint32_t)a.splits;
+    if (at >= (uint32_t)a.T) return;
+    const int32_t row = (int32_t)at, part = (int32_t)(task - at * (uint32_t)a.splits);
     int32_t position = 0;
-    if (a.rot > 0) {
+    if (a.positions) {
         position = as_const(a.positions)[row];
         if (position < 0) return;                             // padding
         position = min(position, a.n_positions - 1);
@@ -252,8 +252,9 @@ __global__ __launch_bounds__(256) void mx4_fetch_kernel(FetchArgs a)
     using H = Heads<E, D>;
     constexpr int N = 2 * H::PE, SHARE = MX4_BLOCK / N;
     const int lane = threadIdx.x & 63, h = lane / H::LANES, j = lane % H::LANES;
-    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-    if (row >= a.T) return;
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    if (at >= (uint32_t)a.T) return;
+    const int32_t row = (int32_t)at;
     const int64_t slot = as_const(a.slot_map)[row];
     if (slot < 0 || slot >= a.n_slots) return;
     const int32_t in = (int32_t)(slot & (((int64_t)1 << a.page_shift) - 1));

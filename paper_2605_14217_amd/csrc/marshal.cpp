@@ -434,10 +434,11 @@ struct Turned { int32_t *positions; const float *rotation; int32_t n, rot, pairs
 bool as_turned(PyObject *const *o, PyObject *const *w, int32_t T, int32_t dim, at::ScalarType type, Turned &t)
 {
     t = {};
+    if (o[0] != Py_None && !as_table(o[0], T, t.positions)) return false;
     if (o[1] != Py_None) {
         const at::Tensor *r = tensor(o[1]);
         if (!r || r->dim() != 2 || r->scalar_type() != at::kFloat || !r->is_cuda() || !r->is_contiguous() || r->size(0) > INT32_MAX || r->size(1) > INT32_MAX ||
-            !as_table(o[0], T, t.positions)) return false;
+            o[0] == Py_None) return false;
         t.rotation = static_cast<const float *>(r->data_ptr());
         t.n = (int32_t)r->size(0);
         t.rot = (int32_t)r->size(1);

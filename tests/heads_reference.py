@@ -30,7 +30,7 @@ def turned(x, heads, weight, eps, positions, rotation, pairs):
     half = torch.finfo(x.dtype).eps / 2
     bound = (half + 2.0 ** -24) * h.abs() * 1.001 + 2.0 ** -44 * size + 1e-40
     h, bound = h.reshape(T, -1), bound.reshape(T, -1)
-    if rotation is not None:
+    if positions is not None:
         h[positions < 0] = float("nan")
     return h, bound
 

@@ -35,7 +35,7 @@ class Case:
         if T > 4:
             slot[2] = self.n_pages * page
         self.slot = torch.from_numpy(slot)
-        self.real = torch.ones(T, dtype=torch.bool) if rot == 0 else self.positions >= 0
+        self.real = self.positions >= 0
 
     def dev(self):
         d = lambda t: None if t is None else t.cuda()  # noqa: E731
