@@ -6,6 +6,7 @@
 #include "attention_mx.hpp"
 #include "attention_plan.hpp"
 
+#include <algorithm>
 #include <cmath>
 
 namespace {
@@ -22,7 +23,11 @@ int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
     else hipLaunchKernelGGL((attention_kernel<E, D, KEYS == PAGES, DIRECT>), grid, dim3(256), 0, st, a);
     if (p.merge) {
         const unsigned tiles = (unsigned)(a.s.l.merge_cap < 1024 ? a.s.l.merge_cap : 1024);
-        const unsigned z = tiles * (unsigned)a.s.kv_heads < 256 && (int64_t)a.s.T * a.s.group > 4 ? 16u : 1u;      // workgroups that share a tile's columns
+        unsigned z = tiles * (unsigned)a.s.kv_heads < 256 && (int64_t)a.s.T * a.s.group > 4 ? 16u : 1u;      // workgroups that share a tile's columns
+        // 4-bit pages: a wavefront takes a microsecond a column, and tiles of 16 columns and more on average are shared by up to 2048 workgroups in all (28 requests of 8 rows with 4 prefixes
+        // of 10 544 tokens, 32 heads over 8: 74 us, of which the join took 19 of 84)
+        if (KEYS == MX_PAGES && z == 1 && (int64_t)a.s.T * a.s.group >= 16 * (int64_t)a.s.l.merge_cap)
+            z = std::max(1u, std::min(8u, 2048u / (tiles * (unsigned)a.s.kv_heads)));
         hipLaunchKernelGGL((attention_merge_kernel<E, D>), dim3(tiles, (unsigned)a.s.kv_heads, z), dim3(256), 0, st, a, KEYS == PACKED ? 1 : 2);
     }
     return launched();
@@ -58,8 +63,6 @@ int check_call(int32_t T, int32_t S, int32_t heads, int32_t kv_heads, int32_t he
     return sizes_fit(T, S, heads, groups) ? PREFT_OK : PREFT_ETOOLARGE;
 }
 
-constexpr int32_t ATTN_MX_TYPE = 0x10;
-
 int cached_call(Keys keys_in, void *out, int64_t ldo, const void *q, int64_t ldq, int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                 const int32_t *seg_start, const int32_t *seg_prefill_len, const int32_t *kv_len, int32_t S, const void *k_cache, const void *v_cache, int32_t n_pages,
                 int32_t page_size, const int32_t *block_table, int64_t ld_table, int32_t max_pages, const int32_t *group_start, const int32_t *group_prefix_len,
@@ -93,13 +96,8 @@ int cached_call(Keys keys_in, void *out, int64_t ldo, const void *q, int64_t ldq
     s.S = S; s.T = T; s.n_groups = n_groups; s.heads = n_heads; s.kv_heads = n_kv_heads; s.group = n_heads / n_kv_heads; s.l = lists_of(l, workspace);
     a.per_head = ((1u << 21) + (uint32_t)s.group - 1) / (uint32_t)s.group;
     const int64_t most_keys = keys ? (int64_t)max_pages << shift : 0;
-    if (keys_in == PAGES) {
-        cached_rules(s, dtype, most_keys);
-        return run<PAGES>(a, dtype, head_dim, mode, st);
-    }
-    cached_rules(s, PREFT_BF16, most_keys);            // the products are bf16's, whatever the queries are
-    s.dtype = ATTN_MX_TYPE | dtype;                    // and the schedule is no other pages'
-    return run<MX_PAGES>(a, dtype, head_dim, mode, st);
+    cached_rules(s, keys_in == MX_PAGES ? ATTN_MX_TYPE | dtype : dtype, most_keys);
+    return keys_in == MX_PAGES ? run<MX_PAGES>(a, dtype, head_dim, mode, st) : run<PAGES>(a, dtype, head_dim, mode, st);
 }
 
 }  // namespace

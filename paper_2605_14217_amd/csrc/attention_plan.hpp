@@ -120,13 +120,21 @@ inline void prompt_rules(AttnScheduleArgs &s, int dtype)
     s.min_tiles = s.min_wide;
 }
 
+// A schedule is of one type of pages.
+constexpr int32_t ATTN_MX_TYPE = 0x10;
+
 // A call over pages; most_keys: what a row of the block table has room for.
 inline void cached_rules(AttnScheduleArgs &s, int dtype, int64_t most_keys)
 {
     s.max_keys = (int32_t)(most_keys < (1 << 30) ? most_keys : (1 << 30));
     s.dtype = dtype;
     s.can_split = 1;
-    spread(s, dtype);
+    const bool mx = (dtype & ATTN_MX_TYPE) != 0;
+    const int64_t n = (int64_t)s.l.tile_cap * s.kv_heads;
+    // A second unit on a compute unit takes of the first one's time, and a part has to be written and joined: 16 requests of 40 rows over 1500 tokens, 24 key tiles, 41 us, in two parts 52;
+    // over 3000 tokens 70 and 73.  A key tile of f32 queries takes three times as long (20 requests of 20 rows over 1300..2600 tokens: 150, cut 81).
+    s.fill = mx && n > ATTN_TARGET / 8 && n < ATTN_TARGET && (int64_t)s.T * s.group > (int64_t)s.S * ATTN_FEW_COLS ? ((dtype & 1) == PREFT_BF16 ? 24 : 8) : 0;
+    spread(s, mx ? PREFT_BF16 : dtype);                   // over 4-bit pages the products are bf16's, whatever the queries are
 }
 
 // Few segments and workgroups: the schedule kernel's launch is a third of the call (one decode row over 1500 keys: 17.0 us with it, 11.7 without; 40 chat-length

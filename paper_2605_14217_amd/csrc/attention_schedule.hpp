@@ -61,6 +61,7 @@ struct AttnScheduleArgs {
     const int32_t *kv_len;                                 // null: packed whole prompts
     const int32_t *group_start, *group_prefix;
     int32_t S, T, n_groups, heads, kv_heads, group, max_keys, dtype, can_split, min_tiles, min_wide, spread;    // group: heads / kv_heads; spread: workgroups that a range's length is meant for
+    int32_t fill;          // attn_direct looks for a cut into one full round of workgroups, by ranges of this length at least; 0: no
     AttnLists l;
 };
 
@@ -95,9 +96,9 @@ __device__ __forceinline__ int32_t key_tiles(int32_t key0, int32_t key1) { retur
 
 // A part of a wide tile is 64 KB written and read again, which on a full chip takes the time of some 14 key tiles: cut only where tiles are few, or this one long.
 // (16 requests of 40 rows over 100..2000 tokens: 56 us, cut by `range` 85; one prompt of 900 rows 23 us, cut by 8 key tiles 37; of 2000 rows and 8 heads 33 us cut by 8, uncut 40.)
-__device__ __forceinline__ int32_t wide_range(const AttnScheduleArgs &a, int32_t range)
+__device__ __forceinline__ int32_t wide_range(const AttnScheduleArgs &a, int32_t range, bool filled = false)
 {
-    return max(a.min_wide, a.spread <= ATTN_TARGET / 2 ? min(range, INT32_MAX / 2) * 2 : range);
+    return max(a.min_wide, !filled && a.spread <= ATTN_TARGET / 2 ? min(range, INT32_MAX / 2) * 2 : range);
 }
 __device__ __forceinline__ int32_t ranges_of(int32_t tiles, int32_t range) { return tiles > range ? (int32_t)((uint32_t)(tiles - 1) / (uint32_t)range) + 1 : 1; }
 // where part k of `parts` of n tiles begins: the first n % parts have one more
@@ -410,6 +411,16 @@ __device__ __forceinline__ int32_t wave_inclusive(int32_t v, int32_t n)
     return v;
 }
 
+// One full round of workgroups: with a range of 1/512, else 1/384 of all the work the units may be no more than run side by side, though n tiles cut into ranges of 1/spread make
+// n + spread of them at worst.  For calls with wide tiles; the look takes half a microsecond of each workgroup's.  (4-bit pages, 30 requests of 10 rows over 1000..5000 tokens: 65 us, without
+// it 103; 512 rows over 30 000 tokens 237, 266; 20 requests of 20 f32 rows over 2500..5000 tokens 125, 236.)
+constexpr int ATTN_FILLS = 2;
+__device__ __forceinline__ int32_t fill_range(uint64_t work, int k)
+{
+    const uint32_t spread = ATTN_TARGET - k * (ATTN_TARGET / 4);
+    return (int32_t)min((work + spread - 1) / spread, (uint64_t)INT32_MAX);
+}
+
 // the unit `index` of the call
 __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int32_t index)
 {
@@ -438,16 +449,31 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
     AttnDirect r = {};
     if (__any(back)) return r;
     int32_t range = INT32_MAX;
+    bool filled = false;
+    auto is_wide = [&](int c) { return it[c].rows * G > ATTN_FEW_COLS; };
     if (a.can_split) {
         const int32_t n = min(a.S, 64);
         cost = (uint32_t)__builtin_amdgcn_readlane(wave_inclusive((int32_t)cost, n), n - 1);
         range = max(a.min_tiles, (int32_t)min(((uint64_t)cost * (uint32_t)a.kv_heads + a.spread - 1) / (uint32_t)a.spread, (uint64_t)INT32_MAX));
+        if (a.fill) {
+            const uint64_t work = (uint64_t)cost * (uint32_t)a.kv_heads;
+#pragma unroll
+            for (int k = ATTN_FILLS - 1; k >= 0; --k) {
+                const int32_t to = fill_range(work, k);
+                if (to < a.fill) continue;
+                int32_t units = 0;
+#pragma unroll
+                for (int c = 0; c < EACH; ++c)
+                    if (c * 64 < a.S) units += min(tiles[c] * ranges_of(key_tiles(0, it[c].key1), is_wide(c) ? wide_range(a, to, true) : to), ATTN_TARGET + 1);
+                if (__builtin_amdgcn_readlane(wave_inclusive(units, n), n - 1) * a.kv_heads <= ATTN_TARGET) { range = to; filled = true; }
+            }
+        }
     }
     int32_t before = 0, slots = 0, tiles_before = 0;
 #pragma unroll
     for (int c = 0; c < EACH; ++c) {
         if (c * 64 >= a.S) continue;
-        const int32_t parts = ranges_of(key_tiles(0, it[c].key1), it[c].rows * G > ATTN_FEW_COLS ? wide_range(a, range) : range), units = tiles[c] * parts;
+        const int32_t parts = ranges_of(key_tiles(0, it[c].key1), is_wide(c) ? wide_range(a, range, filled) : range), units = tiles[c] * parts;
         const int32_t need = parts > 1 ? (int32_t)min((int64_t)it[c].rows * G * parts * a.kv_heads, (int64_t)a.l.slot_cap) : 0;
         const int32_t lanes = min(a.S - c * 64, 64);
         const int32_t upto = wave_inclusive(units, lanes), slot = a.can_split ? wave_inclusive(need, lanes) : 0;

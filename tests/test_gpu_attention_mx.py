@@ -193,6 +193,15 @@ def test_one_long_request(dtype, H, Hkv, D):
     c.check(rows={0, 1, 63, 64, 65, 128, 129})
 
 
+@pytest.mark.parametrize("dtype,kv", [("bf16", 3000), ("f32", 1500)])
+def test_tiles_cut_into_one_round_of_workgroups(dtype, kv):
+    """30 tiles of 40 columns for each of 8 heads, which take two parts each, and a join that is shared by several workgroups a tile."""
+    print(f"\n[case] 4-bit one round {dtype}", flush=True)
+    c = Case(dtype, 32, 8, 64, 64, [10] * 30, [kv + 3 * s for s in range(30)], seed=9)
+    c.check(rows={0, 4, 9, 10, 144, 150, 155, 290, 299})
+    assert preft.preft_schedule_counts(c.ws)[1] == 30
+
+
 @pytest.mark.parametrize("most,page,prefix", [(64, 16, 64), (96, 8, 75), (192, 16, 100), (1500, 64, 1100), (700, 16, 256)])
 @pytest.mark.parametrize("dtype,H,Hkv,D", HEADS)
 def test_groups(dtype, H, Hkv, D, most, page, prefix):
