@@ -484,6 +484,10 @@ __device__ __forceinline__ void mx_attend_columns(const AttnArgs &a, const AttnU
         if (i + 1 < n) put(i + 1);
     };
     int32_t i = 0;
+    if (__builtin_expect(wave * 32 >= u.ncols, 0)) {              // no columns: its share of the tiles only (100 requests of 10 rows over 1000..5000 tokens: 147 us, 170 with their products)
+        for (; i < n; ++i) arrive(i);
+        return;
+    }
     for (; i < full; ++i) {
         arrive(i);
         const lds_t kt = k_tile(i), vt = v_tile(i);
