@@ -401,8 +401,8 @@ __device__ __forceinline__ void mx4_put(lds_t to, u32x4_t numbers, uint32_t powe
 
 // ---------------------------------------------------------------------------------------
 // A unit of more than 32 columns: as in attend_columns, but the tiles of 64 keys come through registers: each thread has 32 numbers of K and 32 of V (heads of 64: of one)
-// of the tile after next on their way while this one's products run.  Four requests' further chunks, 6000 rows over 5000..17 000 tokens, 32 heads over 8 of 128: 867 us, 1150 TFLOP/s, 96 % of
-// a large matrix product's 1200; before the wavefronts' priorities and the weights without a look for the largest score 999, with them 958, with scalar addresses 900, with reads ordered ahead of the
+// of the tile after next on their way while this one's products run.  Four requests' further chunks, 6000 rows over 5000..17 000 tokens, 32 heads over 8 of 128: 867-885 us, 1120-1150 TFLOP/s, 93-96 %
+// of a large matrix product's 1200; before the wavefronts' priorities and the weights without a look for the largest score 999, with them 958, with scalar addresses 900, with reads ordered ahead of the
 // products and rows at a pitch 867 (half of the products of a tile stood waiting for LDS; a K tile further ahead, its products beside the exponentials, took 1040).
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, bool ONE>
@@ -687,6 +687,9 @@ template <typename E, int D> struct MxFewColumns {
 // ---------------------------------------------------------------------------------------
 // A unit of up to 32 columns (C: MxColumns), or up to 16 (MxFewColumns): bound by the bytes of its keys.  The four wavefronts take blocks of 32 keys in turn, AHEAD of them on their way in
 // registers, V through LDS of their own without a barrier, and join their sums at the end.  SOLO: the unit is one wavefront's.
+// 512 rows over 4000 tokens, 32 heads over 8 of 128: 395 us, 5.6 TB/s (reads alone come at up to 6.8); 224 rows over 256..4096 tokens 110 us with their schedule and join, 5.4 TB/s in the kernel.
+// Units of 32 columns on 32x32x16 products alone 117.7; powers loaded as bytes, after which a loop waits at its end for all loads, 114.  Four blocks ahead: 129 in pages of 16 (heads of 64: 48 us, two
+// ahead 40; the waits are not for memory).
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, typename C, int AHEAD, bool SOLO, bool ONE>
 __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)
