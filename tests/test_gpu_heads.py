@@ -131,6 +131,42 @@ def test_append(dtype, heads, kv_heads, dim, pairs, rot, norm, mx4):
                 np.testing.assert_array_equal(back.cpu().double().numpy(), want.reshape(T, -1))
 
 
+@pytest.mark.parametrize("dtype,heads,kv_heads,dim,rot", [("bf16", 4, 2, 128, 112), ("bf16", 3, 1, 128, 80), ("f32", 3, 2, 128, 112), ("f32", 2, 2, 64, 48), ("bf16", 1024, 1024, 64, 32)])
+def test_other_shares_that_turn_and_the_most_heads(dtype, heads, kv_heads, dim, rot):
+    """Shares of a head that are no power of two, whose last lanes turn nothing; and as many heads as there may be."""
+    for pairs in (0, 1):
+        c = Case(DTYPE[dtype], heads, kv_heads, dim, 19, rot, True, seed=rot)
+        q_out, k_out = torch.full_like(c.q, 7.0), torch.full_like(c.k, 7.0)
+        preft.preft_qk_rotate(q_out, c.q, k_out, c.k, n_heads=heads, n_kv_heads=kv_heads, pairs=pairs, **c.dev())
+        for out, x, n, w in ((q_out, c.q, heads, c.weights[0]), (k_out, c.k, kv_heads, c.weights[1])):
+            ref.check_rows(out, torch.full_like(out, 7.0), *c.want(x, n, w, pairs), c.real)
+
+
+@pytest.mark.parametrize("mx4", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_rows_with_one_slot(dtype, mx4):
+    """Every 16 bytes of pages of activations, every number and every power of 4-bit pages, are one row's or the other's; nothing else is touched."""
+    heads, dim, page, T = 3, 64, 8, 40
+    c = Case(DTYPE[dtype], 2, heads, dim, T, 0, False, seed=5, pad=False)
+    slot = torch.arange(T) // 2 * 3                            # rows 2 i and 2 i + 1 to slot 3 i
+    n_pages = 3 * T // 2 // page + 1
+    append = preft.preft_kv_append_mx if mx4 else preft.preft_kv_append
+    results = []
+    for rows in (slice(0, T), slice(0, T, 2), slice(1, T, 2)):
+        caches = [torch.full((n_pages, heads, page, dim * 17 // 32), 0x5a, dtype=torch.uint8, device="cuda") if mx4 else
+                  torch.full((n_pages, heads, page, dim), 9.0, dtype=c.dtype, device="cuda") for _ in "kv"]
+        append(*caches, None, None, None, c.k[rows], c.v[rows], slot[rows].contiguous().cuda(), None, None, 0)
+        results.append([x.cpu() for x in caches])
+    for both, first, second in zip(*results):
+        if mx4:
+            parts = [ref.split(x.numpy(), dim) for x in (both, first, second)]
+            for x, a, b in zip(*parts):
+                assert ((x == a) | (x == b)).all()
+        else:
+            x, a, b = (t.reshape(-1).view(torch.int32).reshape(-1, 4) for t in (both, first, second))
+            assert bool(((x == a).all(1) | (x == b).all(1)).all())
+
+
 @pytest.mark.parametrize("T", [1000, 4500])
 def test_many_rows(T):
     """A row's heads are one wavefront's or several's, by the rows."""
