@@ -412,7 +412,8 @@ __device__ __forceinline__ int32_t wave_inclusive(int32_t v, int32_t n)
 }
 
 // One full round of workgroups: with a range of 1/512, else 1/384 of all the work the units may be no more than run side by side, though n tiles cut into ranges of 1/spread make
-// n + spread of them at worst.  For calls with wide tiles; the look takes half a microsecond of each workgroup's.  (4-bit pages, 30 requests of 10 rows over 1000..5000 tokens: 65 us, without
+// n + spread of them at worst.  Half as many again are taken too where the longest tile takes longer than a part and an even share of the work (8 prompts of 100..200 rows over 1000..15 000 tokens,
+// 4-bit pages: 238 us, without it 314).  For calls with wide tiles; the look takes half a microsecond of each workgroup's.  (4-bit pages, 30 requests of 10 rows over 1000..5000 tokens: 65 us, without
 // it 103; 512 rows over 30 000 tokens 237, 266; 20 requests of 20 f32 rows over 2500..5000 tokens 125, 236.)
 constexpr int ATTN_FILLS = 2;
 __device__ __forceinline__ int32_t fill_range(uint64_t work, int k)
@@ -457,6 +458,7 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
         range = max(a.min_tiles, (int32_t)min(((uint64_t)cost * (uint32_t)a.kv_heads + a.spread - 1) / (uint32_t)a.spread, (uint64_t)INT32_MAX));
         if (a.fill) {
             const uint64_t work = (uint64_t)cost * (uint32_t)a.kv_heads;
+            bool over[ATTN_FILLS] = {};
 #pragma unroll
             for (int k = ATTN_FILLS - 1; k >= 0; --k) {
                 const int32_t to = fill_range(work, k);
@@ -465,7 +467,21 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
 #pragma unroll
                 for (int c = 0; c < EACH; ++c)
                     if (c * 64 < a.S) units += min(tiles[c] * ranges_of(key_tiles(0, it[c].key1), is_wide(c) ? wide_range(a, to, true) : to), ATTN_TARGET + 1);
-                if (__builtin_amdgcn_readlane(wave_inclusive(units, n), n - 1) * a.kv_heads <= ATTN_TARGET) { range = to; filled = true; }
+                units = __builtin_amdgcn_readlane(wave_inclusive(units, n), n - 1) * a.kv_heads;
+                if (units <= ATTN_TARGET) { range = to; filled = true; }
+                over[k] = units > ATTN_TARGET && units <= ATTN_TARGET + ATTN_TARGET / 2;
+            }
+            if (!filled && (over[0] || over[1])) {
+                int32_t longest = 0;
+#pragma unroll
+                for (int c = 0; c < EACH; ++c)
+                    if (tiles[c] > 0) longest = max(longest, key_tiles(0, it[c].key1));
+                for (int off = 32; off > 0; off >>= 1) longest = max(longest, __shfl_xor(longest, off, 64));
+#pragma unroll
+                for (int k = ATTN_FILLS - 1; k >= 0; --k) {
+                    const int32_t to = fill_range(work, k);
+                    if (!filled && over[k] && to + work / ATTN_TARGET < (uint64_t)longest) { range = to; filled = true; }
+                }
             }
         }
     }

@@ -19,6 +19,15 @@ def test_one_full_round(driver, rows, kv, units, units_f32):  # noqa: F811
         assert direct and split and merge and got == want <= grid
 
 
+def test_a_little_more_than_one_round(driver):  # noqa: F811
+    """40 tiles of 16 to 140 key tiles, 8 heads: by 1/384 of the work they make more than 512 workgroups and fewer than 768, a part and an even share of the work are shorter than the longest tile."""
+    kv = [1000 + 200 * s for s in range(40)]
+    (direct, split, merge, got, grid, _), = answers(driver, [call(CACHED, MX | BF16, 32, 8, [10] * 40, kv=kv, max_keys=16384)])
+    tiles = [-(-k // 64) for k in kv]
+    to = -(-sum(tiles) * 8 // 384)
+    assert direct and split and merge and got == sum(-(-n // to) for n in tiles) <= grid and 64 < got <= 96
+
+
 @pytest.mark.parametrize("seed", range(3))
 def test_random_calls_of_wide_tiles(driver, seed):  # noqa: F811
     """Around the sizes that it is for: tiles of all key/value heads between 64 and 512, lengths alike and not, tables short and long; and the lists that groups need."""
