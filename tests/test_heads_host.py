@@ -32,7 +32,7 @@ def test_rotate_refusals(lib):
     for bad in (dict(qo=A + 8), dict(ldq=2052), dict(qw=D_ + 2), dict(kw=D_ + 8), dict(rot=F + 4)):
         assert rotate(lib, **bad) == -3, bad
     # the rows' own place, or beside them, is no overlap: the call gets as far as the weights
-    for good in (dict(qo=B, ldqo=2048), dict(ko=B + 2048, ldko=2048), dict(qo=B, ldqo=2048, ko=B + 2048, ldko=2048), dict(qo=B + 3072 - 512, ldqo=2048, H=2, q=B)):
+    for good in (dict(qo=B, ldqo=2048), dict(ko=B + 2048, ldko=2048), dict(qo=B, ldqo=2048, ko=B + 2048, ldko=2048), dict(qo=B + 2560, ldqo=2048, H=2, q=B)):
         assert rotate(lib, qw=D_ + 2, **good) == -3, good
     assert rotate(lib, T=0) == 0 and rotate(lib, H=0, Hkv=0) == 0
     assert rotate(lib, H=0, Hkv=0, qo=None, q=None, ko=None, k=None, pos=None, rot=None, n=0, rdim=0) == 0
