@@ -290,8 +290,21 @@ __global__ __launch_bounds__(256) void mx4_fetch_kernel(FetchArgs a)
     }
 }
 
+int launch_fetch(const FetchArgs &a, int dtype, int32_t head_dim, hipStream_t st)
+{
+    const dim3 grid((unsigned)(((int64_t)a.T + 3) / 4), 2), block(256);
+    if (dtype == PREFT_BF16) {
+        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 64>), grid, block, 0, st, a);
+    } else {
+        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<float, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((mx4_fetch_kernel<float, 64>), grid, block, 0, st, a);
+    }
+    return launched();
+}
+
 template <int PAGES, bool HALVES>
-int launch_heads(const HeadsArgs &a, int dtype, int32_t head_dim, hipStream_t st)
+int launch_rows(const HeadsArgs &a, int dtype, int32_t head_dim, hipStream_t st)
 {
     const dim3 grid((unsigned)(((int64_t)a.T * a.splits + 3) / 4)), block(256);
     if (dtype == PREFT_BF16) {
@@ -302,6 +315,21 @@ int launch_heads(const HeadsArgs &a, int dtype, int32_t head_dim, hipStream_t st
         else hipLaunchKernelGGL((heads_kernel<float, 64, PAGES, HALVES>), grid, block, 0, st, a);
     }
     return launched();
+}
+
+template <int PAGES, bool HALVES>
+int launch_heads(const HeadsArgs &call, int dtype, int32_t head_dim, hipStream_t st)
+{
+    int rc = PREFT_OK;
+    for (int64_t row = 0; row < call.T && rc == PREFT_OK; row += ROWS_A_LAUNCH) {
+        HeadsArgs a = call;
+        a.T = rows_of_launch(call.T, (int32_t)row);
+        a.q = moved(call.q, row * call.ldq); a.k = moved(call.k, row * call.ldk); a.v = moved(call.v, row * call.ldv);
+        a.q_out = moved(call.q_out, row * call.ldqo); a.k_out = moved(call.k_out, row * call.ldko);
+        a.positions = moved(call.positions, row); a.slot_map = moved(call.slot_map, row);
+        rc = launch_rows<PAGES, HALVES>(a, dtype, head_dim, st);
+    }
+    return rc;
 }
 
 // Rows that a call writes over its own input do so in place; any other overlap is refused.
@@ -422,18 +450,15 @@ int preft_kv_fetch_mx(void *k, int64_t ldk, void *v, int64_t ldv, int32_t T, int
     for (const Span &o : {Span{k, ((int64_t)(T - 1) * ldk + width) * e}, Span{v, ((int64_t)(T - 1) * ldv + width) * e}})
         if (o.meets({k_cache, cache}) || o.meets({v_cache, cache})) return PREFT_EINVAL;
     FetchArgs a;
-    a.k = (char *)k; a.v = (char *)v; a.k_cache = (const char *)k_cache; a.v_cache = (const char *)v_cache; a.slot_map = slot_map;
-    a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.T = T; a.kv_heads = n_kv_heads; a.page_shift = shift;
-    const dim3 grid((unsigned)(((int64_t)T + 3) / 4), 2), block(256);
+    a.k_cache = (const char *)k_cache; a.v_cache = (const char *)v_cache;
+    a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.kv_heads = n_kv_heads; a.page_shift = shift;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (dtype == PREFT_BF16) {
-        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 64>), grid, block, 0, st, a);
-    } else {
-        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<float, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((mx4_fetch_kernel<float, 64>), grid, block, 0, st, a);
+    for (int64_t row = 0; row < T && rc == PREFT_OK; row += ROWS_A_LAUNCH) {
+        a.T = rows_of_launch(T, (int32_t)row);
+        a.k = (char *)k + row * a.ldk; a.v = (char *)v + row * a.ldv; a.slot_map = slot_map + row;
+        rc = launch_fetch(a, dtype, head_dim, st);
     }
-    return launched();
+    return rc;
 }
 
 }  // extern "C"
