@@ -79,3 +79,16 @@ def test_append_and_fetch(mx4):
             assert torch.equal(b[rows], w) and bool(w.any())
             b[rows] = 7.0
             assert bool((b == 7.0).all())
+
+
+def test_store():
+    print(f"\n[case] store {T} rows", flush=True)
+    gen = torch.Generator().manual_seed(4)
+    k, v = (torch.randn(T, DIM, device="cuda", dtype=torch.bfloat16) for _ in "kv")
+    slot, rows = slots(gen), torch.tensor(ROWS, device="cuda")
+    caches = [torch.zeros(PAGES, 1, PAGE, DIM, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    preft.preft_kv_store(*caches, k, v, slot)
+    for cache, x in zip(caches, (k, v)):
+        want = torch.zeros(PAGES * PAGE, DIM, dtype=torch.bfloat16, device="cuda")
+        want[slot[rows]] = x[rows]
+        assert torch.equal(cache.view(-1, DIM), want)
