@@ -16,11 +16,16 @@ using namespace preft;
 enum Keys { PACKED, PAGES, MX_PAGES };                           // where a call's keys are
 
 template <typename E, int D, int KEYS, bool DIRECT>
-int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
+int launch(AttnArgs &a, const Plan &p, hipStream_t st)
 {
-    const dim3 grid((unsigned)(p.units * a.s.kv_heads));
-    if constexpr (KEYS == MX_PAGES) launch_mx_attention(a, (int)sizeof(E), D, DIRECT, grid, st);
-    else hipLaunchKernelGGL((attention_kernel<E, D, KEYS == PAGES, DIRECT>), grid, dim3(256), 0, st, a);
+    // a launch has fewer than 2^32 threads (HIP): units of 2^23 workgroups at once
+    const int64_t most = (1 << 23) / a.s.kv_heads;
+    for (int64_t first = 0; first < p.units; first += most) {
+        const dim3 grid((unsigned)(std::min(p.units - first, most) * a.s.kv_heads));
+        a.first = (int32_t)first;
+        if constexpr (KEYS == MX_PAGES) launch_mx_attention(a, (int)sizeof(E), D, DIRECT, grid, st);
+        else hipLaunchKernelGGL((attention_kernel<E, D, KEYS == PAGES, DIRECT>), grid, dim3(256), 0, st, a);
+    }
     if (p.merge) {
         const unsigned tiles = (unsigned)(a.s.l.merge_cap < 1024 ? a.s.l.merge_cap : 1024);
         unsigned z = tiles * (unsigned)a.s.kv_heads < 256 && (int64_t)a.s.T * a.s.group > 4 ? 16u : 1u;      // workgroups that share a tile's columns
@@ -34,7 +39,7 @@ int launch(const AttnArgs &a, const Plan &p, hipStream_t st)
 }
 
 template <int KEYS, bool DIRECT>
-int launch_typed(const AttnArgs &a, int dtype, int32_t head_dim, const Plan &p, hipStream_t st)
+int launch_typed(AttnArgs &a, int dtype, int32_t head_dim, const Plan &p, hipStream_t st)
 {
     if (dtype == PREFT_BF16)
         return head_dim == 128 ? launch<__bf16, 128, KEYS, DIRECT>(a, p, st) : launch<__bf16, 64, KEYS, DIRECT>(a, p, st);

@@ -34,6 +34,7 @@ struct AttnArgs {
     float scale_log2;
     uint32_t per_head;                // ceil(2^21 / G): x / G = x per_head >> 21 for x < 2048 (G <= 1024)
     int32_t ready;                    // direct calls: the header is there already
+    int32_t first;                    // listed calls: the launch's first unit
 };
 
 constexpr float ATTN_LOWEST = -3.0e38f;   // below every score's exponent, and finite: 2^(-inf - it) is 0, not NaN
@@ -709,7 +710,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
     constexpr int JOIN = 4 * 32 * (D + 4) * 4, KIND = PAGED ? 2 : 1;
     __shared__ __align__(1024) char lds[X::LDS > JOIN ? X::LDS : JOIN];
     __shared__ float join[256];
-    const int32_t unit = (int32_t)blockIdx.x / a.s.kv_heads, kv_head = (int32_t)blockIdx.x % a.s.kv_heads;
+    const int32_t unit = (DIRECT ? 0 : a.first) + (int32_t)blockIdx.x / a.s.kv_heads, kv_head = (int32_t)blockIdx.x % a.s.kv_heads;
     AttnUnit u;
     if constexpr (DIRECT) {
         if (a.ready && !attn_schedule_is(a, KIND)) return;
@@ -718,8 +719,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnArgs a)
         if (!attn_schedule_is(a, KIND)) return;
         // short units: one a wavefront, four a workgroup
         const int32_t units = as_const(a.s.l.header)[AH_UNITS], alone = as_const(a.s.l.header)[AH_SHORT];
-        const int32_t i = unit < alone ? unit : alone + 4 * (unit - alone) + uniform(threadIdx.x >> 6);
-        if (i >= units) return;
+        const uint32_t i = unit < alone ? (uint32_t)unit : (uint32_t)alone + 4u * (uint32_t)(unit - alone) + (uint32_t)uniform(threadIdx.x >> 6);     // units: fewer than 2^30
+        if (i >= (uint32_t)units) return;
         const PREFT_CONST AttnUnit *p = as_const(a.s.l.units) + i;
         u.table = p->table; u.head0 = p->head0; u.ncols = p->ncols; u.key0 = p->key0; u.key1 = p->key1; u.row0 = p->row0; u.lim0 = p->lim0; u.slot = p->slot;
         if (unit >= alone) {
