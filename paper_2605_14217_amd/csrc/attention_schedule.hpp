@@ -456,7 +456,10 @@ __device__ __forceinline__ AttnDirect attn_direct(const AttnScheduleArgs &a, int
         const int32_t n = min(a.S, 64);
         cost = (uint32_t)__builtin_amdgcn_readlane(wave_inclusive((int32_t)cost, n), n - 1);
         range = max(a.min_tiles, (int32_t)min(((uint64_t)cost * (uint32_t)a.kv_heads + a.spread - 1) / (uint32_t)a.spread, (uint64_t)INT32_MAX));
-        if (a.fill) {
+        bool wide = false;                                        // of the call's own rows: T and fill count prompt rows that it skips, too
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) wide = wide || is_wide(c);
+        if (a.fill && __any(wide)) {
             const uint64_t work = (uint64_t)cost * (uint32_t)a.kv_heads;
             bool over[ATTN_FILLS] = {};
 #pragma unroll

@@ -55,3 +55,19 @@ def test_very_long_tables(driver):  # noqa: F811
              call(CACHED, MX | BF16, 32, 8, [100] * 2, kv=[1 << 30] * 2, max_keys=1 << 30)]
     got = answers(driver, calls)
     assert all(units <= grid for _, _, _, units, grid, _ in got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_decode_rows_beside_a_prompt_are_cut_as_without_it(driver, dtype):  # noqa: F811
+    """A prompt's rows are in the batch, but not in the call: its tiles are all narrow, for which one full round is not looked for.  40 rows, 8 heads: ranges of 1/256 of all their key tiles."""
+    kv = [1000 + 200 * s for s in range(40)] + [350]
+    (direct, split, merge, got, grid, _), = answers(driver, [call(CACHED, MX | dtype, 32, 8, [1] * 40 + [350], [0] * 40 + [350], kv, 16384)])
+    tiles = [-(-k // 64) for k in kv[:40]]
+    to = -(-sum(tiles) * 8 // 256)
+    assert direct and split and merge and got == sum(-(-n // to) for n in tiles) <= grid
+    # a chunk of ten rows among them is a wide tile
+    kv[39] = 9000
+    (direct, _, _, got, _, _), = answers(driver, [call(CACHED, MX | dtype, 32, 8, [1] * 39 + [10, 350], [0] * 40 + [350], kv, 16384)])
+    tiles[39] = -(-9000 // 64)
+    to = -(-sum(tiles) * 8 // 384)
+    assert direct and got == sum(-(-n // to) for n in tiles)
