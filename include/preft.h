@@ -468,7 +468,8 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
  *
  * 4-bit pages: a number is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6; 32 consecutive numbers of a head share a power of two (the 4-bit format of the OCP Microscaling
  * specification: E2M1 elements, E8M0 scales).  It is the least power 2^e, -125 <= e <= 125, at which the largest of the 32 is below 7; the numbers are rounded to nearest,
- * in the middle to even, and no larger than 6.  So a number is off by at most a fifth of itself or a quarter of the power.  Where one of the 32 is infinite or NaN, all are NaN.  What is
+ * in the middle to even, and no larger than 6.  So a number is off by at most a fifth of itself or a quarter of the power.  Where the largest is 7 * 2^125 or more there is no such power: it is
+ * 2^125 then, and a number above 6 * 2^125 becomes that, off by up to a quarter of itself.  Where one of the 32 is infinite or NaN, all are NaN.  What is
  * rounded is k as preft_kv_append would store it.
  * A cache is n_pages * n_kv_heads * page_size * (head_dim / 2 + head_dim / 32) bytes, one for keys and one for values, 16-byte aligned: page after page, of a page head after head,
  * and of a head first the numbers of its page_size tokens (head_dim / 2 bytes each, two numbers a byte, the first in the low bits; the top bit of the four is the sign, the others are the place in the list

@@ -227,6 +227,35 @@ def test_numbers_on_borders(dtype):
     assert np.isfinite(v).sum() > 0.95 * v.size and np.isnan(v).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_how_far_a_number_is_off(dtype):
+    """At most a fifth of itself or a quarter of its power; from 7 * 2^125 on, where no power puts the largest of the 32 below 7, what is above 6 * 2^125 becomes that: up to a quarter of itself."""
+    print(f"\n[case] how far {dtype}", flush=True)
+    td = DTYPE[dtype]
+    top, gen = 2.0 ** 125, torch.Generator().manual_seed(1)
+    x = torch.randn(64, 128, generator=gen).double() * torch.logspace(-120, 120, 64, 2.0, dtype=torch.float64)[:, None]
+    edge = torch.tensor([top, 6 * top, 6.5 * top, 6.9375 * top, 7 * top, 7.5 * top, torch.finfo(td).max], dtype=torch.float64)
+    x = torch.cat([x, edge[:, None] * (2 * torch.rand(7, 128, generator=gen).double() - 1)])
+    x[64:, ::32] = edge[:, None]
+    x = x.to(td)
+    T = x.shape[0]
+    caches = [preft.new_mx_cache(T // 8 + 1, 1, 8, 128) for _ in "kv"]
+    slot = torch.arange(T, device="cuda")
+    preft.preft_kv_append_mx(*caches, None, None, None, x.cuda(), x.cuda(), slot, None, None, 0)
+    back = [torch.zeros(T, 128, dtype=td, device="cuda") for _ in "kv"]
+    preft.preft_kv_fetch_mx(*back, slot, *caches)
+    x = x.double().view(T, 4, 32)
+    powers = torch.from_numpy(ref.split(caches[0].cpu().numpy(), 128)[1].transpose(0, 2, 1, 3).reshape(-1, 4)[:T].astype(np.float64)) - 127
+    unit, most = 2.0 ** powers[..., None], x.abs().amax(-1, keepdim=True)
+    assert bool((powers <= 125).all()) and bool(((most < 7 * unit) | (most >= 7 * top)).all()) and bool((most >= 7 * top).any())
+    for b in back:
+        off = (b.cpu().double().view(T, 4, 32) - x).abs()
+        usual = (off <= x.abs() / 5) | (off <= unit / 4)
+        cut = (most >= 7 * top) & (x.abs() > 6 * top)
+        assert bool((usual | (cut & (off == x.abs() - 6 * top) & (off < x.abs() / 4 * (1 + 2.0 ** -20)))).all())
+        assert bool(usual.all(2)[:64].all()) and not bool(usual[-1].all())
+
+
 @pytest.mark.parametrize("what", [float("inf"), float("nan")])
 def test_what_is_not_finite_stays_in_its_head(what):
     print(f"\n[case] not finite {what}", flush=True)
