@@ -58,12 +58,9 @@ inline bool rows_meet(const void *p, int64_t ldp, int64_t wp, const void *q, int
 
 inline bool aligned_workspace(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// A launch has fewer than 2^32 threads in a dimension (HIP refuses others): where a row takes a wavefront, calls of more rows than this are several launches.
-constexpr int32_t ROWS_A_LAUNCH = 1 << 25;
-// rows `row` .. of `T` that one of these launches takes
-inline int32_t rows_of_launch(int32_t T, int32_t row) { return T - row < ROWS_A_LAUNCH ? T - row : ROWS_A_LAUNCH; }
-// an array's entry, where there is an array
-template <typename P> P *moved(P *p, int64_t by) { return p ? p + by : p; }
+// Workgroups of kernels whose wavefronts take a row each.  A launch may have fewer than 2^32 threads in a dimension, and of one that asks for more the remainder runs, without an error: the threads
+// stand along y, so that along x only workgroups count, and these are fewer than 2^31 for any number of rows.
+inline dim3 row_threads() { return dim3(1, 256); }
 
 inline int launched() { return hipGetLastError() == hipSuccess ? PREFT_OK : PREFT_EHIP; }
 

@@ -65,7 +65,7 @@ template <typename E, int D, bool HALVES> struct Turn {
 
     __device__ __forceinline__ void init(const HeadsArgs &a, int32_t position)
     {
-        const int j = (threadIdx.x & 63) % H::LANES, half = a.rot / PE / 2;      // the first `half` lanes of a head turn theirs
+        const int j = (threadIdx.y & 63) % H::LANES, half = a.rot / PE / 2;      // the first `half` lanes of a head turn theirs
         turns = j < half;
         lo = 16 * (HALVES && turns ? j : 2 * j);
         hi = 16 * (HALVES && turns ? j + half : 2 * j + 1);
@@ -116,7 +116,7 @@ template <typename E, int D> struct Mx4Put {
 
     static __device__ __forceinline__ void put(gptr_t head, int64_t page_shift, int32_t in, float *x, bool there)
     {
-        const int j = (threadIdx.x & 63) % H::LANES;
+        const int j = (threadIdx.y & 63) % H::LANES;
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
@@ -154,7 +154,8 @@ __device__ __forceinline__ void wave_fence()
 //   17 100 rows of 64 + 8 heads of 128, bf16, 639 MB in and out                            125-128 us, 5.0 TB/s (a copy: 4.8)
 //   37 100 rows of 32 + 8 heads, values beside, keys and values to pages and keys kept     183-186 us, 5.3 TB/s
 //   12 350 rows of 64 + 8 heads, values beside, to 4-bit pages                             107-110 us, 4.4 TB/s
-//   one row of 32 + 8 heads                                                                2.8-3.0 us
+//   one row of 32 + 8 heads                                                                2.8-3.2 us
+// and whole calls of f32 rows, twice the bytes: the first 250 us, 5.1 TB/s, the second 381, 5.2, the third and the fetch of its rows 227, 4.6.
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, int PAGES, bool HALVES>
 __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
     using H = Heads<E, D>;
     constexpr int PE = H::PE;
     __shared__ __align__(16) char lds[PAGES == MX4_PAGES ? 4 * 2048 : 16];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane / H::LANES, j = lane % H::LANES;
+    const int wave = threadIdx.y >> 6, lane = threadIdx.y & 63, h = lane / H::LANES, j = lane % H::LANES;
     const uint32_t task = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + wave)), at = task / (uint32_t)a.splits;
     if (at >= (uint32_t)a.T) return;
     const int32_t row = (int32_t)at, part = (int32_t)(task - at * (uint32_t)a.splits);
@@ -262,8 +263,8 @@ __global__ __launch_bounds__(256) void mx4_fetch_kernel(FetchArgs a)
 {
     using H = Heads<E, D>;
     constexpr int N = 2 * H::PE, SHARE = MX4_BLOCK / N;
-    const int lane = threadIdx.x & 63, h = lane / H::LANES, j = lane % H::LANES;
-    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    const int lane = threadIdx.y & 63, h = lane / H::LANES, j = lane % H::LANES;
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.y >> 6)));
     if (at >= (uint32_t)a.T) return;
     const int32_t row = (int32_t)at;
     const int64_t slot = as_const(a.slot_map)[row];
@@ -290,23 +291,10 @@ __global__ __launch_bounds__(256) void mx4_fetch_kernel(FetchArgs a)
     }
 }
 
-int launch_fetch(const FetchArgs &a, int dtype, int32_t head_dim, hipStream_t st)
-{
-    const dim3 grid((unsigned)(((int64_t)a.T + 3) / 4), 2), block(256);
-    if (dtype == PREFT_BF16) {
-        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 64>), grid, block, 0, st, a);
-    } else {
-        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<float, 128>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((mx4_fetch_kernel<float, 64>), grid, block, 0, st, a);
-    }
-    return launched();
-}
-
 template <int PAGES, bool HALVES>
-int launch_rows(const HeadsArgs &a, int dtype, int32_t head_dim, hipStream_t st)
+int launch_heads(const HeadsArgs &a, int dtype, int32_t head_dim, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((int64_t)a.T * a.splits + 3) / 4)), block(256);
+    const dim3 grid((unsigned)(((int64_t)a.T * a.splits + 3) / 4)), block = row_threads();
     if (dtype == PREFT_BF16) {
         if (head_dim == 128) hipLaunchKernelGGL((heads_kernel<__bf16, 128, PAGES, HALVES>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((heads_kernel<__bf16, 64, PAGES, HALVES>), grid, block, 0, st, a);
@@ -315,21 +303,6 @@ int launch_rows(const HeadsArgs &a, int dtype, int32_t head_dim, hipStream_t st)
         else hipLaunchKernelGGL((heads_kernel<float, 64, PAGES, HALVES>), grid, block, 0, st, a);
     }
     return launched();
-}
-
-template <int PAGES, bool HALVES>
-int launch_heads(const HeadsArgs &call, int dtype, int32_t head_dim, hipStream_t st)
-{
-    int rc = PREFT_OK;
-    for (int64_t row = 0; row < call.T && rc == PREFT_OK; row += ROWS_A_LAUNCH) {
-        HeadsArgs a = call;
-        a.T = rows_of_launch(call.T, (int32_t)row);
-        a.q = moved(call.q, row * call.ldq); a.k = moved(call.k, row * call.ldk); a.v = moved(call.v, row * call.ldv);
-        a.q_out = moved(call.q_out, row * call.ldqo); a.k_out = moved(call.k_out, row * call.ldko);
-        a.positions = moved(call.positions, row); a.slot_map = moved(call.slot_map, row);
-        rc = launch_rows<PAGES, HALVES>(a, dtype, head_dim, st);
-    }
-    return rc;
 }
 
 // Rows that a call writes over its own input do so in place; any other overlap is refused.
@@ -450,15 +423,18 @@ int preft_kv_fetch_mx(void *k, int64_t ldk, void *v, int64_t ldv, int32_t T, int
     for (const Span &o : {Span{k, ((int64_t)(T - 1) * ldk + width) * e}, Span{v, ((int64_t)(T - 1) * ldv + width) * e}})
         if (o.meets({k_cache, cache}) || o.meets({v_cache, cache})) return PREFT_EINVAL;
     FetchArgs a;
-    a.k_cache = (const char *)k_cache; a.v_cache = (const char *)v_cache;
-    a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.kv_heads = n_kv_heads; a.page_shift = shift;
+    a.k = (char *)k; a.v = (char *)v; a.k_cache = (const char *)k_cache; a.v_cache = (const char *)v_cache; a.slot_map = slot_map;
+    a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.T = T; a.kv_heads = n_kv_heads; a.page_shift = shift;
+    const dim3 grid((unsigned)(((int64_t)T + 3) / 4), 2), block = row_threads();
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    for (int64_t row = 0; row < T && rc == PREFT_OK; row += ROWS_A_LAUNCH) {
-        a.T = rows_of_launch(T, (int32_t)row);
-        a.k = (char *)k + row * a.ldk; a.v = (char *)v + row * a.ldv; a.slot_map = slot_map + row;
-        rc = launch_fetch(a, dtype, head_dim, st);
+    if (dtype == PREFT_BF16) {
+        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((mx4_fetch_kernel<__bf16, 64>), grid, block, 0, st, a);
+    } else {
+        if (head_dim == 128) hipLaunchKernelGGL((mx4_fetch_kernel<float, 128>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((mx4_fetch_kernel<float, 64>), grid, block, 0, st, a);
     }
-    return rc;
+    return launched();
 }
 
 }  // extern "C"

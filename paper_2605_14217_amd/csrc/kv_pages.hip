@@ -153,8 +153,8 @@ struct StoreArgs {
 // or with it on the loads too (the store alone 65.5 us, 4.6 TB/s; 71 and 63.8).
 __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    const int lane = threadIdx.y & 63;
+    const int32_t row = __builtin_amdgcn_readfirstlane((int32_t)(blockIdx.x * 4 + (threadIdx.y >> 6)));
     if (row >= a.T) return;
     const int64_t slot = as_const(a.slot_map)[row];
     if (slot < 0 || slot >= a.n_slots) return;
@@ -222,16 +222,11 @@ int preft_kv_store(void *k_cache, void *v_cache, int32_t n_pages, int32_t page_s
         for (const Span &i : in)
             if (o.meets(i)) return PREFT_EINVAL;
     StoreArgs a;
-    a.k_cache = (char *)k_cache; a.v_cache = (char *)v_cache;
-    a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.page_shift = shift; a.heads = n_kv_heads;
+    a.k_cache = (char *)k_cache; a.v_cache = (char *)v_cache; a.k = (const char *)k; a.v = (const char *)v; a.slot_map = slot_map;
+    a.ldk = ldk * e; a.ldv = ldv * e; a.n_slots = (int64_t)n_pages * page_size; a.T = T; a.page_shift = shift; a.heads = n_kv_heads;
     a.head_bytes = (int32_t)(head_dim * e);
-    for (int64_t row = 0; row < T && rc == PREFT_OK; row += ROWS_A_LAUNCH) {
-        a.T = rows_of_launch(T, (int32_t)row);
-        a.k = (const char *)k + row * a.ldk; a.v = (const char *)v + row * a.ldv; a.slot_map = slot_map + row;
-        hipLaunchKernelGGL(kv_store_kernel, dim3((unsigned)((a.T + 3) / 4), 2), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
-        rc = launched();
-    }
-    return rc;
+    hipLaunchKernelGGL(kv_store_kernel, dim3((unsigned)(((int64_t)T + 3) / 4), 2), row_threads(), 0, reinterpret_cast<hipStream_t>(stream), a);
+    return launched();
 }
 
 }  // extern "C"

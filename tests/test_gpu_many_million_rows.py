@@ -1,4 +1,4 @@
-"""Calls of more rows than one launch may have threads for (64 a row, fewer than 2^32 in all): every row is done, those at the borders of the launches among them."""
+"""Calls of more rows than a launch may have threads for along one dimension (64 a row, fewer than 2^32): every row is done."""
 import numpy as np
 import pytest
 import torch
