@@ -21,7 +21,8 @@ template <int D> struct MxTile {
     static constexpr int STEPS = PIECES / 2, BLOCKS = D / 32;
     static constexpr int MINE = D / 64;                            // 16-byte pieces of a key, of 32 numbers each, that a lane of 32 keys has
     // Rows in LDS are further apart than they are long, so that what is read in one cycle comes from all banks: of K, 16 lanes' 16 bytes of as many rows; of V, 64 bytes each
-    // of 4 rows.  (Turning the pieces of a row does it too, but takes a register for every address: with 16-byte pieces at constant distances one is enough, and nothing spills.)
+    // of 4 rows.  (Turning the pieces of a row does it too, but takes a register for every address: with 16-byte pieces at constant distances one is enough.  So nothing spills, but in the kernels of f32
+    // heads of 128, whose three parts of a query are 96 registers: 15 spilled, 44 bytes a lane.)
     static constexpr int K_PITCH = ROW + 16;
     static __device__ __forceinline__ constexpr int v_row(int row) { return row * (ROW + 64) + (row >> 2) * 16; }       // (and what is written, 16 bytes of 16 rows)
     static constexpr int K_TILE = ATTN_KEYS * K_PITCH, V_TILE = ATTN_KEYS * (ROW + 68), LDS = 2 * (K_TILE + V_TILE);
@@ -62,7 +63,8 @@ template <typename E, int PARTS, int STEPS> __device__ __forceinline__ void mx_q
         }
     }
 }
-// two weights likewise: put(part, both)
+// Two weights likewise: put(part, both).  Those of bf16 rows are rounded to bf16, each off by up to 2^-8 of itself, as over bf16 pages: a row's result is as near whatever its pages hold and however wide
+// its unit is.  With a remainder beside them outputs would be off by 0.17 % of their norm, their own rounding, instead of 0.23 %; wide units, which the matrix cores bound, have no time for half as many products again.
 template <int PARTS, typename Put> __device__ __forceinline__ void mx_weights(float x, float y, Put put)
 {
     if constexpr (PARTS == 1) {
@@ -149,8 +151,8 @@ template <typename E, int D> struct MxColumns : AttnColumns<E, D> {
         return s;
     }
 
-    // S^T -> P^T by the m there is, without the largest S, a tenth of a tile's vector instructions: true where a weight may pass 2^8, S^T and m are then to be taken anew.  (Sums that
-    // are NaN stay: so is the result.)
+    // S^T -> P^T by the m there is, without the largest S, a tenth of a tile's vector instructions: true where a weight may pass 2^8, S^T is then to be taken anew, and `exponentials` to look at the largest S.  It
+    // raises m where that is more than 2^8 above; where many are 2^4 to 2^8 above and none is further, m stays, and the next tile is taken twice again.  (Sums that are NaN stay: so is the result.)
     __device__ __forceinline__ bool try_exponentials(f32x16_t (&s)[2], float c)
     {
         float sum = 0.0f;
@@ -401,8 +403,8 @@ __device__ __forceinline__ void mx4_put(lds_t to, u32x4_t numbers, uint32_t powe
 
 // ---------------------------------------------------------------------------------------
 // A unit of more than 32 columns: as in attend_columns, but the tiles of 64 keys come through registers: each thread has 32 numbers of K and 32 of V (heads of 64: of one)
-// of the tile after next on their way while this one's products run.  Four requests' further chunks, 6000 rows over 5000..17 000 tokens, 32 heads over 8 of 128: 867-885 us, 1120-1150 TFLOP/s, 93-96 %
-// of a large matrix product's 1200; before the wavefronts' priorities and the weights without a look for the largest score 999, with them 958, with scalar addresses 900, with reads ordered ahead of the
+// of the tile after next on their way while this one's products run.  Four requests' further chunks, 6000 rows over 5000..17 000 tokens, 32 heads over 8 of 128: 867-895 us with schedule and join, by the card, 1110-1150 TFLOP/s,
+// 92-95 % of a large matrix product's 1200 (keys that all score 2^4 to 2^8 above those of the first tile, so that each tile is taken twice: 1175, all alike 755); before the wavefronts' priorities and the weights without a look for the largest score 999, with them 958, with scalar addresses 900, with reads ordered ahead of the
 // products and rows at a pitch 867 (half of the products of a tile stood waiting for LDS; a K tile further ahead, its products beside the exponentials, took 1040).
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, bool ONE>
@@ -687,9 +689,9 @@ template <typename E, int D> struct MxFewColumns {
 // ---------------------------------------------------------------------------------------
 // A unit of up to 32 columns (C: MxColumns), or up to 16 (MxFewColumns): bound by the bytes of its keys.  The four wavefronts take blocks of 32 keys in turn, AHEAD of them on their way in
 // registers, V through LDS of their own without a barrier, and join their sums at the end.  SOLO: the unit is one wavefront's.
-// 512 rows over 4000 tokens, 32 heads over 8 of 128: 395 us, 5.6 TB/s (reads alone come at up to 6.8); 224 rows over 256..4096 tokens 110 us with their schedule and join, 5.4 TB/s in the kernel.
+// 512 rows over 4000 tokens, 32 heads over 8 of 128: 396 us, 5.65 TB/s; 224 rows over 256..4096 tokens 110 us with their schedule and join, 101-104 of them in the kernel under the profiler, 5.1-5.3 TB/s.
 // Units of 32 columns on 32x32x16 products alone 117.7; powers loaded as bytes, after which a loop waits at its end for all loads, 114.  Four blocks ahead: 129 in pages of 16 (heads of 64: 48 us, two
-// ahead 40; the waits are not for memory).
+// ahead 40, where their bytes would take 14: more loads on their way do not help, and what the time goes to is not known).
 // ---------------------------------------------------------------------------------------
 template <typename E, int D, typename C, int AHEAD, bool SOLO, bool ONE>
 __device__ __forceinline__ void mx_attend_keys(const AttnArgs &a, const AttnUnit &u, int kv_head, lds_t lds, float *join)

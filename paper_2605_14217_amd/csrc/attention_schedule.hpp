@@ -413,8 +413,8 @@ __device__ __forceinline__ int32_t wave_inclusive(int32_t v, int32_t n)
 
 // One full round of workgroups: with a range of 1/512, else 1/384 of all the work the units may be no more than run side by side, though n tiles cut into ranges of 1/spread make
 // n + spread of them at worst.  Half as many again are taken too where the longest tile takes longer than a part and an even share of the work (8 prompts of 100..200 rows over 1000..15 000 tokens,
-// 4-bit pages: 238 us, without it 314).  For calls with wide tiles; the look takes half a microsecond of each workgroup's.  (4-bit pages, 30 requests of 10 rows over 1000..5000 tokens: 65 us, without
-// it 103; 512 rows over 30 000 tokens 237, 266; 20 requests of 20 f32 rows over 2500..5000 tokens 125, 236.)
+// 4-bit pages: 238 us, without it 314).  For calls with wide tiles; the look takes half a microsecond of each workgroup's.  (4-bit pages, 30 requests of 10 rows over 1000..5000 tokens: 57-65 us, without
+// it 103; 512 rows over 30 000 tokens 240, 266; 20 requests of 20 f32 rows over 2500..5000 tokens 117-125, 236.  40 decode rows over 1000..9000 tokens beside a prompt that the call skips: 62.6, with it 64.5.)
 constexpr int ATTN_FILLS = 2;
 __device__ __forceinline__ int32_t fill_range(uint64_t work, int k)
 {
